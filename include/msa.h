@@ -307,6 +307,54 @@ int msa_layers_step(const msa_config_t* cfg, const msa_config_t* attend_cfg, con
                     size_t score_workspace_bytes, void* attend_workspace, size_t attend_workspace_bytes,
                     msa_stream_t caller, msa_stream_t route, msa_stream_t attend, void* fork_event, void* join_event);
 
+/*
+ * From a layer's projections to its attention: norm of every query and key head, rotation to the token's position, and
+ * the append of keys and values to the local cache, in one pass.  For token (b, m) at position p = pos[b][m]:
+ *     y(x, w)_u  = x_u * rsqrt(mean_u x_u^2 + eps) * w_u        (w == NULL: y = x)
+ *     q_out[b][m][h][:]                    = RoPE(y(q[b][m][h][:], q_weight), p)
+ *     Kloc[b][g][p - local_pos0][:]        = RoPE(y(k[b][m][g][:], k_weight), p)
+ *     Vloc[b][g][p - local_pos0][:]        = v[b][m][g][:]
+ * in fp32, rounded to bf16 once.  rotate == 0 leaves the rotation out: then q_out and Kloc are what msa_sparse_attend and
+ * msa_build_routing_keys take, which rotate by themselves; rotate == 1 gives what msa_window_attend and
+ * msa_sparse_attend4 take.  With documents in the place of sequences (B documents, M = G tokens, positions 0..G-1,
+ * Lloc = G) Kloc, Vloc are a bank.  A token of negative position is padding: nothing of it is written.  A position
+ * outside [local_pos0, local_pos0 + Lloc) has no row in the cache: its query alone is written.  Rows that no token of the
+ * call is at keep what they held.  Tokens of one sequence have positions of their own; of a row that two of them claim the
+ * contents are undefined (that row's alone).  Reads n_q_heads, n_kv_heads, head_dim and rope_base of cfg.
+ *   q, k, v   in   bf16, heads and dims dense ([Hq][d], [Hkv][d]), token (b, m) at (b*M + m) * stride elements: a fused
+ *                  projection is read where it lies.  Strides are multiples of 8, at least the heads' elements.
+ *                  q may be NULL with q_out (no queries), k with Kloc, v with Vloc; not all three
+ *   weights   in   bf16 [d] or NULL
+ *   pos       in   int32 [B][M]
+ *   q_out     out  bf16 [B][M][Hq][d]
+ *   Kloc,Vloc out  bf16 [B][Hkv][Lloc][d]
+ * The outputs overlap neither each other nor the inputs.
+ */
+int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const void* v, int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                    int32_t rotate, const int32_t* pos, int32_t B, int32_t M, void* q_out, void* Kloc, void* Vloc,
+                    int32_t Lloc, int32_t local_pos0, msa_stream_t stream);
+
+/*
+ * A bank in four bits.  A row of d elements is d/32 blocks of 32; a block is a byte e, the scale 2^(e - 127), and 32 codes
+ * of four bits, sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7; bit 3 is the sign):
+ *     e    = the smallest with max|x| <= 7 * 2^(e - 127), but 2 at least and 252 at most
+ *     code = x / 2^(e - 127) rounded to nearest, ties to the even code, 6 at most
+ * so that nothing short of 2^127 is off by more than half a step.  Exact arithmetic: the same bits everywhere.  Half of a
+ * byte per element and 1/32 of one: 0.266 of bf16.
+ *   K4, V4    uint8 [N][Hkv][G][d/2]    dim 2i in the low half of byte i, dim 2i + 1 in the high half
+ *   K4s, V4s  uint8 [N][Hkv][G][d/32]   the bytes e
+ * msa_pack_kv4 packs documents [doc_begin, doc_begin + doc_count) of the bank K, V bf16 [N][Hkv][G][d], any G.  Keys go in
+ * position-encoded: with cfg->bank_keys_rotated they are taken as stored, without it they are turned by their positions
+ * 0..G-1 (in fp32) first.  With cfg->doc_lens rows past a document's length are not read and become zeros.
+ * K or V may be NULL with its two outputs.  msa_unpack_kv4 writes what the codes stand for (exact in bf16).
+ * The scale bytes of msa_unpack_kv4 and msa_sparse_attend4 lie in 2..252, as msa_pack_kv4 writes them.
+ */
+int msa_pack_kv4(const msa_config_t* cfg, const void* K, const void* V, int32_t doc_begin, int32_t doc_count, void* K4,
+                 void* K4s, void* V4, void* V4s, msa_stream_t stream);
+int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, const void* V4, const void* V4s,
+                   int32_t doc_begin, int32_t doc_count, void* K, void* V, msa_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,8 @@ EXPORTS = ("msa_version", "msa_status_string", "msa_routing_keys_bytes", "msa_in
            "msa_pooled_bank_bytes", "msa_score_topk_workspace_bytes",
            "msa_sparse_attend_workspace_bytes", "msa_build_routing_keys", "msa_pool_kv", "msa_score_topk",
            "msa_sparse_attend", "msa_fetch_slots", "msa_fetch_selected",
-           "msa_noalloc_scratch_bytes", "msa_score_topk_noalloc", "msa_layers_step")
+           "msa_noalloc_scratch_bytes", "msa_score_topk_noalloc", "msa_layers_step", "msa_norm_rotate", "msa_pack_kv4",
+           "msa_unpack_kv4")
 
 
 class MsaConfig(ctypes.Structure):
@@ -132,6 +133,14 @@ def load_library():
                                       vp, vp, sz, vp]
     lib.msa_layers_step.restype = ctypes.c_int
     lib.msa_layers_step.argtypes = [cfgp, cfgp, ctypes.POINTER(MsaLayer)] + [i32] * 3 + [vp, vp, sz, vp, sz] + [vp] * 5
+    i64 = ctypes.c_int64
+    lib.msa_norm_rotate.restype = ctypes.c_int
+    lib.msa_norm_rotate.argtypes = [cfgp, vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_float, i32, vp, i32, i32, vp, vp, vp,
+                                    i32, i32, vp]
+    lib.msa_pack_kv4.restype = ctypes.c_int
+    lib.msa_pack_kv4.argtypes = [cfgp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.msa_unpack_kv4.restype = ctypes.c_int
+    lib.msa_unpack_kv4.argtypes = [cfgp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -354,3 +363,138 @@ def msa_fetch_selected(cfg, K_host, V_host, idx, B, M, K_stage=None, V_stage=Non
     _check(rc, "msa_fetch_selected")
     scfg = cfg.replace(n_docs=n_slots, doc_lens=lens_stage if cfg.doc_lens_tensor is not None else None)
     return K_stage, V_stage, idx_stage, scfg
+
+
+# ---- around a layer's projections, the local cache and a bank in four bits --------------------------------------------
+def _need_shape(t, dtype, shape, name):
+    _need(t, dtype, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _same_device(first, *tensors):
+    for t in tensors:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device} in one call")
+
+
+def _call(name, device, *args):
+    """The entry point `name`, with the tensors' device as the current one."""
+    fn = getattr(load_library(), name)
+    if device.index is None or device.index == torch.cuda.current_device():
+        rc = fn(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args)
+    _check(rc, name)
+
+
+def _token_stride(t, heads, d, name):
+    """Elements from one token of [B][M][heads][d] to the next; a view of a fused projection is taken as it lies."""
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 4 and t.shape[2] == heads and t.shape[3] == d):
+        raise ValueError(f"{name}: expected a CUDA tensor of torch.bfloat16, [B][M][{heads}][{d}]")
+    B, M = t.shape[:2]
+    sb, sm, sh, sd = t.stride()
+    step = sm if M > 1 else (sb if B > 1 else heads * d)
+    if sd != 1 or (heads > 1 and sh != d) or (B > 1 and M > 1 and sb != M * sm):
+        raise ValueError(f"{name}: heads and dims have to be dense, and tokens the same distance apart")
+    return step
+
+
+def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None, eps=1e-6, rotate=True, local_pos0=0,
+                    q_out=None, stream=None):
+    """q bf16 [B][M][Hq][d], k, v bf16 [B][M][Hkv][d] (views of a fused projection are read where they lie), pos int32
+    [B][M] -> q_out bf16 [B][M][Hq][d]; keys and values go into rows pos - local_pos0 of Kloc, Vloc bf16
+    [B][Hkv][Lloc][d].  q, or k with Kloc, or v with Vloc, may be None.  Weights bf16 [d], None for no norm."""
+    Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    src = next((t for t in (q, k, v) if t is not None), None)
+    if src is None or src.dim() != 4:
+        raise ValueError("msa_norm_rotate: expected q, k or v as [B][M][heads][d]")
+    B, M = src.shape[:2]
+    strides = [0 if t is None else _token_stride(t, h, d, n)
+               for t, h, n in ((q, Hq, "q"), (k, Hkv, "k"), (v, Hkv, "v"))]
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        if t is not None and tuple(t.shape[:2]) != (B, M):
+            raise ValueError(f"{n}: expected [{B}][{M}] tokens")
+    if (k is None) != (Kloc is None) or (v is None) != (Vloc is None) or (q is None and q_out is not None):
+        raise ValueError("msa_norm_rotate: k comes with Kloc, v with Vloc, q_out with q")
+    _need_shape(pos, torch.int32, (B, M), "pos")
+    cache = Kloc if Kloc is not None else Vloc
+    Lloc = 0 if cache is None else cache.shape[2]
+    for t, n in ((Kloc, "Kloc"), (Vloc, "Vloc")):
+        if t is not None:
+            _need_shape(t, torch.bfloat16, (B, Hkv, Lloc, d), n)
+    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None:
+            _need_shape(t, torch.bfloat16, (d,), n)
+    if q is not None and q_out is None:
+        q_out = torch.empty((B, M, Hq, d), dtype=torch.bfloat16, device=q.device)
+    if q is not None:
+        _need_shape(q_out, torch.bfloat16, (B, M, Hq, d), "q_out")
+    _same_device(src, q, k, v, pos, Kloc, Vloc, q_weight, k_weight, q_out)
+    _call("msa_norm_rotate", src.device, ctypes.byref(cfg), _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
+          strides[2], _ptr(q_weight), _ptr(k_weight), eps, int(bool(rotate)), _ptr(pos), B, M, _ptr(q_out),
+          _ptr(Kloc), _ptr(Vloc), Lloc, local_pos0, _stream(stream, src.device))
+    return q_out
+
+
+def alloc_kv4(cfg, device="cuda"):
+    """(K4, K4s, V4, V4s) of a bank in four bits: codes uint8 [N][Hkv][G][d/2], scale bytes uint8 [N][Hkv][G][d/32]."""
+    rows = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len)
+    return tuple(torch.empty(rows + (cfg.head_dim // n,), dtype=torch.uint8, device=device) for n in (2, 32, 2, 32))
+
+
+def _need_kv4(cfg, bank):
+    rows = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len)
+    for t, n, name in zip(bank, (2, 32, 2, 32), ("K4", "K4s", "V4", "V4s")):
+        if t is not None:
+            _need_shape(t, torch.uint8, rows + (cfg.head_dim // n,), name)
+
+
+def msa_pack_kv4(cfg, K, V, doc_begin=0, doc_count=None, bank=None, stream=None):
+    """K, V bf16 [N][Hkv][G][d] -> bank (K4, K4s, V4, V4s) for documents [doc_begin, doc_begin + doc_count).  K or V may be
+    None: that half is left as it is.  Keys are turned by their positions unless cfg.bank_keys_rotated."""
+    src = K if K is not None else V
+    if src is None:
+        raise ValueError("msa_pack_kv4: K and V are both None")
+    shape = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len, cfg.head_dim)
+    for t, n in ((K, "K"), (V, "V")):
+        if t is not None:
+            _need_shape(t, torch.bfloat16, shape, n)
+    if doc_count is None:
+        doc_count = cfg.n_docs - doc_begin
+    if bank is None:
+        bank = alloc_kv4(cfg, src.device)
+    _need_kv4(cfg, bank)
+    _same_device(src, K, V, *bank)
+    out = [None if (K if i < 2 else V) is None else t for i, t in enumerate(bank)]
+    _call("msa_pack_kv4", src.device, ctypes.byref(cfg), _ptr(K), _ptr(V), doc_begin, doc_count, *map(_ptr, out),
+          _stream(stream, src.device))
+    return bank
+
+
+def msa_unpack_kv4(cfg, bank, doc_begin=0, doc_count=None, K=None, V=None, stream=None):
+    """What bank = (K4, K4s, V4, V4s) stands for -> (K, V) bf16 [N][Hkv][G][d], documents [doc_begin, doc_begin +
+    doc_count) of it.  K4 and K4s, or V4 and V4s, may be None: that half comes back as None."""
+    _need_kv4(cfg, bank)
+    if (bank[0] is None) != (bank[1] is None) or (bank[2] is None) != (bank[3] is None):
+        raise ValueError("msa_unpack_kv4: codes come with their scale bytes")
+    src = bank[0] if bank[0] is not None else bank[2]
+    if src is None:
+        raise ValueError("msa_unpack_kv4: the bank is empty")
+    shape = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len, cfg.head_dim)
+    out = []
+    for t, codes, n in ((K, bank[0], "K"), (V, bank[2], "V")):
+        if codes is None:
+            t = None
+        elif t is None:
+            t = torch.empty(shape, dtype=torch.bfloat16, device=src.device)
+        else:
+            _need_shape(t, torch.bfloat16, shape, n)
+        out.append(t)
+    if doc_count is None:
+        doc_count = cfg.n_docs - doc_begin
+    _same_device(src, *bank, *out)
+    _call("msa_unpack_kv4", src.device, ctypes.byref(cfg), *map(_ptr, bank), doc_begin, doc_count, *map(_ptr, out),
+          _stream(stream, src.device))
+    return tuple(out)

@@ -376,4 +376,84 @@ int msa_layers_step(const msa_config_t* cfg, const msa_config_t* attend_cfg, con
   return rc;
 }
 
+int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const void* v, int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                    int32_t rotate, const int32_t* pos, int32_t B, int32_t M, void* q_out, void* Kloc, void* Vloc,
+                    int32_t Lloc, int32_t local_pos0, msa_stream_t stream) {
+  Dims dm;
+  const int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (pos == nullptr || (q == nullptr && k == nullptr && v == nullptr)) return MSA_ERR_INVALID_ARG;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (Kloc == nullptr) || (v == nullptr) != (Vloc == nullptr))
+    return MSA_ERR_INVALID_ARG;
+  if (B < 1 || M < 1 || Lloc < 0 || local_pos0 < 0 || (rotate != 0 && rotate != 1)) return MSA_ERR_INVALID_ARG;
+  if ((q_weight != nullptr || k_weight != nullptr) && !(eps > 0.f && eps < INFINITY)) return MSA_ERR_INVALID_ARG;
+  const int64_t nq = (int64_t)dm.Hq * dm.d, nk = (int64_t)dm.Hkv * dm.d;
+  if ((q != nullptr && q_stride < nq) || (k != nullptr && k_stride < nk) || (v != nullptr && v_stride < nk))
+    return MSA_ERR_INVALID_ARG;
+  if ((int64_t)B * M > (1 << 28) || (int64_t)local_pos0 + Lloc > INT32_MAX) return MSA_ERR_UNSUPPORTED;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_weight) || misaligned(k_weight) ||
+      misaligned(q_out) || misaligned(Kloc) || misaligned(Vloc) || misaligned4(pos) ||
+      (q != nullptr && q_stride % 8 != 0) || (k != nullptr && k_stride % 8 != 0) || (v != nullptr && v_stride % 8 != 0))
+    return MSA_ERR_MISALIGNED;
+  NormArgs a = {};
+  a.q = (const uint16_t*)q;
+  a.k = (const uint16_t*)k;
+  a.v = (const uint16_t*)v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.qw = (const uint16_t*)q_weight;
+  a.kw = (const uint16_t*)k_weight;
+  a.pos = pos;
+  a.q_out = (uint16_t*)q_out;
+  a.Kloc = (uint16_t*)Kloc;
+  a.Vloc = (uint16_t*)Vloc;
+  a.BM = (long long)B * M;
+  a.M = M;
+  a.Lloc = Lloc;
+  a.pos0 = local_pos0;
+  a.rotate = rotate;
+  a.eps = eps;
+  return launch_norm_rotate(dm, a, (hipStream_t)stream);
+}
+
+int msa_pack_kv4(const msa_config_t* cfg, const void* K, const void* V, int32_t doc_begin, int32_t doc_count, void* K4,
+                 void* K4s, void* V4, void* V4s, msa_stream_t stream) {
+  Dims dm;
+  int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (K == nullptr && V == nullptr) return MSA_ERR_INVALID_ARG;
+  if ((K == nullptr) != (K4 == nullptr) || (K == nullptr) != (K4s == nullptr) || (V == nullptr) != (V4 == nullptr) ||
+      (V == nullptr) != (V4s == nullptr))
+    return MSA_ERR_INVALID_ARG;
+  if (doc_begin < 0 || doc_count < 0 || (int64_t)doc_begin + doc_count > dm.N) return MSA_ERR_INVALID_ARG;
+  if (misaligned(K) || misaligned(V) || misaligned(K4) || misaligned(K4s) || misaligned(V4) || misaligned(V4s) ||
+      misaligned4(dm.lens))
+    return MSA_ERR_MISALIGNED;
+  if (K != nullptr) {
+    rc = launch_pack4(dm, K, doc_begin, doc_count, K4, K4s, cfg->bank_keys_rotated == 0, (hipStream_t)stream);
+    if (rc != MSA_OK) return rc;
+  }
+  return V != nullptr ? launch_pack4(dm, V, doc_begin, doc_count, V4, V4s, false, (hipStream_t)stream) : MSA_OK;
+}
+
+int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, const void* V4, const void* V4s,
+                   int32_t doc_begin, int32_t doc_count, void* K, void* V, msa_stream_t stream) {
+  Dims dm;
+  int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (K == nullptr && V == nullptr) return MSA_ERR_INVALID_ARG;
+  if ((K != nullptr && (K4 == nullptr || K4s == nullptr)) || (V != nullptr && (V4 == nullptr || V4s == nullptr)))
+    return MSA_ERR_INVALID_ARG;
+  if (doc_begin < 0 || doc_count < 0 || (int64_t)doc_begin + doc_count > dm.N) return MSA_ERR_INVALID_ARG;
+  if (misaligned(K) || misaligned(V) || misaligned(K4) || misaligned(K4s) || misaligned(V4) || misaligned(V4s))
+    return MSA_ERR_MISALIGNED;
+  if (K != nullptr) {
+    rc = launch_unpack4(dm, K4, K4s, doc_begin, doc_count, K, (hipStream_t)stream);
+    if (rc != MSA_OK) return rc;
+  }
+  return V != nullptr ? launch_unpack4(dm, V4, V4s, doc_begin, doc_count, V, (hipStream_t)stream) : MSA_OK;
+}
+
 }  // extern "C"

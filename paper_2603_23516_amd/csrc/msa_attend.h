@@ -15,6 +15,10 @@ struct RopeTheta {
   float2 e16[kMaxHalf];  // (cos, sin)(16 theta_u)
 };
 
+struct NormTheta {
+  double th[kMaxHalf];
+};
+
 struct AttendArgs {
   const uint16_t* q;     // [BM][Hq][D]
   const uint16_t* K;     // [N][Hkv][G][D]
@@ -42,6 +46,9 @@ struct AttendArgs {
   float* final_lse;
   int lin_per, lin_total;  // decode kernel, linear split: steps per workgroup, steps in all; 0: the grid says it
 };
+
+// The table of a (base, d), kept per host thread (msa_attend.hip).
+const RopeTheta& rope_table(float base, int d);
 
 // Many tokens with selections of their own, document by document (msa_attend_docs.hip): one window of tokens.
 struct DocsArgs {

@@ -965,7 +965,7 @@ AttendPlan plan_attend(const Dims& dm, int B, int M, int k, int Lloc, int bank_k
 
 // The angles of a (base, d): a thread keeps the last table it made (64 powers and 256 sines and cosines are 3 us of host
 // time, a third of a small call's).
-static const RopeTheta& rope_table(float base, int d) {
+const RopeTheta& rope_table(float base, int d) {
   static thread_local RopeTheta th;
   static thread_local float th_base = 0.f;
   static thread_local int th_d = 0;

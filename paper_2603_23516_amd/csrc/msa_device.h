@@ -112,6 +112,16 @@ __device__ __forceinline__ void split_pack_bf16(float x0, float x1, uint32_t& hi
   lo_w = pack_bf16(x0 - bf16_lo(hi_w), x1 - bf16_hi(hi_w));
 }
 
+// Eight four-bit codes (the first in the lowest bits) times a power of two, as bf16.
+__device__ __forceinline__ uint4 fp4x8_to_bf16(uint32_t c, float s) {
+  uint4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+  return r;
+}
+
 __device__ __forceinline__ bf16x8_t as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8_t, v); }
 
 // D(16x16, fp32) += A(16x32, bf16) * B(32x16, bf16).

@@ -191,6 +191,26 @@ int launch_fetch(const Dims& dm, const void* K_dev_view, const void* V_dev_view,
                  long long n_rows, int k, void* K_stage, void* V_stage, int32_t* idx_stage,
                  int32_t* lens_stage, hipStream_t st);
 
+// Head norms and rotation (msa_norm.hip).
+struct NormArgs {
+  const uint16_t *q, *k, *v;            // rows of a token, null = none of them
+  long long q_stride, k_stride, v_stride;  // elements from one token to the next
+  const uint16_t *qw, *kw;              // [D] or null: no norm
+  const int32_t* pos;                   // [BM]
+  uint16_t *q_out, *Kloc, *Vloc;
+  long long BM;
+  int M, Hq, Hkv, Lloc, pos0, rotate;
+  float eps;
+  int turns_q, turns_k, turns, shares;  // groups of heads a wave takes at a time; waves that share a token
+};
+int launch_norm_rotate(const Dims& dm, NormArgs a, hipStream_t st);
+
+// A bank in four bits (msa_kv4.hip).
+int launch_pack4(const Dims& dm, const void* X, int doc_begin, int doc_count, void* codes, void* scales, bool rotate,
+                 hipStream_t st);
+int launch_unpack4(const Dims& dm, const void* codes, const void* scales, int doc_begin, int doc_count, void* X,
+                   hipStream_t st);
+
 inline size_t round_up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // A 48-bit non-zero value that differs from call to call (clock ticks through a 64-bit mixer): the tag of the

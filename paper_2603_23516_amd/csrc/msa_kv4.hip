@@ -1,0 +1,139 @@
+// msa_pack_kv4, msa_unpack_kv4: a bank's keys and values in four bits.
+//
+// A row of d elements is d/32 blocks of 32.  A block has one power of two s = 2^(e - 127), held as the byte e, and 32 codes of
+// four bits (sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6), the format that gfx950's conversions
+// (v_cvt_scalef32_pk_*_fp4) take apart for nothing.  s is the smallest with max|x| <= 7 s: 7 rounds to 6, so that no element
+// is off by more than half the step at its place, and all of it is exact arithmetic (a shift of the exponent and one rounding
+// to nearest, ties to even), the same on every machine.  e stays in 2 .. 252, where every value is a normal bf16 number;
+// beyond 2^125 * 6 values saturate.
+//
+// Both are streams: 2 bytes read and 0.53 written per element, or the other way round.  A lane takes eight elements (one 16-byte
+// access in bf16, 4 bytes of codes); the block's maximum comes from the quad of lanes that share it.
+#include "msa_attend.h"
+
+namespace msa {
+
+__device__ __forceinline__ uint32_t quad_max_u(uint32_t x) {
+  uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kDppXor1, 0xf, 0xf, false);
+  x = x > y ? x : y;
+  y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kDppXor2, 0xf, 0xf, false);
+  return x > y ? x : y;
+}
+
+// The scale byte of a block from the bits of its largest magnitude (fp32): 1.f * 2^x <= 1.75 * 2^(k + 2) decides.
+__device__ __forceinline__ int scale_byte(uint32_t amax_bits) {
+  int e = (int)(amax_bits >> 23) - 2 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return e < 2 ? 2 : (e > 252 ? 252 : e);
+}
+
+// ROT: keys that are not position-encoded yet are turned by their position in the document before they are rounded.
+template <int D, bool ROT>
+__global__ __launch_bounds__(256) void pack4_kernel(const uint16_t* __restrict__ X, uint8_t* __restrict__ codes,
+                                                    uint8_t* __restrict__ scales, const int32_t* __restrict__ lens,
+                                                    int doc_begin, long long n_rows, int Hkv, int G, NormTheta th) {
+  constexpr int LPR = D / 8;          // lanes per row
+  constexpr int RPB = 256 / LPR;      // rows per workgroup and turn
+  const int lr = threadIdx.x % LPR;
+  const long long row0 = (long long)doc_begin * Hkv * G;
+  for (long long r = (long long)blockIdx.x * RPB + threadIdx.x / LPR; r < n_rows; r += (long long)gridDim.x * RPB) {
+    const long long row = row0 + r;
+    bool live = true;
+    int t = 0;
+    if (ROT || lens != nullptr) {
+      const long long slab = row / G;
+      t = (int)(row - slab * G);
+      if (lens != nullptr) {
+        int len = lens[slab / Hkv];
+        len = len < 1 ? 1 : (len > G ? G : len);
+        live = t < len;
+      }
+    }
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (live) x = *reinterpret_cast<const uint4*>(X + row * D + 8 * lr);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+    if (ROT) {
+      const bool second = lr >= LPR / 2;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float o = __shfl_xor(f[j], LPR / 2, 64);
+        const float2 c = cis_pos(t, th.th[8 * (lr & (LPR / 2 - 1)) + j]);
+        f[j] = f[j] * c.x + (second ? o : -o) * c.y;
+      }
+    }
+    uint32_t amax = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t m = __float_as_uint(f[j]) & 0x7fffffffu;
+      amax = m > amax ? m : amax;
+    }
+    const int e = scale_byte(quad_max_u(amax));
+    const float s = __uint_as_float((uint32_t)e << 23);
+    uint32_t c4 = 0;
+    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[0], f[1], s, 0);
+    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[2], f[3], s, 1);
+    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[4], f[5], s, 2);
+    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[6], f[7], s, 3);
+    *reinterpret_cast<uint32_t*>(codes + row * (D / 2) + 4 * lr) = c4;
+    if ((lr & 3) == 0) scales[row * (D / 32) + lr / 4] = (uint8_t)e;
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void unpack4_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                      uint16_t* __restrict__ X, long long row0, long long n_rows) {
+  constexpr int LPR = D / 8;
+  constexpr int RPB = 256 / LPR;
+  const int lr = threadIdx.x % LPR;
+  for (long long r = (long long)blockIdx.x * RPB + threadIdx.x / LPR; r < n_rows; r += (long long)gridDim.x * RPB) {
+    const long long row = row0 + r;
+    const uint32_t c4 = *reinterpret_cast<const uint32_t*>(codes + row * (D / 2) + 4 * lr);
+    const float s = __uint_as_float((uint32_t)scales[row * (D / 32) + lr / 4] << 23);
+    *reinterpret_cast<uint4*>(X + row * D + 8 * lr) = fp4x8_to_bf16(c4, s);
+  }
+}
+
+static unsigned stream_blocks(long long n_rows, int rows_per_block) {
+  const long long n = (n_rows + rows_per_block - 1) / rows_per_block;
+  return (unsigned)(n < 1 ? 1 : (n > 16384 ? 16384 : n));
+}
+
+int launch_pack4(const Dims& dm, const void* X, int doc_begin, int doc_count, void* codes, void* scales, bool rotate,
+                 hipStream_t st) {
+  const long long n_rows = (long long)doc_count * dm.Hkv * dm.G;
+  if (n_rows == 0) return MSA_OK;
+  NormTheta th = {};
+  if (rotate) {
+    const RopeTheta& table = rope_table(dm.base, dm.d);
+    for (int u = 0; u < kMaxHalf; ++u) th.th[u] = table.th[u];
+  }
+  const dim3 grid(stream_blocks(n_rows, 256 / (dm.d / 8)));
+#define MSA_PACK4(DD, RR)                                                                                             \
+  hipLaunchKernelGGL((pack4_kernel<DD, RR>), grid, dim3(256), 0, st, (const uint16_t*)X, (uint8_t*)codes, (uint8_t*)scales, \
+                     dm.lens, doc_begin, n_rows, dm.Hkv, dm.G, th)
+  if (dm.d == 128) {
+    if (rotate) MSA_PACK4(128, true); else MSA_PACK4(128, false);
+  } else {
+    if (rotate) MSA_PACK4(64, true); else MSA_PACK4(64, false);
+  }
+#undef MSA_PACK4
+  return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
+}
+
+int launch_unpack4(const Dims& dm, const void* codes, const void* scales, int doc_begin, int doc_count, void* X,
+                   hipStream_t st) {
+  const long long n_rows = (long long)doc_count * dm.Hkv * dm.G, row0 = (long long)doc_begin * dm.Hkv * dm.G;
+  if (n_rows == 0) return MSA_OK;
+  const dim3 grid(stream_blocks(n_rows, 256 / (dm.d / 8)));
+  if (dm.d == 128)
+    hipLaunchKernelGGL(unpack4_kernel<128>, grid, dim3(256), 0, st, (const uint8_t*)codes, (const uint8_t*)scales,
+                       (uint16_t*)X, row0, n_rows);
+  else
+    hipLaunchKernelGGL(unpack4_kernel<64>, grid, dim3(256), 0, st, (const uint8_t*)codes, (const uint8_t*)scales,
+                       (uint16_t*)X, row0, n_rows);
+  return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
+}
+
+}  // namespace msa
