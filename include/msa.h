@@ -355,6 +355,57 @@ int msa_pack_kv4(const msa_config_t* cfg, const void* K, const void* V, int32_t 
 int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, const void* V4, const void* V4s,
                    int32_t doc_begin, int32_t doc_count, void* K, void* V, msa_stream_t stream);
 
+/*
+ * Attention over the local cache alone, for the layers that do not route: a sliding window of `window` tokens and the first
+ * `sinks` tokens, which stay visible.  Queries and keys carry their positions (msa_norm_rotate with rotate = 1).  Cache row t
+ * is the token at position local_pos0 + t; with p = q_pos[b][m] - local_pos0 token (b, m) sees the rows
+ *     t <= p, t < Lloc, and (p - t < window or t < sinks)
+ *     out[b][m][h][:] = softmax_t( q[b][m][h][:] . Kloc[b][g][t][:] / sqrt(d) ) . Vloc[b][g][t][:]
+ *     lse[b][m][h]    = log sum_t exp( ... )        (natural log; -inf and out = 0 if no row is seen, as with q_pos < local_pos0:
+ *                                                    the way to mark the padding of a batch)
+ * Positions may come in any order; tokens that the caller appends later lie behind q_pos and are not read.  A row up to the
+ * largest position of a sequence's tokens holds numbers, seen or not; what rows behind it hold has no effect.
+ *   q         in   bf16 [B][M][Hq][d]
+ *   Kloc,Vloc in   bf16 [B][Hkv][Lloc][d]
+ *   window         >= 1; Lloc or more: causal attention;  sinks >= 0
+ *   q_pos     in   int32 [B][M]
+ *   out       out  bf16 [B][M][Hq][d]
+ *   lse       out  fp32 [B][M][Hq], may be NULL
+ *   workspace      >= msa_window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks); contents undefined on entry/exit
+ * Scores, their maximum and sum and the outputs are accumulated in fp32.  With few tokens the softmax weights are carried as
+ * bf16 (hi, lo) pairs, with many as bf16.  Reads n_q_heads, n_kv_heads and head_dim of cfg.
+ */
+size_t msa_window_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
+                                         int32_t sinks);
+int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kloc, const void* Vloc,
+                      int32_t Lloc, int32_t local_pos0, int32_t window, int32_t sinks, const int32_t* q_pos, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, msa_stream_t stream);
+
+/*
+ * msa_sparse_attend over a bank in four bits (msa_pack_kv4).  Queries, bank keys and local keys carry their positions already
+ * (msa_norm_rotate with rotate = 1, msa_pack_kv4), and nothing is turned here:
+ *     keys of (b, m), KV group g:  every row p < G (p < doc_lens[i] with cfg->doc_lens) of every document idx[b][m][g][j] in
+ *                                  [0, N), and every local row t < Lloc with local_pos0 + t <= q_pos[b][m]
+ *     out, lse                     softmax over them with scale 1/sqrt(d), as in msa_sparse_attend
+ * Selections, select_scope, token_pool, doc_lens, pads and documents listed twice are read as msa_sparse_attend reads them;
+ * any doc_len is served; k * G <= 2^28.  cfg->bank_keys_rotated is not read.  Local rows up to the largest position of a
+ * sequence's tokens hold numbers.
+ *   q         in   bf16 [B][M][Hq][d]
+ *   K4, K4s, V4, V4s  in  as msa_pack_kv4 writes them
+ *   idx       in   int32 [B][M'][S][k]
+ *   Kloc,Vloc in   bf16 [B][Hkv][Lloc][d]; may be NULL iff Lloc == 0
+ *   q_pos     in   int32 [B][M]
+ *   out       out  bf16 [B][M][Hq][d]
+ *   lse       out  fp32 [B][M][Hq], may be NULL
+ *   workspace      >= msa_sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc); with token_pool = 1 and M >= 8 it holds the
+ *                  selected documents in bf16, B * Hkv * k * G * d * 4 bytes
+ */
+size_t msa_sparse_attend4_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t k, int32_t Lloc);
+int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* K4, const void* K4s,
+                       const void* V4, const void* V4s, const int32_t* idx, int32_t k, const void* Kloc, const void* Vloc,
+                       int32_t Lloc, int32_t local_pos0, const int32_t* q_pos, void* out, float* lse, void* workspace,
+                       size_t workspace_bytes, msa_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

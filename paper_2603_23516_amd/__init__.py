@@ -22,7 +22,8 @@ EXPORTS = ("msa_version", "msa_status_string", "msa_routing_keys_bytes", "msa_in
            "msa_sparse_attend_workspace_bytes", "msa_build_routing_keys", "msa_pool_kv", "msa_score_topk",
            "msa_sparse_attend", "msa_fetch_slots", "msa_fetch_selected",
            "msa_noalloc_scratch_bytes", "msa_score_topk_noalloc", "msa_layers_step", "msa_norm_rotate", "msa_pack_kv4",
-           "msa_unpack_kv4")
+           "msa_unpack_kv4", "msa_window_attend_workspace_bytes", "msa_window_attend",
+           "msa_sparse_attend4_workspace_bytes", "msa_sparse_attend4")
 
 
 class MsaConfig(ctypes.Structure):
@@ -141,6 +142,14 @@ def load_library():
     lib.msa_pack_kv4.argtypes = [cfgp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
     lib.msa_unpack_kv4.restype = ctypes.c_int
     lib.msa_unpack_kv4.argtypes = [cfgp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.msa_window_attend_workspace_bytes.restype = sz
+    lib.msa_window_attend_workspace_bytes.argtypes = [cfgp] + [i32] * 5
+    lib.msa_window_attend.restype = ctypes.c_int
+    lib.msa_window_attend.argtypes = [cfgp, vp, i32, i32, vp, vp] + [i32] * 4 + [vp, vp, vp, vp, sz, vp]
+    lib.msa_sparse_attend4_workspace_bytes.restype = sz
+    lib.msa_sparse_attend4_workspace_bytes.argtypes = [cfgp] + [i32] * 4
+    lib.msa_sparse_attend4.restype = ctypes.c_int
+    lib.msa_sparse_attend4.argtypes = [cfgp, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -498,3 +507,68 @@ def msa_unpack_kv4(cfg, bank, doc_begin=0, doc_count=None, K=None, V=None, strea
     _call("msa_unpack_kv4", src.device, ctypes.byref(cfg), *map(_ptr, bank), doc_begin, doc_count, *map(_ptr, out),
           _stream(stream, src.device))
     return tuple(out)
+
+
+def window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks=0):
+    return load_library().msa_window_attend_workspace_bytes(ctypes.byref(cfg), B, M, Lloc, window, sinks)
+
+
+def sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc):
+    return load_library().msa_sparse_attend4_workspace_bytes(ctypes.byref(cfg), B, M, k, Lloc)
+
+
+def _attend_buffers(cfg, q, out, lse, workspace, size):
+    B, M = q.shape[:2]
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty((B, M, cfg.n_q_heads), dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(size(), 256), dtype=torch.uint8, device=q.device)
+    _need_shape(out, torch.bfloat16, q.shape, "out")
+    _need_shape(lse, torch.float32, (B, M, cfg.n_q_heads), "lse")
+    _need(workspace, torch.uint8, "workspace")
+    return out, lse, workspace
+
+
+def msa_window_attend(cfg, q, Kloc, Vloc, q_pos, window, sinks=0, local_pos0=0, out=None, lse=None, workspace=None,
+                      stream=None):
+    """q bf16 [B][M][Hq][d] and Kloc bf16 [B][Hkv][Lloc][d] as msa_norm_rotate writes them, Vloc, q_pos int32 [B][M] ->
+    (out bf16 like q, lse fp32 [B][M][Hq]): attention over the last `window` tokens and the first `sinks`."""
+    B, M = q.shape[:2]
+    Lloc = Kloc.shape[2]
+    _need_shape(q, torch.bfloat16, (B, M, cfg.n_q_heads, cfg.head_dim), "q")
+    _need_shape(Kloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Kloc")
+    _need_shape(Vloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Vloc")
+    _need_shape(q_pos, torch.int32, (B, M), "q_pos")
+    out, lse, workspace = _attend_buffers(cfg, q, out, lse, workspace,
+                                          lambda: window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks))
+    _same_device(q, Kloc, Vloc, q_pos, out, lse, workspace)
+    _call("msa_window_attend", q.device, ctypes.byref(cfg), _ptr(q), B, M, _ptr(Kloc), _ptr(Vloc), Lloc, local_pos0, window,
+          sinks, _ptr(q_pos), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream, q.device))
+    return out, lse
+
+
+def msa_sparse_attend4(cfg, q, bank, idx, Kloc, Vloc, local_pos0, q_pos, out=None, lse=None, workspace=None, stream=None):
+    """msa_sparse_attend over bank = (K4, K4s, V4, V4s) of msa_pack_kv4; q and Kloc carry their positions (msa_norm_rotate).
+    idx int32 [B][M'][S][k] as msa_score_topk writes it for cfg -> (out bf16 like q, lse fp32 [B][M][Hq])."""
+    B, M = q.shape[:2]
+    k = idx.shape[-1]
+    Lloc = 0 if Kloc is None else Kloc.shape[2]
+    _need_shape(q, torch.bfloat16, (B, M, cfg.n_q_heads, cfg.head_dim), "q")
+    _need_kv4(cfg, bank)
+    _need_shape(idx, torch.int32, (B, 1 if cfg.token_pool else M,
+                                   1 if cfg.select_scope == MSA_SCOPE_ALL else cfg.n_kv_heads, k), "idx")
+    if (Kloc is None) != (Vloc is None) or any(t is None for t in bank):
+        raise ValueError("msa_sparse_attend4: keys come with their values")
+    if Kloc is not None:
+        _need_shape(Kloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Kloc")
+        _need_shape(Vloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Vloc")
+    _need_shape(q_pos, torch.int32, (B, M), "q_pos")
+    out, lse, workspace = _attend_buffers(cfg, q, out, lse, workspace,
+                                          lambda: sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc))
+    _same_device(q, *bank, idx, Kloc, Vloc, q_pos, out, lse, workspace)
+    _call("msa_sparse_attend4", q.device, ctypes.byref(cfg), _ptr(q), B, M, *map(_ptr, bank), _ptr(idx), k, _ptr(Kloc),
+          _ptr(Vloc), Lloc, local_pos0, _ptr(q_pos), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
+          _stream(stream, q.device))
+    return out, lse

@@ -1,4 +1,5 @@
 // C-ABI layer: argument validation (host only, before anything is enqueued), work plans, launches.
+#include "msa_encoded.h"
 #include "msa_host.h"
 
 #include <chrono>
@@ -454,6 +455,108 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
     if (rc != MSA_OK) return rc;
   }
   return V != nullptr ? launch_unpack4(dm, V4, V4s, doc_begin, doc_count, V, (hipStream_t)stream) : MSA_OK;
+}
+
+static int plan_window(const Dims& dm, int32_t B, int32_t M, int32_t Lloc, int32_t window, int32_t sinks, EncodedPlan* pl) {
+  if (B < 1 || M < 1 || Lloc < 1 || window < 1 || sinks < 0) return MSA_ERR_INVALID_ARG;
+  if ((int64_t)B * M > 65535 || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
+  const long long seen = (long long)window + sinks;
+  *pl = plan_encoded(dm, B, M, 0, false, seen < Lloc ? seen : Lloc, Lloc);
+  return MSA_OK;
+}
+
+size_t msa_window_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
+                                         int32_t sinks) {
+  Dims dm;
+  EncodedPlan pl;
+  if (make_dims(cfg, &dm, kForAttend) != MSA_OK || plan_window(dm, B, M, Lloc, window, sinks, &pl) != MSA_OK) return 0;
+  return pl.ws_bytes;
+}
+
+int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kloc, const void* Vloc,
+                      int32_t Lloc, int32_t local_pos0, int32_t window, int32_t sinks, const int32_t* q_pos, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, msa_stream_t stream) {
+  Dims dm;
+  EncodedPlan pl;
+  int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (q == nullptr || Kloc == nullptr || Vloc == nullptr || q_pos == nullptr || out == nullptr || workspace == nullptr ||
+      local_pos0 < 0)
+    return MSA_ERR_INVALID_ARG;
+  rc = plan_window(dm, B, M, Lloc, window, sinks, &pl);
+  if (rc != MSA_OK) return rc;
+  if (misaligned(q) || misaligned(Kloc) || misaligned(Vloc) || misaligned4(q_pos) || misaligned(out) || misaligned4(lse) ||
+      misaligned(workspace))
+    return MSA_ERR_MISALIGNED;
+  if (workspace_bytes < pl.ws_bytes) return MSA_ERR_WORKSPACE;
+  EncodedArgs a = {};
+  a.q = (const uint16_t*)q;
+  a.Kloc = (const uint16_t*)Kloc;
+  a.Vloc = (const uint16_t*)Vloc;
+  a.q_pos = q_pos;
+  a.out = (uint16_t*)out;
+  a.lse = lse;
+  a.M = M;
+  a.Lloc = Lloc;
+  a.pos0 = local_pos0;
+  a.window = window;
+  a.sinks = sinks;
+  return launch_encoded(dm, pl, a, B, workspace, (hipStream_t)stream);
+}
+
+static int plan_attend4(const Dims& dm, int32_t B, int32_t M, int32_t k, int32_t Lloc, EncodedPlan* pl) {
+  if (B < 1 || M < 1 || k < 1 || Lloc < 0) return MSA_ERR_INVALID_ARG;
+  if (k > MSA_MAX_TOPK || (int64_t)B * M > 65535 || (int64_t)k * dm.G > (1 << 28) || Lloc > (1 << 28))
+    return MSA_ERR_UNSUPPORTED;
+  *pl = plan_encoded(dm, B, M, (long long)k * dm.G, dm.token_pool == 1, Lloc, Lloc);
+  return MSA_OK;
+}
+
+size_t msa_sparse_attend4_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t k, int32_t Lloc) {
+  Dims dm;
+  EncodedPlan pl;
+  if (make_dims(cfg, &dm, kForAttend) != MSA_OK || plan_attend4(dm, B, M, k, Lloc, &pl) != MSA_OK) return 0;
+  return pl.ws_bytes;
+}
+
+int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* K4, const void* K4s,
+                       const void* V4, const void* V4s, const int32_t* idx, int32_t k, const void* Kloc, const void* Vloc,
+                       int32_t Lloc, int32_t local_pos0, const int32_t* q_pos, void* out, float* lse, void* workspace,
+                       size_t workspace_bytes, msa_stream_t stream) {
+  Dims dm;
+  EncodedPlan pl;
+  int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (q == nullptr || K4 == nullptr || K4s == nullptr || V4 == nullptr || V4s == nullptr || idx == nullptr ||
+      q_pos == nullptr || out == nullptr || workspace == nullptr || local_pos0 < 0)
+    return MSA_ERR_INVALID_ARG;
+  if (Lloc > 0 && (Kloc == nullptr || Vloc == nullptr)) return MSA_ERR_INVALID_ARG;
+  rc = plan_attend4(dm, B, M, k, Lloc, &pl);
+  if (rc != MSA_OK) return rc;
+  if (misaligned(q) || misaligned(K4) || misaligned(K4s) || misaligned(V4) || misaligned(V4s) || misaligned4(idx) ||
+      misaligned(Kloc) || misaligned(Vloc) || misaligned4(q_pos) || misaligned(out) || misaligned4(lse) ||
+      misaligned(workspace) || misaligned4(dm.lens))
+    return MSA_ERR_MISALIGNED;
+  if (workspace_bytes < pl.ws_bytes) return MSA_ERR_WORKSPACE;
+  EncodedArgs a = {};
+  a.q = (const uint16_t*)q;
+  a.K4 = (const uint8_t*)K4;
+  a.K4s = (const uint8_t*)K4s;
+  a.V4 = (const uint8_t*)V4;
+  a.V4s = (const uint8_t*)V4s;
+  a.idx = idx;
+  a.k = k;
+  a.Kloc = (const uint16_t*)Kloc;
+  a.Vloc = (const uint16_t*)Vloc;
+  a.q_pos = q_pos;
+  a.out = (uint16_t*)out;
+  a.lse = lse;
+  a.M = M;
+  a.Lloc = Lloc;
+  a.pos0 = local_pos0;
+  a.window = INT32_MAX;
+  a.sinks = 0;
+  return launch_encoded(dm, pl, a, B, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

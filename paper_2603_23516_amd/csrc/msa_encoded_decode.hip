@@ -1,0 +1,365 @@
+// Attention of single query tokens over position-encoded keys: msa_window_attend with few tokens, msa_sparse_attend4 where
+// every token has documents of its own.  Each row is read once per (token, KV head) and serves the r query heads of the group.
+//
+// The rows that a (token, KV head) pair sees are numbered through, the bank's rows first (document by document, pads and rows
+// past a document's end left out), then the local ones, in steps of 32; a workgroup has a contiguous range of steps, dealt to
+// its four waves in turn.  Per step, with 16x16x32 bf16 MFMA:
+//   S^T[key][col] = K q^T        A: lane (qd, n) holds dims of key row n; columns h and 8 + h both hold query head h
+//   softmax over the keys, online, per column, in powers of two
+//   O^T[dd][col] += V^T[dd][key] P^T[key][col]
+//                                B: columns h hold the bf16 weights and columns 8 + h what they lack (weights of 16 bits at
+//                                   no matrix work more: r <= 8 heads leave those columns empty)
+//                                A: value rows go through LDS and come back transposed (ds_read_b64_tr_b16)
+// Bank rows in four bits: lane (qd, n) takes the qd-th quarter of row n, 16 bytes at d = 128, and turns it into bf16 (exactly)
+// by v_cvt_scalef32_pk_bf16_fp4, which applies the block's scale; the query's dims are laid out to match.
+// The workgroup that arrives last at a pair merges its splits.
+#include "msa_encoded.h"
+
+namespace msa {
+
+__device__ __forceinline__ float max_xor16_32(float x) {
+  uint32_t u = __float_as_uint(x);
+  auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  u = __float_as_uint(x);
+  r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int D>
+struct Raw4 {  // a quarter of a row in four bits
+  uint32_t w[D / 32];
+};
+template <int D>
+__device__ __forceinline__ Raw4<D> load_raw4(const uint8_t* p) {
+  Raw4<D> x;
+  if constexpr (D == 128) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    x.w[0] = v.x; x.w[1] = v.y; x.w[2] = v.z; x.w[3] = v.w;
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    x.w[0] = v.x; x.w[1] = v.y;
+  }
+  return x;
+}
+
+template <int D, bool BANK4>
+__global__ __launch_bounds__(256) void encoded_decode_kernel(EncodedArgs a) {
+  constexpr int NS = D / 32;   // contraction slices of the score product, and 32-bit words of a quarter row's codes
+  constexpr int NC = D / 16;   // 16-row tiles of the output product
+  constexpr int ROW = D * 2;   // bytes of a value row in LDS
+  constexpr int OROW = D + 4;  // floats of a row of a wave's output in the merge
+  constexpr int STAGE = 32 * ROW > 8 * OROW * 4 ? 32 * ROW : 8 * OROW * 4;
+  __shared__ __attribute__((aligned(16))) unsigned char stage[4][STAGE];
+  __shared__ float wm[4][8], wl[4][8];
+  __shared__ int pre[MSA_MAX_TOPK + 1], docs[MSA_MAX_TOPK];
+  __shared__ uint32_t arrived;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qd = lane >> 4, n = lane & 15, h = n & 7;
+  const int sp = blockIdx.x, g = blockIdx.y, bm = blockIdx.z, b = bm / a.M, r = a.r;
+  const Seen see = seen_rows((long long)a.q_pos[bm] - a.pos0, a.Lloc, a.window, a.sinks);
+
+  int rows_mem = 0;
+  if (BANK4) {
+    if (wave == 0) number_rows(a, b, bm, g, lane, pre, docs);
+    __syncthreads();
+    rows_mem = __builtin_amdgcn_readfirstlane(pre[MSA_MAX_TOPK]);
+  }
+  const int steps_mem = (rows_mem + 31) / 32, steps_a = (see.first + 31) / 32, steps_b = (see.to - see.from + 31) / 32;
+  const int steps = steps_mem + steps_a + steps_b;
+  const int s_begin = (int)((long long)steps * sp / a.n_splits), s_end = (int)((long long)steps * (sp + 1) / a.n_splits);
+
+  // queries: column n holds head n % 8; B operand of slice s: dims 32 s + 8 qd .. + 8 (local rows), or the s-th eight dims of
+  // the qd-th quarter (bank rows)
+  bf16x8_t bq[NS], bq4[BANK4 ? NS : 1];
+  {
+    const uint16_t* qp = a.q + ((long long)bm * a.Hq + g * r + (h < r ? h : 0)) * D;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      uint4 x = *reinterpret_cast<const uint4*>(qp + 32 * s + 8 * qd);
+      if (h >= r) x = make_uint4(0, 0, 0, 0);
+      bq[s] = as_bf16x8(x);
+      if (BANK4) {
+        x = *reinterpret_cast<const uint4*>(qp + (D / 4) * qd + 8 * s);
+        if (h >= r) x = make_uint4(0, 0, 0, 0);
+        bq4[s] = as_bf16x8(x);
+      }
+    }
+  }
+
+  // Value rows in LDS: 16-byte piece p of row i lies at place p ^ swz(i), so that neither the writes (16 rows, one piece) nor
+  // the transposing reads (four rows, two pieces) meet in a bank.
+  unsigned char* const vt = stage[wave];
+  auto swz = [](int i) { return D == 128 ? 2 * (i & 7) : 2 * ((i >> 1) & 3); };
+  auto put = [&](int i, int p, uint4 x) { *reinterpret_cast<uint4*>(vt + i * ROW + ((p ^ swz(i)) * 16)) = x; };
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4_t o[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) o[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+
+  // scores of a step's 32 keys (of which `cnt` exist) -> weights, and the second product over the rows in LDS
+  auto finish = [&](f32x4_t s0, f32x4_t s1, int cnt) __attribute__((always_inline)) {
+    float x[8];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int key = (i >> 2) * 16 + 4 * qd + (i & 3);
+      x[i] = key < cnt ? (i < 4 ? s0[i & 3] : s1[i & 3]) * a.qscale : -INFINITY;
+      mx = fmaxf(mx, x[i]);
+    }
+    mx = max_xor16_32(mx);
+    if (__ballot(mx > m_run) != 0) {
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) o[c] *= alpha;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    uint32_t pw[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float p0 = __builtin_amdgcn_exp2f(x[2 * j] - m_use), p1 = __builtin_amdgcn_exp2f(x[2 * j + 1] - m_use);
+      l_run += p0 + p1;
+      uint32_t hi, lo;
+      split_pack_bf16(p0, p1, hi, lo);
+      pw[j] = n < 8 ? hi : lo;
+    }
+    const bf16x8_t pb = as_bf16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int row = 4 * qd + (n >> 2);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const unsigned char* vp = vt + row * ROW + (((2 * c + ((n & 3) >> 1)) ^ swz(row)) * 16) + 8 * (n & 1);
+      const s16x4_t v0 = lds_read_tr16(vp), v1 = lds_read_tr16(vp + 16 * ROW);  // rows 16 apart: the same swizzle
+      const bf16x8_t av = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      o[c] = mfma16(av, pb, o[c]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+
+  int s = s_begin + wave;
+  if (BANK4) {
+    int slot[2] = {0, 0};
+    for (; s < s_end && s < steps_mem; s += 4) {
+      Raw4<D> kc[2], vc[2];
+      float ks[2], vs[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        int row = 32 * s + 16 * t + n;
+        row = row < rows_mem ? row : rows_mem - 1;
+        while (row >= pre[slot[t] + 1]) ++slot[t];  // ends: row < pre[k]
+        const long long at = ((long long)docs[slot[t]] * a.Hkv + g) * a.G + (row - pre[slot[t]]);
+        kc[t] = load_raw4<D>(a.K4 + at * (D / 2) + (D / 8) * qd);
+        vc[t] = load_raw4<D>(a.V4 + at * (D / 2) + (D / 8) * qd);
+        const int sb = D == 128 ? qd : qd >> 1;
+        ks[t] = __uint_as_float((uint32_t)a.K4s[at * (D / 32) + sb] << 23);
+        vs[t] = __uint_as_float((uint32_t)a.V4s[at * (D / 32) + sb] << 23);
+      }
+      f32x4_t sc[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sc[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          sc[t] = mfma16(as_bf16x8(fp4x8_to_bf16(kc[t].w[j], ks[t])), bq4[j], sc[t]);
+          put(16 * t + n, NS * qd + j, fp4x8_to_bf16(vc[t].w[j], vs[t]));
+        }
+      }
+      finish(sc[0], sc[1], rows_mem - 32 * s < 32 ? rows_mem - 32 * s : 32);
+    }
+  }
+  const long long loc = ((long long)b * a.Hkv + g) * a.Lloc;
+  for (; s < s_end; s += 4) {
+    const int j0 = s - steps_mem;
+    const int t0 = j0 < steps_a ? 32 * j0 : see.from + 32 * (j0 - steps_a);
+    const int end = j0 < steps_a ? see.first : see.to;
+    uint4 kx[2][NS], vx[2][NS];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      int row = t0 + 16 * t + n;
+      row = row < end ? row : end - 1;
+      const uint16_t* kp = a.Kloc + (loc + row) * D + 8 * qd;
+      const uint16_t* vp = a.Vloc + (loc + row) * D + 8 * qd;
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        kx[t][j] = *reinterpret_cast<const uint4*>(kp + 32 * j);
+        vx[t][j] = *reinterpret_cast<const uint4*>(vp + 32 * j);
+      }
+    }
+    f32x4_t sc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      sc[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < NS; ++j) {
+        sc[t] = mfma16(as_bf16x8(kx[t][j]), bq[j], sc[t]);
+        put(16 * t + n, 4 * j + qd, vx[t][j]);
+      }
+    }
+    finish(sc[0], sc[1], end - t0 < 32 ? end - t0 : 32);
+  }
+
+  // ---- the four waves' results, then the splits' --------------------------------------------------------------
+  l_run = add_xor32(add_xor16(l_run));
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[c][i] += dpp_f<kDppRor8>(o[c][i]);  // columns h and 8 + h
+  float* const mine = reinterpret_cast<float*>(stage[wave]);
+  if (n < r) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4_t*>(mine + n * OROW + 16 * c + 4 * qd) = o[c];
+    if (qd == 0) {
+      wm[wave][n] = m_run;
+      wl[wave][n] = l_run;
+    }
+  }
+  __syncthreads();
+  const long long qh0 = (long long)bm * a.Hq + g * r;
+  for (int e = tid; e < r * D; e += 256) {
+    const int hh = e / D, dd = e % D;
+    float m = wm[0][hh];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, wm[w][hh]);
+    float l = 0.f, x = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = wm[w][hh] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[w][hh] - m);
+      l += f * wl[w][hh];
+      x += f * reinterpret_cast<const float*>(stage[w])[hh * OROW + dd];
+    }
+    if (a.n_splits == 1) {
+      a.out[(qh0 + hh) * D + dd] = (uint16_t)pack_bf16(l > 0.f ? x / l : 0.f, 0.f);
+      if (dd == 0 && a.lse != nullptr) a.lse[qh0 + hh] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    } else {
+      const long long ph = (qh0 + hh) * a.n_splits + sp;
+      store_dev(a.part_o + ph * D + dd, x);
+      if (dd == 0)
+        store_dev(reinterpret_cast<unsigned long long*>(a.part_ml + ph),
+                  ((unsigned long long)__float_as_uint(l) << 32) | __float_as_uint(m));
+    }
+  }
+  if (a.n_splits == 1) return;
+  wait_stores_done();
+  __syncthreads();
+  unsigned long long* const ticket = a.tickets + (long long)bm * a.Hkv + g;
+  if (tid == 0) arrived = arrive_at(ticket, a.nonce);
+  __syncthreads();
+  if (arrived != (uint32_t)a.n_splits - 1) return;
+  if (tid == 0) store_dev(ticket, 0ull);
+  for (int e = tid; e < r * D; e += 256) {
+    const int hh = e / D, dd = e % D;
+    const long long ph = (qh0 + hh) * a.n_splits;
+    float m = -INFINITY, l = 0.f, x = 0.f;
+    for (int i = 0; i < a.n_splits; ++i) {
+      const unsigned long long ml = load_dev(reinterpret_cast<const unsigned long long*>(a.part_ml + ph + i));
+      const float mi = __uint_as_float((uint32_t)ml), li = __uint_as_float((uint32_t)(ml >> 32));
+      const float xi = load_dev(a.part_o + (ph + i) * D + dd);
+      if (mi == -INFINITY) continue;
+      const float mn = fmaxf(m, mi);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), fi = __builtin_amdgcn_exp2f(mi - mn);
+      l = l * f + li * fi;
+      x = x * f + xi * fi;
+      m = mn;
+    }
+    a.out[(qh0 + hh) * D + dd] = (uint16_t)pack_bf16(l > 0.f ? x / l : 0.f, 0.f);
+    if (dd == 0 && a.lse != nullptr) a.lse[qh0 + hh] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  }
+}
+
+EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc) {
+  EncodedPlan p = {};
+  const long long pairs = (long long)B * M * dm.Hkv;
+  p.tiled = M >= 8 && (mem_rows == 0 || shared) ? 1 : 0;
+  long long n, most;
+  if (p.tiled) {
+    // 256 columns to a workgroup where that leaves one for every CU, 128 else; ranges of 4 steps at least
+    auto tiles = [&](int cb) {
+      p.cb = cb;
+      p.tpw = 32 * cb / dm.r;
+      p.n_tiles = (M + 4 * p.tpw - 1) / (4 * p.tpw);
+      return (long long)B * p.n_tiles * dm.Hkv;
+    };
+    long long t = tiles(2);
+    if (t < 256) t = tiles(1);
+    const long long seen = local_rows + 4 * p.tpw;
+    const long long steps = (mem_rows + 31) / 32 + ((seen < Lloc ? seen : Lloc) + 31) / 32;
+    n = (p.cb == 2 ? 256 : 512) / t;
+    most = steps / 4;
+  } else {
+    // about 1024 workgroups, ranges of 8 steps at least
+    n = (1024 + pairs - 1) / pairs;
+    most = ((mem_rows + 31) / 32 + (local_rows + 31) / 32 + 7) / 8;
+  }
+  if (n > most) n = most;
+  p.n_splits = (int)(n < 1 ? 1 : (n > 32 ? 32 : n));
+  const size_t heads = (size_t)B * M * dm.Hq;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += round_up256(bytes);
+    return here;
+  };
+  if (p.n_splits > 1) {
+    take(heads * p.n_splits * dm.d * sizeof(float));
+    p.off_ml = take(heads * p.n_splits * sizeof(float2));
+    if (!p.tiled) p.off_tickets = take((size_t)pairs * sizeof(unsigned long long));
+  }
+  if (p.tiled && mem_rows > 0) {
+    const size_t x = (size_t)B * dm.Hkv * mem_rows * dm.d * 2;
+    p.off_kx = take(x);
+    p.off_vx = take(x);
+    p.off_mem_rows = take((size_t)B * dm.Hkv * sizeof(int));
+  }
+  p.ws_bytes = at > 256 ? at : 256;
+  return p;
+}
+
+int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, void* ws, hipStream_t st) {
+  unsigned char* const w = (unsigned char*)ws;
+  a.Hq = dm.Hq;
+  a.Hkv = dm.Hkv;
+  a.r = dm.r;
+  a.G = dm.G;
+  a.N = dm.N;
+  a.idx_sel = dm.scope_all ? 1 : dm.Hkv;
+  a.idx_rows_per_b = dm.token_pool ? 1 : a.M;
+  a.lens = dm.lens;
+  a.qscale = (float)(1.4426950408889634 / sqrt((double)dm.d));
+  a.n_splits = pl.n_splits;
+  a.part_o = (float*)w;
+  a.part_ml = (float2*)(w + pl.off_ml);
+  a.tickets = (unsigned long long*)(w + pl.off_tickets);
+  if (pl.tiled) {
+    TiledArgs ta = {};
+    ta.tpw = pl.tpw;
+    ta.n_tiles = pl.n_tiles;
+    ta.cb = pl.cb;
+    if (a.K4 != nullptr) {
+      ta.Kx = (uint16_t*)(w + pl.off_kx);
+      ta.Vx = (uint16_t*)(w + pl.off_vx);
+      ta.mem_rows = (int*)(w + pl.off_mem_rows);
+      ta.mem_cap = a.k * dm.G;
+    }
+    return launch_encoded_tiled(dm, a, ta, B, st);
+  }
+  a.nonce = launch_nonce48();
+  const dim3 grid(a.n_splits, dm.Hkv, B * a.M), block(256);
+  if (dm.d == 128) {
+    if (a.K4 != nullptr) hipLaunchKernelGGL((encoded_decode_kernel<128, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((encoded_decode_kernel<128, false>), grid, block, 0, st, a);
+  } else {
+    if (a.K4 != nullptr) hipLaunchKernelGGL((encoded_decode_kernel<64, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((encoded_decode_kernel<64, false>), grid, block, 0, st, a);
+  }
+  return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
+}
+
+}  // namespace msa

@@ -46,27 +46,57 @@ def unpack4(codes, scales):
 
 
 def attend(q, K, V, seen):
-    """q [d], K, V [t][d], seen [t] -> (output [d], log of the sum); nothing seen: zeros, -inf."""
+    """q [d], K, V [t][d], seen [t] -> output [d], log of the sum (nothing seen: zeros, -inf), and for error bounds the same mean
+    of |V|, the largest sum of |q_i k_i| / sqrt(d) and the number of rows."""
     if not bool(seen.any()):
-        return torch.zeros(V.shape[1], dtype=torch.float64), -math.inf
+        return torch.zeros(V.shape[1], dtype=torch.float64), -math.inf, torch.zeros(V.shape[1], dtype=torch.float64), 0.0, 0
     x = (K[seen] @ q) / math.sqrt(q.shape[0])
     lse = torch.logsumexp(x, 0)
-    return torch.exp(x - lse) @ V[seen], float(lse)
+    w = torch.exp(x - lse)
+    size = float((K[seen].abs() @ q.abs()).max()) / math.sqrt(q.shape[0])
+    return w @ V[seen], float(lse), w @ V[seen].abs(), size, int(seen.sum())
+
+
+class Attended:
+    """Outputs and log-sums of many heads with their error bounds.
+
+    Scores: fp32 sums of d <= 128 exact products, off by d 2^-24 sum|q_i k_i| at most, scaled and rounded a few times: a weight
+    is off by delta = 2^-16 (S + 1) relative, S the largest sum|q_i k_i| / sqrt(d).  The sum of n weights adds n 2^-23.  Weights
+    rounded to bf16 are off by 2^-8 at most, those carried as (hi, lo) pairs by 2^-16.  The output is rounded to bf16: 2^-8."""
+
+    def __init__(self, shape, d):
+        z = dict(dtype=torch.float64)
+        self.out, self.mass = torch.zeros(shape + (d,), **z), torch.zeros(shape + (d,), **z)
+        self.lse, self.size, self.n = torch.full(shape, -math.inf, **z), torch.zeros(shape, **z), torch.zeros(shape, **z)
+
+    def put(self, at, got):
+        self.out[at], self.lse[at], self.mass[at], self.size[at], self.n[at] = got
+
+    def check(self, out, lse, weights=2.0 ** -8):
+        out, lse = out.double().cpu(), lse.double().cpu()
+        delta = 2.0 ** -16 * (self.size + 1) + self.n * 2.0 ** -23
+        tol = 2.0 ** -8 * self.out.abs() + (weights + 2 * delta)[..., None] * self.mass
+        err = (out - self.out).abs()
+        assert bool((err <= tol).all()), f"output: off by {float((err - tol).max())} more than the bound"
+        empty = torch.isinf(self.lse)
+        assert torch.equal(torch.isinf(lse) & (lse < 0), empty)
+        off = (lse - self.lse).abs()[~empty] - (delta + 2.0 ** -22 * self.lse.abs())[~empty]
+        assert bool((off <= 0).all()), f"log-sum: off by {float(off.max())} more than the bound"
 
 
 def window_attend(q, Kloc, Vloc, q_pos, window, sinks, pos0):
     """q [B][M][Hq][d], caches [B][Hkv][L][d], all float64."""
     B, M, Hq, d = q.shape
     r = Hq // Kloc.shape[1]
-    out, lse = torch.zeros_like(q), torch.full((B, M, Hq), -math.inf, dtype=torch.float64)
+    res = Attended((B, M, Hq), d)
     t = torch.arange(Kloc.shape[2])
     for b in range(B):
         for m in range(M):
             p = int(q_pos[b, m]) - pos0
             seen = (t <= p) & ((p - t < window) | (t < sinks))
             for h in range(Hq):
-                out[b, m, h], lse[b, m, h] = attend(q[b, m, h], Kloc[b, h // r], Vloc[b, h // r], seen)
-    return out, lse
+                res.put((b, m, h), attend(q[b, m, h], Kloc[b, h // r], Vloc[b, h // r], seen))
+    return res
 
 
 def sparse_attend4(q, K, V, idx, lens, Kloc, Vloc, q_pos, pos0):
@@ -74,7 +104,7 @@ def sparse_attend4(q, K, V, idx, lens, Kloc, Vloc, q_pos, pos0):
     B, M, Hq, d = q.shape
     N, Hkv, G, _ = K.shape
     r, Mp, S = Hq // Hkv, idx.shape[1], idx.shape[2]
-    out, lse = torch.zeros_like(q), torch.full((B, M, Hq), -math.inf, dtype=torch.float64)
+    res = Attended((B, M, Hq), d)
     for b in range(B):
         for m in range(M):
             near = torch.arange(Kloc.shape[2]) + pos0 <= int(q_pos[b, m])
@@ -85,5 +115,5 @@ def sparse_attend4(q, K, V, idx, lens, Kloc, Vloc, q_pos, pos0):
                 Vx = torch.cat([V[i, g, :x] for i, x in zip(docs, n)] + [Vloc[b, g][near]])
                 seen = torch.ones(Kx.shape[0], dtype=torch.bool)
                 for h in range(g * r, g * r + r):
-                    out[b, m, h], lse[b, m, h] = attend(q[b, m, h], Kx, Vx, seen)
-    return out, lse
+                    res.put((b, m, h), attend(q[b, m, h], Kx, Vx, seen))
+    return res

@@ -1,0 +1,174 @@
+"""msa_window_attend against the plain definition in 64 bits: windows, first tokens, positions in any order, empty rows."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2603_23516_amd as msa
+import plain64 as P
+
+FEW = 2.0 ** -16      # softmax weights of few tokens: bf16 (hi, lo) pairs
+MANY = 2.0 ** -8      # of many: bf16
+
+
+def _cfg(Hq=8, Hkv=2, d=64):
+    return msa.MsaConfig(1, 1, 1, Hq, Hkv, d, 1e4)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return msa.load_library()
+
+
+def _call(lib, cfg, **kw):
+    p = ctypes.c_void_p(0x10000)
+    a = dict(q=p, B=1, M=1, K=p, V=p, L=64, pos0=0, W=16, S=0, q_pos=p, out=p, lse=p, ws=p, bytes=1 << 40)
+    a.update(kw)
+    return lib.msa_window_attend(ctypes.byref(cfg), a["q"], a["B"], a["M"], a["K"], a["V"], a["L"], a["pos0"], a["W"], a["S"],
+                                 a["q_pos"], a["out"], a["lse"], a["ws"], a["bytes"], None)
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(q=None), -1), (dict(K=None), -1), (dict(V=None), -1), (dict(q_pos=None), -1), (dict(out=None), -1), (dict(ws=None), -1),
+    (dict(B=0), -1), (dict(M=0), -1), (dict(L=0), -1), (dict(W=0), -1), (dict(S=-1), -1), (dict(pos0=-1), -1),
+    (dict(B=256, M=256), -2), (dict(L=(1 << 28) + 1), -2), (dict(bytes=255), -3),
+    (dict(q=ctypes.c_void_p(0x10008)), -4), (dict(K=ctypes.c_void_p(0x10002)), -4), (dict(q_pos=ctypes.c_void_p(0x10002)), -4),
+    (dict(lse=ctypes.c_void_p(0x10002)), -4), (dict(ws=ctypes.c_void_p(0x10010 + 4)), -4),
+])
+def test_refusals(lib, kw, status):
+    assert _call(lib, _cfg(), **kw) == status
+
+
+def test_workspace_sizes(lib):
+    c = _cfg(32, 8, 128)
+    for B, M, L, W, S in ((1, 1, 1, 1, 0), (1, 1, 1 << 20, 1 << 20, 4), (40, 1, 8192, 4096, 4), (1, 8192, 8192, 4096, 4), (1, 8, 65536, 65536, 0)):
+        n = msa.window_attend_workspace_bytes(c, B, M, L, W, S)
+        assert n >= 256 and n % 256 == 0
+        assert _call(lib, c, B=B, M=M, L=L, W=W, S=S, bytes=n - 1) == msa.MSA_ERR_WORKSPACE
+    assert msa.window_attend_workspace_bytes(c, 1, 1, 0, 4, 0) == 0
+    assert msa.window_attend_workspace_bytes(c, 1, 1, 8, 0, 0) == 0
+    # a longer cache or window never asks for less
+    sizes = [msa.window_attend_workspace_bytes(c, 2, 1, L, W, 4) for L, W in ((100, 50), (1000, 50), (1000, 500), (9000, 8000))]
+    assert sizes == sorted(sizes)
+
+
+def _make(B, M, Hq, Hkv, d, L, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn(s, generator=g).to(torch.bfloat16) for s in ((B, M, Hq, d), (B, Hkv, L, d), (B, Hkv, L, d))]
+
+
+def _check(Hq, Hkv, d, q, K, V, q_pos, W, S, pos0, **kw):
+    B, M = q.shape[:2]
+    cfg = _cfg(Hq, Hkv, d)
+    ws = torch.full((msa.window_attend_workspace_bytes(cfg, B, M, K.shape[2], W, S),), 0xA5, dtype=torch.uint8, device="cuda")
+    Kd, Vd = K.clone(), V.clone()
+    for b in range(B):          # what lies behind every token of a sequence has no effect
+        behind = max(0, int(q_pos[b].max()) - pos0 + 1)
+        Kd[b, :, behind:] = float("nan")
+        Vd[b, :, behind:] = float("inf")
+    out, lse = msa.msa_window_attend(cfg, q.cuda(), Kd.cuda(), Vd.cuda(), q_pos.cuda(), W, sinks=S, local_pos0=pos0,
+                                     workspace=ws, **kw)
+    torch.cuda.synchronize()
+    P.window_attend(q.double(), K.double(), V.double(), q_pos, W, S, pos0).check(out, lse, FEW if M < 8 else MANY)
+    return out, lse
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 3, 8, 45])
+@pytest.mark.parametrize("Hq, Hkv, d", [(4, 4, 64), (4, 2, 128), (6, 2, 64), (4, 1, 64), (8, 1, 128), (5, 1, 128)])
+@pytest.mark.parametrize("L, W, S", [(1, 1, 0), (50, 1, 0), (50, 7, 3), (97, 32, 33), (130, 200, 4), (161, 33, 0)])
+def test_against_64_bits(M, Hq, Hkv, d, L, W, S):
+    q, K, V = _make(2, M, Hq, Hkv, d, L, M + L)
+    pos0 = 5
+    last = torch.tensor([[L - 1], [max(L // 2, 0)]]) + pos0
+    q_pos = (last - M + 1 + torch.arange(M)).to(torch.int32)      # the first tokens may lie in front of the cache: they see nothing
+    _check(Hq, Hkv, d, q, K, V, q_pos, W, S, pos0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [2, 40])
+def test_positions_in_any_order(M):
+    """Padding, positions past the cache's end, the same position twice, tokens far apart in one tile."""
+    g = torch.Generator().manual_seed(2)
+    q, K, V = _make(3, M, 4, 2, 64, 300, 1)
+    q_pos = torch.randint(-3, 340, (3, M), generator=g, dtype=torch.int32)
+    q_pos[0, 0], q_pos[1, 1], q_pos[2] = -2 ** 31, 2 ** 31 - 1, -1
+    for W, S in ((16, 4), (400, 0), (1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (60, 100)):
+        _check(4, 2, 64, q, K, V, q_pos, W, S, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M, L, W, S", [(1, 3000, 2500, 9), (4, 2100, 2100, 0), (9, 2500, 2500, 0), (20, 1700, 900, 70)])
+def test_split_rows(M, L, W, S):
+    """Long windows with few tokens: the rows are shared out and the parts joined."""
+    q, K, V = _make(1, M, 4, 1, 128, L, 4)
+    q_pos = (L - M + torch.arange(M)).reshape(1, M).to(torch.int32)
+    _check(4, 1, 128, q, K, V, q_pos, W, S, 0)
+    q_pos[0, 0] = 31                                              # one of them sees a single step: most parts of it are empty
+    _check(4, 1, 128, q, K, V, q_pos, W, S, 0)
+
+
+@pytest.mark.gpu
+def test_large_scores():
+    """Scores of hundreds: one row takes all; and equal scores: the mean."""
+    q, K, V = _make(1, 12, 4, 2, 64, 200, 5)
+    q_pos = (188 + torch.arange(12)).reshape(1, 12).to(torch.int32)
+    for M in (12, 2):
+        _check(4, 2, 64, (q[:, :M] * 30).to(torch.bfloat16), (K * 10).to(torch.bfloat16), V, q_pos[:, :M].contiguous(), 100, 3, 0)
+        _check(4, 2, 64, torch.zeros_like(q[:, :M]), K, V, q_pos[:, :M].contiguous(), 100, 3, 0)
+
+
+@pytest.mark.gpu
+def test_tokens_do_not_depend_on_their_neighbours():
+    """A prompt in one call and in chunks, and a second sequence beside it: the same results within the weights' rounding."""
+    q, K, V = _make(2, 300, 8, 2, 128, 300, 6)
+    cfg = _cfg(8, 2, 128)
+    q, K, V = q.cuda(), K.cuda(), V.cuda()
+    q_pos = torch.arange(300, dtype=torch.int32, device="cuda").expand(2, 300).contiguous()
+    out, lse = msa.msa_window_attend(cfg, q, K, V, q_pos, 64, sinks=4)
+    for m0, m1 in ((0, 100), (100, 300), (299, 300)):
+        o, y = msa.msa_window_attend(cfg, q[:1, m0:m1].contiguous(), K[:1].contiguous(), V[:1].contiguous(), q_pos[:1, m0:m1].contiguous(), 64, sinks=4)
+        assert float((o.float() - out[:1, m0:m1].float()).abs().max()) <= 2.0 ** -5      # |V| < 5: 2^-8 of it twice, bf16 steps
+        assert float((y - lse[:1, m0:m1]).abs().max()) <= 1e-4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M, L", [(1, 2000), (12, 700)])
+def test_graph_replays_and_streams(M, L):
+    """A captured call, replayed on new inputs with other work between, on a stream of its own, with split rows (tickets)."""
+    cfg = _cfg(8, 1, 128)
+    q, K, V = (t.cuda() for t in _make(1, M, 8, 1, 128, L, 7))
+    q_pos = (L - M + torch.arange(M)).reshape(1, M).to(torch.int32).cuda()
+    ws = torch.full((msa.window_attend_workspace_bytes(cfg, 1, M, L, L, 0),), 0xFF, dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((1, M, 8), dtype=torch.float32, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        msa.msa_window_attend(cfg, q, K, V, q_pos, L, out=out, lse=lse, workspace=ws)
+    for i in range(4):
+        q.copy_(torch.randn_like(q.float()).to(torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        o, y = msa.msa_window_attend(cfg, q, K, V, q_pos, L)
+        torch.cuda.synchronize()
+        assert torch.equal(o, out) and torch.equal(y, lse), i
+    with torch.cuda.stream(side):
+        o2, y2 = msa.msa_window_attend(cfg, q, K, V, q_pos, L, workspace=ws)
+    side.synchronize()
+    assert torch.equal(o2, out) and torch.equal(y2, lse)
+
+
+@pytest.mark.gpu
+def test_python_refusals():
+    cfg = _cfg()
+    q, K, V = (t.cuda() for t in _make(2, 3, 8, 2, 64, 9))
+    pos = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    for bad in (dict(q=q[:1]), dict(q=q.transpose(1, 2)), dict(Kloc=K[:, :, :5]), dict(Vloc=V.float()), dict(q_pos=pos[:, :2]),
+                dict(q_pos=pos.long()), dict(out=q[:1])):
+        a = dict(q=q, Kloc=K, Vloc=V, q_pos=pos, window=4)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            msa.msa_window_attend(cfg, **a)
+    with pytest.raises(msa.MsaError):
+        msa.msa_window_attend(cfg, q, K, V, pos, 0)
