@@ -375,39 +375,48 @@ def msa_fetch_selected(cfg, K_host, V_host, idx, B, M, K_stage=None, V_stage=Non
 
 
 # ---- around a layer's projections, the local cache and a bank in four bits --------------------------------------------
-def _need_shape(t, dtype, shape, name):
-    _need(t, dtype, name)
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+# These calls are over in microseconds, so what is checked per tensor is checked in one place, once (2 us of a call's 8).
+_BF16, _I32, _F32, _U8 = torch.bfloat16, torch.int32, torch.float32, torch.uint8
 
 
-def _same_device(first, *tensors):
-    for t in tensors:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"tensors on {first.device} and {t.device} in one call")
+def _at(t, dtype, shape, dev, name):
+    """The address of a dense tensor of this type and shape on GPU `dev`."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous tensor of {dtype}, shape {tuple(shape)}, on cuda:{dev}, got {t.dtype}, "
+                     f"{tuple(t.shape)}, {t.device}")
 
 
-def _call(name, device, *args):
-    """The entry point `name`, with the tensors' device as the current one."""
-    fn = getattr(load_library(), name)
-    if device.index is None or device.index == torch.cuda.current_device():
-        rc = fn(*args)
+def _gpu(t, name):
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    return dev
+
+
+def _call(name, dev, stream, cfg, *args):
+    """The entry point `name` on `stream` (None: the tensors' device's current one), with that device as the current one."""
+    fn = getattr(_lib or load_library(), name)
+    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if dev == torch.cuda.current_device():
+        rc = fn(cfg, *args, raw)
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args)
-    _check(rc, name)
+        with torch.cuda.device(dev):
+            rc = fn(cfg, *args, raw)
+    if rc != MSA_OK:
+        raise MsaError(rc, name)
 
 
-def _token_stride(t, heads, d, name):
-    """Elements from one token of [B][M][heads][d] to the next; a view of a fused projection is taken as it lies."""
-    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 4 and t.shape[2] == heads and t.shape[3] == d):
-        raise ValueError(f"{name}: expected a CUDA tensor of torch.bfloat16, [B][M][{heads}][{d}]")
-    B, M = t.shape[:2]
-    sb, sm, sh, sd = t.stride()
-    step = sm if M > 1 else (sb if B > 1 else heads * d)
-    if sd != 1 or (heads > 1 and sh != d) or (B > 1 and M > 1 and sb != M * sm):
-        raise ValueError(f"{name}: heads and dims have to be dense, and tokens the same distance apart")
-    return step
+def _tokens_at(t, B, M, heads, d, dev, name):
+    """(address, elements from one token to the next) of a tensor [B][M][heads][d]; a view of a fused projection is taken as
+    it lies."""
+    if t.dtype is _BF16 and t.shape == (B, M, heads, d) and t.get_device() == dev:
+        sb, sm, sh, sd = t.stride()
+        step = sm if M > 1 else (sb if B > 1 else heads * d)
+        if sd == 1 and (heads == 1 or sh == d) and (B == 1 or M == 1 or sb == M * sm):
+            return t.data_ptr(), step
+    raise ValueError(f"{name}: expected torch.bfloat16 [{B}][{M}][{heads}][{d}] on cuda:{dev}, heads and dims dense, tokens the "
+                     f"same distance apart, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()}, {t.device}")
 
 
 def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None, eps=1e-6, rotate=True, local_pos0=0,
@@ -416,48 +425,47 @@ def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None,
     [B][M] -> q_out bf16 [B][M][Hq][d]; keys and values go into rows pos - local_pos0 of Kloc, Vloc bf16
     [B][Hkv][Lloc][d].  q, or k with Kloc, or v with Vloc, may be None.  Weights bf16 [d], None for no norm."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
-    src = next((t for t in (q, k, v) if t is not None), None)
-    if src is None or src.dim() != 4:
-        raise ValueError("msa_norm_rotate: expected q, k or v as [B][M][heads][d]")
-    B, M = src.shape[:2]
-    strides = [0 if t is None else _token_stride(t, h, d, n)
-               for t, h, n in ((q, Hq, "q"), (k, Hkv, "k"), (v, Hkv, "v"))]
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        if t is not None and tuple(t.shape[:2]) != (B, M):
-            raise ValueError(f"{n}: expected [{B}][{M}] tokens")
     if (k is None) != (Kloc is None) or (v is None) != (Vloc is None) or (q is None and q_out is not None):
         raise ValueError("msa_norm_rotate: k comes with Kloc, v with Vloc, q_out with q")
-    _need_shape(pos, torch.int32, (B, M), "pos")
-    cache = Kloc if Kloc is not None else Vloc
-    Lloc = 0 if cache is None else cache.shape[2]
-    for t, n in ((Kloc, "Kloc"), (Vloc, "Vloc")):
-        if t is not None:
-            _need_shape(t, torch.bfloat16, (B, Hkv, Lloc, d), n)
-    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if t is not None:
-            _need_shape(t, torch.bfloat16, (d,), n)
-    if q is not None and q_out is None:
-        q_out = torch.empty((B, M, Hq, d), dtype=torch.bfloat16, device=q.device)
+    src = q if q is not None else k if k is not None else v
+    if src is None or src.dim() != 4:
+        raise ValueError("msa_norm_rotate: expected q, k or v as [B][M][heads][d]")
+    dev = _gpu(src, "msa_norm_rotate")
+    B, M = src.shape[:2]
+    qa = ka = va = qo = Ka = Va = None
+    qs = ks = vs = Lloc = 0
     if q is not None:
-        _need_shape(q_out, torch.bfloat16, (B, M, Hq, d), "q_out")
-    _same_device(src, q, k, v, pos, Kloc, Vloc, q_weight, k_weight, q_out)
-    _call("msa_norm_rotate", src.device, ctypes.byref(cfg), _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
-          strides[2], _ptr(q_weight), _ptr(k_weight), eps, int(bool(rotate)), _ptr(pos), B, M, _ptr(q_out),
-          _ptr(Kloc), _ptr(Vloc), Lloc, local_pos0, _stream(stream, src.device))
+        qa, qs = _tokens_at(q, B, M, Hq, d, dev, "q")
+        if q_out is None:
+            q_out = torch.empty((B, M, Hq, d), dtype=_BF16, device=q.device)
+        qo = _at(q_out, _BF16, (B, M, Hq, d), dev, "q_out")
+    if k is not None:
+        ka, ks = _tokens_at(k, B, M, Hkv, d, dev, "k")
+        Lloc = Kloc.shape[2]
+        Ka = _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc")
+    if v is not None:
+        va, vs = _tokens_at(v, B, M, Hkv, d, dev, "v")
+        if k is None:
+            Lloc = Vloc.shape[2]
+        Va = _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc")
+    _call("msa_norm_rotate", dev, stream, ctypes.byref(cfg), qa, qs, ka, ks, va, vs,
+          None if q_weight is None else _at(q_weight, _BF16, (d,), dev, "q_weight"),
+          None if k_weight is None else _at(k_weight, _BF16, (d,), dev, "k_weight"), eps, 1 if rotate else 0,
+          _at(pos, _I32, (B, M), dev, "pos"), B, M, qo, Ka, Va, Lloc, local_pos0)
     return q_out
 
 
 def alloc_kv4(cfg, device="cuda"):
     """(K4, K4s, V4, V4s) of a bank in four bits: codes uint8 [N][Hkv][G][d/2], scale bytes uint8 [N][Hkv][G][d/32]."""
     rows = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len)
-    return tuple(torch.empty(rows + (cfg.head_dim // n,), dtype=torch.uint8, device=device) for n in (2, 32, 2, 32))
+    return tuple(torch.empty(rows + (cfg.head_dim // n,), dtype=_U8, device=device) for n in (2, 32, 2, 32))
 
 
-def _need_kv4(cfg, bank):
-    rows = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len)
-    for t, n, name in zip(bank, (2, 32, 2, 32), ("K4", "K4s", "V4", "V4s")):
-        if t is not None:
-            _need_shape(t, torch.uint8, rows + (cfg.head_dim // n,), name)
+def _kv4_at(cfg, bank, dev):
+    N, Hkv, G, d = cfg.n_docs, cfg.n_kv_heads, cfg.doc_len, cfg.head_dim
+    codes, scales = (N, Hkv, G, d // 2), (N, Hkv, G, d // 32)
+    return [None if t is None else _at(t, _U8, s, dev, n)
+            for t, s, n in zip(bank, (codes, scales, codes, scales), ("K4", "K4s", "V4", "V4s"))]
 
 
 def msa_pack_kv4(cfg, K, V, doc_begin=0, doc_count=None, bank=None, stream=None):
@@ -466,47 +474,51 @@ def msa_pack_kv4(cfg, K, V, doc_begin=0, doc_count=None, bank=None, stream=None)
     src = K if K is not None else V
     if src is None:
         raise ValueError("msa_pack_kv4: K and V are both None")
+    dev = _gpu(src, "msa_pack_kv4")
     shape = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len, cfg.head_dim)
-    for t, n in ((K, "K"), (V, "V")):
-        if t is not None:
-            _need_shape(t, torch.bfloat16, shape, n)
     if doc_count is None:
-        doc_count = cfg.n_docs - doc_begin
+        doc_count = shape[0] - doc_begin
     if bank is None:
         bank = alloc_kv4(cfg, src.device)
-    _need_kv4(cfg, bank)
-    _same_device(src, K, V, *bank)
-    out = [None if (K if i < 2 else V) is None else t for i, t in enumerate(bank)]
-    _call("msa_pack_kv4", src.device, ctypes.byref(cfg), _ptr(K), _ptr(V), doc_begin, doc_count, *map(_ptr, out),
-          _stream(stream, src.device))
+    K4, K4s, V4, V4s = _kv4_at(cfg, bank, dev)
+    Ka = Va = None
+    if K is None:
+        K4 = K4s = None
+    else:
+        Ka = _at(K, _BF16, shape, dev, "K")
+    if V is None:
+        V4 = V4s = None
+    else:
+        Va = _at(V, _BF16, shape, dev, "V")
+    _call("msa_pack_kv4", dev, stream, ctypes.byref(cfg), Ka, Va, doc_begin, doc_count, K4, K4s, V4, V4s)
     return bank
 
 
 def msa_unpack_kv4(cfg, bank, doc_begin=0, doc_count=None, K=None, V=None, stream=None):
     """What bank = (K4, K4s, V4, V4s) stands for -> (K, V) bf16 [N][Hkv][G][d], documents [doc_begin, doc_begin +
     doc_count) of it.  K4 and K4s, or V4 and V4s, may be None: that half comes back as None."""
-    _need_kv4(cfg, bank)
-    if (bank[0] is None) != (bank[1] is None) or (bank[2] is None) != (bank[3] is None):
-        raise ValueError("msa_unpack_kv4: codes come with their scale bytes")
-    src = bank[0] if bank[0] is not None else bank[2]
-    if src is None:
-        raise ValueError("msa_unpack_kv4: the bank is empty")
+    K4, K4s, V4, V4s = bank
+    src = K4 if K4 is not None else V4
+    if src is None or (K4 is None) != (K4s is None) or (V4 is None) != (V4s is None):
+        raise ValueError("msa_unpack_kv4: expected codes with their scale bytes")
+    dev = _gpu(src, "msa_unpack_kv4")
     shape = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len, cfg.head_dim)
-    out = []
-    for t, codes, n in ((K, bank[0], "K"), (V, bank[2], "V")):
-        if codes is None:
-            t = None
-        elif t is None:
-            t = torch.empty(shape, dtype=torch.bfloat16, device=src.device)
-        else:
-            _need_shape(t, torch.bfloat16, shape, n)
-        out.append(t)
     if doc_count is None:
-        doc_count = cfg.n_docs - doc_begin
-    _same_device(src, *bank, *out)
-    _call("msa_unpack_kv4", src.device, ctypes.byref(cfg), *map(_ptr, bank), doc_begin, doc_count, *map(_ptr, out),
-          _stream(stream, src.device))
-    return tuple(out)
+        doc_count = shape[0] - doc_begin
+    at = _kv4_at(cfg, bank, dev)
+    Ka = Va = None
+    if K4 is None:
+        K = None
+    else:
+        K = torch.empty(shape, dtype=_BF16, device=src.device) if K is None else K
+        Ka = _at(K, _BF16, shape, dev, "K")
+    if V4 is None:
+        V = None
+    else:
+        V = torch.empty(shape, dtype=_BF16, device=src.device) if V is None else V
+        Va = _at(V, _BF16, shape, dev, "V")
+    _call("msa_unpack_kv4", dev, stream, ctypes.byref(cfg), *at, doc_begin, doc_count, Ka, Va)
+    return K, V
 
 
 def window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks=0):
@@ -517,58 +529,55 @@ def sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc):
     return load_library().msa_sparse_attend4_workspace_bytes(ctypes.byref(cfg), B, M, k, Lloc)
 
 
-def _attend_buffers(cfg, q, out, lse, workspace, size):
-    B, M = q.shape[:2]
-    if out is None:
-        out = torch.empty_like(q)
-    if lse is None:
-        lse = torch.empty((B, M, cfg.n_q_heads), dtype=torch.float32, device=q.device)
-    if workspace is None:
-        workspace = torch.empty(max(size(), 256), dtype=torch.uint8, device=q.device)
-    _need_shape(out, torch.bfloat16, q.shape, "out")
-    _need_shape(lse, torch.float32, (B, M, cfg.n_q_heads), "lse")
-    _need(workspace, torch.uint8, "workspace")
-    return out, lse, workspace
+def _workspace_at(t, dev):
+    if t.dtype is not _U8 or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor of torch.uint8 on cuda:{dev}")
+    return t.data_ptr()
 
 
 def msa_window_attend(cfg, q, Kloc, Vloc, q_pos, window, sinks=0, local_pos0=0, out=None, lse=None, workspace=None,
                       stream=None):
     """q bf16 [B][M][Hq][d] and Kloc bf16 [B][Hkv][Lloc][d] as msa_norm_rotate writes them, Vloc, q_pos int32 [B][M] ->
     (out bf16 like q, lse fp32 [B][M][Hq]): attention over the last `window` tokens and the first `sinks`."""
-    B, M = q.shape[:2]
-    Lloc = Kloc.shape[2]
-    _need_shape(q, torch.bfloat16, (B, M, cfg.n_q_heads, cfg.head_dim), "q")
-    _need_shape(Kloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Kloc")
-    _need_shape(Vloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Vloc")
-    _need_shape(q_pos, torch.int32, (B, M), "q_pos")
-    out, lse, workspace = _attend_buffers(cfg, q, out, lse, workspace,
-                                          lambda: window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks))
-    _same_device(q, Kloc, Vloc, q_pos, out, lse, workspace)
-    _call("msa_window_attend", q.device, ctypes.byref(cfg), _ptr(q), B, M, _ptr(Kloc), _ptr(Vloc), Lloc, local_pos0, window,
-          sinks, _ptr(q_pos), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream, q.device))
+    Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    dev = _gpu(q, "q")
+    B, M, Lloc = q.shape[0], q.shape[1], Kloc.shape[2]
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty((B, M, Hq), dtype=_F32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), 256), dtype=_U8,
+                                device=q.device)
+    _call("msa_window_attend", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M,
+          _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc"), Lloc,
+          local_pos0, window, sinks, _at(q_pos, _I32, (B, M), dev, "q_pos"), _at(out, _BF16, (B, M, Hq, d), dev, "out"),
+          _at(lse, _F32, (B, M, Hq), dev, "lse"), _workspace_at(workspace, dev), workspace.numel())
     return out, lse
 
 
 def msa_sparse_attend4(cfg, q, bank, idx, Kloc, Vloc, local_pos0, q_pos, out=None, lse=None, workspace=None, stream=None):
     """msa_sparse_attend over bank = (K4, K4s, V4, V4s) of msa_pack_kv4; q and Kloc carry their positions (msa_norm_rotate).
     idx int32 [B][M'][S][k] as msa_score_topk writes it for cfg -> (out bf16 like q, lse fp32 [B][M][Hq])."""
-    B, M = q.shape[:2]
-    k = idx.shape[-1]
-    Lloc = 0 if Kloc is None else Kloc.shape[2]
-    _need_shape(q, torch.bfloat16, (B, M, cfg.n_q_heads, cfg.head_dim), "q")
-    _need_kv4(cfg, bank)
-    _need_shape(idx, torch.int32, (B, 1 if cfg.token_pool else M,
-                                   1 if cfg.select_scope == MSA_SCOPE_ALL else cfg.n_kv_heads, k), "idx")
+    Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    dev = _gpu(q, "q")
+    B, M, k = q.shape[0], q.shape[1], idx.shape[-1]
     if (Kloc is None) != (Vloc is None) or any(t is None for t in bank):
         raise ValueError("msa_sparse_attend4: keys come with their values")
+    Lloc, Ka, Va = 0, None, None
     if Kloc is not None:
-        _need_shape(Kloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Kloc")
-        _need_shape(Vloc, torch.bfloat16, (B, cfg.n_kv_heads, Lloc, cfg.head_dim), "Vloc")
-    _need_shape(q_pos, torch.int32, (B, M), "q_pos")
-    out, lse, workspace = _attend_buffers(cfg, q, out, lse, workspace,
-                                          lambda: sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc))
-    _same_device(q, *bank, idx, Kloc, Vloc, q_pos, out, lse, workspace)
-    _call("msa_sparse_attend4", q.device, ctypes.byref(cfg), _ptr(q), B, M, *map(_ptr, bank), _ptr(idx), k, _ptr(Kloc),
-          _ptr(Vloc), Lloc, local_pos0, _ptr(q_pos), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
-          _stream(stream, q.device))
+        Lloc = Kloc.shape[2]
+        Ka, Va = _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc")
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty((B, M, Hq), dtype=_F32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), 256), dtype=_U8, device=q.device)
+    K4, K4s, V4, V4s = _kv4_at(cfg, bank, dev)
+    lists = (B, 1 if cfg.token_pool else M, 1 if cfg.select_scope == MSA_SCOPE_ALL else Hkv, k)
+    _call("msa_sparse_attend4", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M, K4, K4s, V4,
+          V4s, _at(idx, _I32, lists, dev, "idx"), k, Ka, Va, Lloc, local_pos0, _at(q_pos, _I32, (B, M), dev, "q_pos"),
+          _at(out, _BF16, (B, M, Hq, d), dev, "out"), _at(lse, _F32, (B, M, Hq), dev, "lse"),
+          _workspace_at(workspace, dev), workspace.numel())
     return out, lse

@@ -422,7 +422,7 @@ int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, co
 int msa_pack_kv4(const msa_config_t* cfg, const void* K, const void* V, int32_t doc_begin, int32_t doc_count, void* K4,
                  void* K4s, void* V4, void* V4s, msa_stream_t stream) {
   Dims dm;
-  int rc = make_dims(cfg, &dm, kForAttend);
+  const int rc = make_dims(cfg, &dm, kForAttend);
   if (rc != MSA_OK) return rc;
   if (K == nullptr && V == nullptr) return MSA_ERR_INVALID_ARG;
   if ((K == nullptr) != (K4 == nullptr) || (K == nullptr) != (K4s == nullptr) || (V == nullptr) != (V4 == nullptr) ||
@@ -432,17 +432,14 @@ int msa_pack_kv4(const msa_config_t* cfg, const void* K, const void* V, int32_t 
   if (misaligned(K) || misaligned(V) || misaligned(K4) || misaligned(K4s) || misaligned(V4) || misaligned(V4s) ||
       misaligned4(dm.lens))
     return MSA_ERR_MISALIGNED;
-  if (K != nullptr) {
-    rc = launch_pack4(dm, K, doc_begin, doc_count, K4, K4s, cfg->bank_keys_rotated == 0, (hipStream_t)stream);
-    if (rc != MSA_OK) return rc;
-  }
-  return V != nullptr ? launch_pack4(dm, V, doc_begin, doc_count, V4, V4s, false, (hipStream_t)stream) : MSA_OK;
+  const Pack4Args x = {{(uint16_t*)K, (uint16_t*)V}, {(uint8_t*)K4, (uint8_t*)V4}, {(uint8_t*)K4s, (uint8_t*)V4s}};
+  return launch_pack4(dm, x, doc_begin, doc_count, cfg->bank_keys_rotated == 0, (hipStream_t)stream);
 }
 
 int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, const void* V4, const void* V4s,
                    int32_t doc_begin, int32_t doc_count, void* K, void* V, msa_stream_t stream) {
   Dims dm;
-  int rc = make_dims(cfg, &dm, kForAttend);
+  const int rc = make_dims(cfg, &dm, kForAttend);
   if (rc != MSA_OK) return rc;
   if (K == nullptr && V == nullptr) return MSA_ERR_INVALID_ARG;
   if ((K != nullptr && (K4 == nullptr || K4s == nullptr)) || (V != nullptr && (V4 == nullptr || V4s == nullptr)))
@@ -450,11 +447,8 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
   if (doc_begin < 0 || doc_count < 0 || (int64_t)doc_begin + doc_count > dm.N) return MSA_ERR_INVALID_ARG;
   if (misaligned(K) || misaligned(V) || misaligned(K4) || misaligned(K4s) || misaligned(V4) || misaligned(V4s))
     return MSA_ERR_MISALIGNED;
-  if (K != nullptr) {
-    rc = launch_unpack4(dm, K4, K4s, doc_begin, doc_count, K, (hipStream_t)stream);
-    if (rc != MSA_OK) return rc;
-  }
-  return V != nullptr ? launch_unpack4(dm, V4, V4s, doc_begin, doc_count, V, (hipStream_t)stream) : MSA_OK;
+  const Pack4Args x = {{(uint16_t*)K, (uint16_t*)V}, {(uint8_t*)K4, (uint8_t*)V4}, {(uint8_t*)K4s, (uint8_t*)V4s}};
+  return launch_unpack4(dm, x, doc_begin, doc_count, (hipStream_t)stream);
 }
 
 static int plan_window(const Dims& dm, int32_t B, int32_t M, int32_t Lloc, int32_t window, int32_t sinks, EncodedPlan* pl) {

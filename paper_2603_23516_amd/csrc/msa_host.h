@@ -206,10 +206,15 @@ struct NormArgs {
 int launch_norm_rotate(const Dims& dm, NormArgs a, hipStream_t st);
 
 // A bank in four bits (msa_kv4.hip).
-int launch_pack4(const Dims& dm, const void* X, int doc_begin, int doc_count, void* codes, void* scales, bool rotate,
-                 hipStream_t st);
-int launch_unpack4(const Dims& dm, const void* codes, const void* scales, int doc_begin, int doc_count, void* X,
-                   hipStream_t st);
+struct Pack4Args {  // [0] keys, [1] values; null = none of them
+  uint16_t* x[2];
+  uint8_t *codes[2], *scales[2];
+  const int32_t* lens;
+  long long n_rows;
+  int doc_begin, Hkv, G;
+};
+int launch_pack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, bool rotate, hipStream_t st);
+int launch_unpack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, hipStream_t st);
 
 inline size_t round_up256(size_t x) { return (x + 255) & ~(size_t)255; }
 

@@ -28,9 +28,9 @@ __device__ __forceinline__ int scale_byte(uint32_t amax_bits) {
 
 // ROT: keys that are not position-encoded yet are turned by their position in the document before they are rounded.
 template <int D, bool ROT>
-__global__ __launch_bounds__(256) void pack4_kernel(const uint16_t* __restrict__ X, uint8_t* __restrict__ codes,
-                                                    uint8_t* __restrict__ scales, const int32_t* __restrict__ lens,
-                                                    int doc_begin, long long n_rows, int Hkv, int G, NormTheta th) {
+__device__ __forceinline__ void pack4_rows(const uint16_t* __restrict__ X, uint8_t* __restrict__ codes,
+                                           uint8_t* __restrict__ scales, const int32_t* __restrict__ lens, int doc_begin,
+                                           long long n_rows, int Hkv, int G, const NormTheta& th) {
   constexpr int LPR = D / 8;          // lanes per row
   constexpr int RPB = 256 / LPR;      // rows per workgroup and turn
   const int lr = threadIdx.x % LPR;
@@ -81,9 +81,23 @@ __global__ __launch_bounds__(256) void pack4_kernel(const uint16_t* __restrict__
   }
 }
 
+// Keys by the first row of workgroups, values by the second; either may be absent.
+template <int D, bool ROT>
+__global__ __launch_bounds__(256) void pack4_kernel(Pack4Args a, NormTheta th) {
+  const bool values = a.x[0] == nullptr || blockIdx.y == 1;
+  if (!values)
+    pack4_rows<D, ROT>(a.x[0], a.codes[0], a.scales[0], a.lens, a.doc_begin, a.n_rows, a.Hkv, a.G, th);
+  else
+    pack4_rows<D, false>(a.x[1], a.codes[1], a.scales[1], a.lens, a.doc_begin, a.n_rows, a.Hkv, a.G, th);
+}
+
 template <int D>
-__global__ __launch_bounds__(256) void unpack4_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                      uint16_t* __restrict__ X, long long row0, long long n_rows) {
+__global__ __launch_bounds__(256) void unpack4_kernel(Pack4Args a) {
+  const int i = a.x[0] == nullptr || blockIdx.y == 1 ? 1 : 0;
+  const uint8_t* const codes = a.codes[i];
+  const uint8_t* const scales = a.scales[i];
+  uint16_t* const X = a.x[i];
+  const long long n_rows = a.n_rows, row0 = (long long)a.doc_begin * a.Hkv * a.G;
   constexpr int LPR = D / 8;
   constexpr int RPB = 256 / LPR;
   const int lr = threadIdx.x % LPR;
@@ -100,19 +114,26 @@ static unsigned stream_blocks(long long n_rows, int rows_per_block) {
   return (unsigned)(n < 1 ? 1 : (n > 16384 ? 16384 : n));
 }
 
-int launch_pack4(const Dims& dm, const void* X, int doc_begin, int doc_count, void* codes, void* scales, bool rotate,
-                 hipStream_t st) {
-  const long long n_rows = (long long)doc_count * dm.Hkv * dm.G;
-  if (n_rows == 0) return MSA_OK;
+static Pack4Args pack4_args(const Dims& dm, Pack4Args a, int doc_begin, int doc_count) {
+  a.lens = dm.lens;
+  a.doc_begin = doc_begin;
+  a.n_rows = (long long)doc_count * dm.Hkv * dm.G;
+  a.Hkv = dm.Hkv;
+  a.G = dm.G;
+  return a;
+}
+
+int launch_pack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, bool rotate, hipStream_t st) {
+  const Pack4Args a = pack4_args(dm, x, doc_begin, doc_count);
+  if (a.n_rows == 0) return MSA_OK;
   NormTheta th = {};
+  rotate = rotate && a.x[0] != nullptr;
   if (rotate) {
     const RopeTheta& table = rope_table(dm.base, dm.d);
     for (int u = 0; u < kMaxHalf; ++u) th.th[u] = table.th[u];
   }
-  const dim3 grid(stream_blocks(n_rows, 256 / (dm.d / 8)));
-#define MSA_PACK4(DD, RR)                                                                                             \
-  hipLaunchKernelGGL((pack4_kernel<DD, RR>), grid, dim3(256), 0, st, (const uint16_t*)X, (uint8_t*)codes, (uint8_t*)scales, \
-                     dm.lens, doc_begin, n_rows, dm.Hkv, dm.G, th)
+  const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8)), a.x[0] != nullptr && a.x[1] != nullptr ? 2 : 1);
+#define MSA_PACK4(DD, RR) hipLaunchKernelGGL((pack4_kernel<DD, RR>), grid, dim3(256), 0, st, a, th)
   if (dm.d == 128) {
     if (rotate) MSA_PACK4(128, true); else MSA_PACK4(128, false);
   } else {
@@ -122,17 +143,14 @@ int launch_pack4(const Dims& dm, const void* X, int doc_begin, int doc_count, vo
   return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
 }
 
-int launch_unpack4(const Dims& dm, const void* codes, const void* scales, int doc_begin, int doc_count, void* X,
-                   hipStream_t st) {
-  const long long n_rows = (long long)doc_count * dm.Hkv * dm.G, row0 = (long long)doc_begin * dm.Hkv * dm.G;
-  if (n_rows == 0) return MSA_OK;
-  const dim3 grid(stream_blocks(n_rows, 256 / (dm.d / 8)));
+int launch_unpack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, hipStream_t st) {
+  const Pack4Args a = pack4_args(dm, x, doc_begin, doc_count);
+  if (a.n_rows == 0) return MSA_OK;
+  const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8)), a.x[0] != nullptr && a.x[1] != nullptr ? 2 : 1);
   if (dm.d == 128)
-    hipLaunchKernelGGL(unpack4_kernel<128>, grid, dim3(256), 0, st, (const uint8_t*)codes, (const uint8_t*)scales,
-                       (uint16_t*)X, row0, n_rows);
+    hipLaunchKernelGGL(unpack4_kernel<128>, grid, dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL(unpack4_kernel<64>, grid, dim3(256), 0, st, (const uint8_t*)codes, (const uint8_t*)scales,
-                       (uint16_t*)X, row0, n_rows);
+    hipLaunchKernelGGL(unpack4_kernel<64>, grid, dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
 }
 
