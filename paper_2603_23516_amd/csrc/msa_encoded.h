@@ -29,12 +29,11 @@ struct TiledArgs {
   int* mem_rows;      // [B][Hkv] how many there are
   int mem_cap;        // k G
   int tpw, n_tiles;   // tokens per wave, tiles per sequence
-  int cb;             // 32-column blocks per wave
 };
 
 struct EncodedPlan {
   int tiled;           // 1: encoded_tiled_kernel, 0: encoded_decode_kernel
-  int n_splits, tpw, n_tiles, cb;
+  int n_splits, tpw, n_tiles;
   size_t off_ml, off_tickets;           // partials first, then their (max, sum), then the arrival counters
   size_t off_kx, off_vx, off_mem_rows;  // tiled, bank in four bits
   size_t ws_bytes;

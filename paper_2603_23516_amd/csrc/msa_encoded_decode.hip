@@ -280,18 +280,12 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   p.tiled = M >= 8 && (mem_rows == 0 || shared) ? 1 : 0;
   long long n, most;
   if (p.tiled) {
-    // 256 columns to a workgroup where that leaves one for every CU, 128 else; ranges of 4 steps at least
-    auto tiles = [&](int cb) {
-      p.cb = cb;
-      p.tpw = 32 * cb / dm.r;
-      p.n_tiles = (M + 4 * p.tpw - 1) / (4 * p.tpw);
-      return (long long)B * p.n_tiles * dm.Hkv;
-    };
-    long long t = tiles(2);
-    if (t < 256) t = tiles(1);
+    // 128 columns to a workgroup; up to three workgroups for every CU, ranges of 4 steps at least
+    p.tpw = 32 / dm.r;
+    p.n_tiles = (M + 4 * p.tpw - 1) / (4 * p.tpw);
     const long long seen = local_rows + 4 * p.tpw;
     const long long steps = (mem_rows + 31) / 32 + ((seen < Lloc ? seen : Lloc) + 31) / 32;
-    n = (p.cb == 2 ? 256 : 512) / t;
+    n = 768 / ((long long)B * p.n_tiles * dm.Hkv);
     most = steps / 4;
   } else {
     // about 1024 workgroups, ranges of 8 steps at least
@@ -341,7 +335,6 @@ int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, 
     TiledArgs ta = {};
     ta.tpw = pl.tpw;
     ta.n_tiles = pl.n_tiles;
-    ta.cb = pl.cb;
     if (a.K4 != nullptr) {
       ta.Kx = (uint16_t*)(w + pl.off_kx);
       ta.Vx = (uint16_t*)(w + pl.off_vx);
