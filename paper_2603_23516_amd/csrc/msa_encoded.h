@@ -44,9 +44,9 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
 int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, void* ws, hipStream_t st);
 int launch_encoded_tiled(const Dims& dm, const EncodedArgs& a, TiledArgs ta, int B, hipStream_t st);
 
-// The rows of a selection numbered through, by the 64 lanes of one wave: pre[j] rows lie in front of slot j's document docs[j];
-// pads, ids outside the bank and rows past a document's end are left out.  pre has MSA_MAX_TOPK + 1 entries.
-__device__ __forceinline__ void number_rows(const EncodedArgs& a, int b, long long bm, int g, int lane, int* pre, int* docs) {
+// The rows of a selection numbered through, by the 64 lanes of one wave: pre[j] rows lie in front of slot j's document, which
+// lane j gets back; pads, ids outside the bank and rows past a document's end are left out.  pre has MSA_MAX_TOPK + 1 entries.
+__device__ __forceinline__ int number_rows(const EncodedArgs& a, int b, long long bm, int g, int lane, int* pre) {
   int doc = -1, len = 0;
   if (lane < a.k) {
     doc = a.idx[((a.idx_rows_per_b == 1 ? b : bm) * a.idx_sel + (a.idx_sel == 1 ? 0 : g)) * a.k + lane];
@@ -64,9 +64,9 @@ __device__ __forceinline__ void number_rows(const EncodedArgs& a, int b, long lo
     const int up = __shfl_up(sum, off, 64);
     if (lane >= off) sum += up;
   }
-  docs[lane] = doc;
   pre[lane + 1] = sum;
   if (lane == 0) pre[0] = 0;
+  return doc;
 }
 
 // Rows of the local cache that a token at position p (counted from the cache's first row) sees: [0, first) and [from, to).

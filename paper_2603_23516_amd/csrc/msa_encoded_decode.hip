@@ -44,7 +44,7 @@ __device__ __forceinline__ Raw4<D> load_raw4(const uint8_t* p) {
 }
 
 template <int D, bool BANK4>
-__global__ __launch_bounds__(256) void encoded_decode_kernel(EncodedArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void encoded_decode_kernel(EncodedArgs a) {
   constexpr int NS = D / 32;   // contraction slices of the score product, and 32-bit words of a quarter row's codes
   constexpr int NC = D / 16;   // 16-row tiles of the output product
   constexpr int ROW = D * 2;   // bytes of a value row in LDS
@@ -52,7 +52,8 @@ __global__ __launch_bounds__(256) void encoded_decode_kernel(EncodedArgs a) {
   constexpr int STAGE = 32 * ROW > 8 * OROW * 4 ? 32 * ROW : 8 * OROW * 4;
   __shared__ __attribute__((aligned(16))) unsigned char stage[4][STAGE];
   __shared__ float wm[4][8], wl[4][8];
-  __shared__ int pre[MSA_MAX_TOPK + 1], docs[MSA_MAX_TOPK];
+  __shared__ int pre[MSA_MAX_TOPK + 1];
+  __shared__ long long base[MSA_MAX_TOPK];  // bank row of a slot's row i (numbered through) less i
   __shared__ uint32_t arrived;
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -63,7 +64,10 @@ __global__ __launch_bounds__(256) void encoded_decode_kernel(EncodedArgs a) {
 
   int rows_mem = 0;
   if (BANK4) {
-    if (wave == 0) number_rows(a, b, bm, g, lane, pre, docs);
+    if (wave == 0) {
+      const int doc = number_rows(a, b, bm, g, lane, pre);
+      base[lane] = ((long long)doc * a.Hkv + g) * a.G - pre[lane];
+    }
     __syncthreads();
     rows_mem = __builtin_amdgcn_readfirstlane(pre[MSA_MAX_TOPK]);
   }
@@ -111,7 +115,8 @@ __global__ __launch_bounds__(256) void encoded_decode_kernel(EncodedArgs a) {
       mx = fmaxf(mx, x[i]);
     }
     mx = max_xor16_32(mx);
-    if (__ballot(mx > m_run) != 0) {
+    // m_run is what the weights are taken relative to, not the maximum itself: it follows once that is 2^8 ahead
+    if (__ballot(mx > m_run + 8.f) != 0) {
       const float m_new = fmaxf(m_run, mx);
       const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
@@ -146,64 +151,120 @@ __global__ __launch_bounds__(256) void encoded_decode_kernel(EncodedArgs a) {
 
   int s = s_begin + wave;
   if (BANK4) {
-    int slot[2] = {0, 0};
-    for (; s < s_end && s < steps_mem; s += 4) {
-      Raw4<D> kc[2], vc[2];
-      float ks[2], vs[2];
+    // The wave's steps of bank rows, two in flight: a set of registers is filled again as soon as its codes have been turned
+    // into operands.  Loads have no condition (the wait for the older set would have to be one for everything): behind the
+    // last step they repeat it, out of the caches.
+    struct Set {
+      Raw4<D> k[2], v[2];
+      uint32_t ks[2], vs[2];
+    } sets[2];
+    const int s_stop = s_end < steps_mem ? s_end : steps_mem;
+    int slot[2] = {0, 0}, row[2], last[2];  // last: rows in front of the next slot
+    long long at[2];                        // bank row
+    int s_load = s;                         // the step that the next load brings
+    auto find = [&](int t) __attribute__((always_inline)) {
+      const int rc = row[t] < rows_mem ? row[t] : rows_mem - 1;
+      while (rc >= pre[slot[t] + 1]) ++slot[t];  // ends: rc < pre[k]
+      last[t] = pre[slot[t] + 1];
+      at[t] = base[slot[t]] + rc;
+    };
+    auto load = [&](Set& x) __attribute__((always_inline)) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        int row = 32 * s + 16 * t + n;
-        row = row < rows_mem ? row : rows_mem - 1;
-        while (row >= pre[slot[t] + 1]) ++slot[t];  // ends: row < pre[k]
-        const long long at = ((long long)docs[slot[t]] * a.Hkv + g) * a.G + (row - pre[slot[t]]);
-        kc[t] = load_raw4<D>(a.K4 + at * (D / 2) + (D / 8) * qd);
-        vc[t] = load_raw4<D>(a.V4 + at * (D / 2) + (D / 8) * qd);
-        const int sb = D == 128 ? qd : qd >> 1;
-        ks[t] = __uint_as_float((uint32_t)a.K4s[at * (D / 32) + sb] << 23);
-        vs[t] = __uint_as_float((uint32_t)a.V4s[at * (D / 32) + sb] << 23);
+        const long long c = at[t] * (D / 2) + (D / 8) * qd, e = at[t] * (D / 32) + (D == 128 ? qd : qd >> 1);
+        x.k[t] = load_raw4<D>(a.K4 + c);
+        x.v[t] = load_raw4<D>(a.V4 + c);
+        x.ks[t] = a.K4s[e];
+        x.vs[t] = a.V4s[e];
       }
+      if (s_load + 4 < s_stop) {
+        s_load += 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          row[t] += 128;
+          at[t] += 128;
+          if (row[t] >= last[t]) find(t);
+        }
+      }
+    };
+    auto turn = [&](Set& x) __attribute__((always_inline)) {
+      f32x4_t sc[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sc[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        const float ks = __uint_as_float(x.ks[t] << 23), vs = __uint_as_float(x.vs[t] << 23);
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          sc[t] = mfma16(as_bf16x8(fp4x8_to_bf16(x.k[t].w[j], ks)), bq4[j], sc[t]);
+          put(16 * t + n, NS * qd + j, fp4x8_to_bf16(x.v[t].w[j], vs));
+        }
+      }
+      load(x);
+      finish(sc[0], sc[1], rows_mem - 32 * s < 32 ? rows_mem - 32 * s : 32);
+      s += 4;
+    };
+    if (s < s_stop) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        row[t] = 32 * s + 16 * t + n;
+        find(t);
+      }
+      load(sets[0]);
+      load(sets[1]);
+      while (s + 4 < s_stop) {  // (in pairs, without a way out between them: the count of loads in flight stays known)
+        turn(sets[0]);
+        turn(sets[1]);
+      }
+      if (s < s_stop) turn(sets[0]);
+    }
+  }
+  const long long loc = ((long long)b * a.Hkv + g) * a.Lloc;
+  if (s < s_end) {
+    uint4 kx[2][NS], vx[2][NS];
+    int cnt = 0, t0 = 0, end = 0;
+    auto place = [&](int st) __attribute__((always_inline)) {
+      const int j0 = st - steps_mem;
+      t0 = 32 * j0;
+      end = see.first;
+      if (j0 >= steps_a) {
+        t0 += see.from - 32 * steps_a;
+        end = see.to;
+      }
+    };
+    auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        int row = t0 + 16 * t + n;
+        row = row < end ? row : end - 1;
+        const uint16_t* kp = a.Kloc + (loc + row) * D + 8 * qd;
+        const uint16_t* vp = a.Vloc + (loc + row) * D + 8 * qd;
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          kx[t][j] = *reinterpret_cast<const uint4*>(kp + 32 * j);
+          vx[t][j] = *reinterpret_cast<const uint4*>(vp + 32 * j);
+        }
+      }
+    };
+    place(s);
+    load();
+    for (; s < s_end; s += 4) {
       f32x4_t sc[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         sc[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-          sc[t] = mfma16(as_bf16x8(fp4x8_to_bf16(kc[t].w[j], ks[t])), bq4[j], sc[t]);
-          put(16 * t + n, NS * qd + j, fp4x8_to_bf16(vc[t].w[j], vs[t]));
+          sc[t] = mfma16(as_bf16x8(kx[t][j]), bq[j], sc[t]);
+          put(16 * t + n, 4 * j + qd, vx[t][j]);
         }
       }
-      finish(sc[0], sc[1], rows_mem - 32 * s < 32 ? rows_mem - 32 * s : 32);
-    }
-  }
-  const long long loc = ((long long)b * a.Hkv + g) * a.Lloc;
-  for (; s < s_end; s += 4) {
-    const int j0 = s - steps_mem;
-    const int t0 = j0 < steps_a ? 32 * j0 : see.from + 32 * (j0 - steps_a);
-    const int end = j0 < steps_a ? see.first : see.to;
-    uint4 kx[2][NS], vx[2][NS];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      int row = t0 + 16 * t + n;
-      row = row < end ? row : end - 1;
-      const uint16_t* kp = a.Kloc + (loc + row) * D + 8 * qd;
-      const uint16_t* vp = a.Vloc + (loc + row) * D + 8 * qd;
-#pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        kx[t][j] = *reinterpret_cast<const uint4*>(kp + 32 * j);
-        vx[t][j] = *reinterpret_cast<const uint4*>(vp + 32 * j);
+      cnt = end - t0 < 32 ? end - t0 : 32;
+      if (s + 4 < s_end) {
+        place(s + 4);
+        load();  // under way while this step's weights are worked out
       }
+      finish(sc[0], sc[1], cnt);
     }
-    f32x4_t sc[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      sc[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        sc[t] = mfma16(as_bf16x8(kx[t][j]), bq[j], sc[t]);
-        put(16 * t + n, 4 * j + qd, vx[t][j]);
-      }
-    }
-    finish(sc[0], sc[1], end - t0 < 32 ? end - t0 : 32);
   }
 
   // ---- the four waves' results, then the splits' --------------------------------------------------------------
@@ -254,22 +315,36 @@ __global__ __launch_bounds__(256) void encoded_decode_kernel(EncodedArgs a) {
   __syncthreads();
   if (arrived != (uint32_t)a.n_splits - 1) return;
   if (tid == 0) store_dev(ticket, 0ull);
-  for (int e = tid; e < r * D; e += 256) {
+  // All (max, sum) pairs at once, then the outputs eight splits at a time: loads past the L2 take over a microsecond, and one
+  // after another for 16 splits they were a third of a call of 92 us.
+  float2* const parts = reinterpret_cast<float2*>(stage[0]);  // [r][n_splits], 256 at most
+  for (int e = tid; e < r * a.n_splits; e += 256) {
+    const unsigned long long ml = load_dev(reinterpret_cast<const unsigned long long*>(a.part_ml + qh0 * a.n_splits + e));
+    parts[e] = make_float2(__uint_as_float((uint32_t)ml), __uint_as_float((uint32_t)(ml >> 32)));
+  }
+  __syncthreads();
+  for (int e = 2 * tid; e < r * D; e += 512) {
     const int hh = e / D, dd = e % D;
-    const long long ph = (qh0 + hh) * a.n_splits;
-    float m = -INFINITY, l = 0.f, x = 0.f;
-    for (int i = 0; i < a.n_splits; ++i) {
-      const unsigned long long ml = load_dev(reinterpret_cast<const unsigned long long*>(a.part_ml + ph + i));
-      const float mi = __uint_as_float((uint32_t)ml), li = __uint_as_float((uint32_t)(ml >> 32));
-      const float xi = load_dev(a.part_o + (ph + i) * D + dd);
-      if (mi == -INFINITY) continue;
-      const float mn = fmaxf(m, mi);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), fi = __builtin_amdgcn_exp2f(mi - mn);
-      l = l * f + li * fi;
-      x = x * f + xi * fi;
-      m = mn;
+    const float2* const ml = parts + hh * a.n_splits;
+    float m = -INFINITY, l = 0.f, x0 = 0.f, x1 = 0.f;
+    for (int i = 0; i < a.n_splits; ++i) m = fmaxf(m, ml[i].x);
+    const float* const po = a.part_o + (qh0 + hh) * a.n_splits * D + dd;
+    for (int i0 = 0; i0 < a.n_splits; i0 += 8) {
+      unsigned long long v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        v[u] = load_dev(reinterpret_cast<const unsigned long long*>(po + (i0 + u < a.n_splits ? i0 + u : a.n_splits - 1) * D));
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        float f = 0.f;
+        if (i0 + u < a.n_splits && ml[i0 + u].x != -INFINITY) f = __builtin_amdgcn_exp2f(ml[i0 + u].x - m);
+        if (i0 + u < a.n_splits) l += f * ml[i0 + u].y;
+        x0 += f * __uint_as_float((uint32_t)v[u]);
+        x1 += f * __uint_as_float((uint32_t)(v[u] >> 32));
+      }
     }
-    a.out[(qh0 + hh) * D + dd] = (uint16_t)pack_bf16(l > 0.f ? x / l : 0.f, 0.f);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    *reinterpret_cast<uint32_t*>(a.out + (qh0 + hh) * D + dd) = pack_bf16(x0 * inv, x1 * inv);
     if (dd == 0 && a.lse != nullptr) a.lse[qh0 + hh] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
   }
 }
