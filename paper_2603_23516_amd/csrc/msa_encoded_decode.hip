@@ -26,6 +26,8 @@ __device__ __forceinline__ float max_xor16_32(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+constexpr int kLocalCost = 3;
+
 template <int D>
 struct Raw4 {  // a quarter of a row in four bits
   uint32_t w[D / 32];
@@ -60,21 +62,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qd = lane >> 4, n = lane & 15, h = n & 7;
   const int sp = blockIdx.x, g = blockIdx.y, bm = blockIdx.z, b = bm / a.M, r = a.r;
-  const Seen see = seen_rows((long long)a.q_pos[bm] - a.pos0, a.Lloc, a.window, a.sinks);
-
-  int rows_mem = 0;
-  if (BANK4) {
-    if (wave == 0) {
-      const int doc = number_rows(a, b, bm, g, lane, pre);
-      base[lane] = ((long long)doc * a.Hkv + g) * a.G - pre[lane];
-    }
-    __syncthreads();
-    rows_mem = __builtin_amdgcn_readfirstlane(pre[MSA_MAX_TOPK]);
-  }
-  const int steps_mem = (rows_mem + 31) / 32, steps_a = (see.first + 31) / 32, steps_b = (see.to - see.from + 31) / 32;
-  const int steps = steps_mem + steps_a + steps_b;
-  const int s_begin = (int)((long long)steps * sp / a.n_splits), s_end = (int)((long long)steps * (sp + 1) / a.n_splits);
-
+  const int q_pos = a.q_pos[bm];  // (asked for together with the queries and the selection: each is a microsecond away)
   // queries: column n holds head n % 8; B operand of slice s: dims 32 s + 8 qd .. + 8 (local rows), or the s-th eight dims of
   // the qd-th quarter (bank rows)
   bf16x8_t bq[NS], bq4[BANK4 ? NS : 1];
@@ -92,6 +80,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       }
     }
   }
+
+  const Seen see = seen_rows((long long)q_pos - a.pos0, a.Lloc, a.window, a.sinks);
+
+  int rows_mem = 0;
+  if (BANK4) {
+    if (wave == 0) {
+      const int doc = number_rows(a, b, bm, g, lane, pre);
+      base[lane] = ((long long)doc * a.Hkv + g) * a.G - pre[lane];
+    }
+    lds_barrier();
+    rows_mem = __builtin_amdgcn_readfirstlane(pre[MSA_MAX_TOPK]);
+  }
+  const int steps_mem = (rows_mem + 31) / 32, steps_a = (see.first + 31) / 32, steps_b = (see.to - see.from + 31) / 32;
+  // A step of local rows is 16 KiB, one of bank rows 4.25 (d = 128): it counts as kLocalCost of those in the shares.
+  const long long cost = steps_mem + (long long)kLocalCost * (steps_a + steps_b);
+  auto share = [&](int i) {
+    const int c = (int)(cost * i / a.n_splits);
+    return c <= steps_mem ? c : steps_mem + (c - steps_mem) / kLocalCost;
+  };
+  const int s_begin = share(sp), s_end = share(sp + 1);
 
   // Value rows in LDS: 16-byte piece p of row i lies at place p ^ swz(i), so that neither the writes (16 rows, one piece) nor
   // the transposing reads (four rows, two pieces) meet in a bank.
@@ -353,22 +361,36 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   EncodedPlan p = {};
   const long long pairs = (long long)B * M * dm.Hkv;
   p.tiled = M >= 8 && (mem_rows == 0 || shared) ? 1 : 0;
-  long long n, most;
+  int n_most;  // splits that the workspace holds: grows with the rows, so that one sized for the longest call serves all
   if (p.tiled) {
     // 128 columns to a workgroup; up to three workgroups for every CU, ranges of 4 steps at least
     p.tpw = 32 / dm.r;
     p.n_tiles = (M + 4 * p.tpw - 1) / (4 * p.tpw);
     const long long seen = local_rows + 4 * p.tpw;
     const long long steps = (mem_rows + 31) / 32 + ((seen < Lloc ? seen : Lloc) + 31) / 32;
-    n = 768 / ((long long)B * p.n_tiles * dm.Hkv);
-    most = steps / 4;
+    long long n = 768 / ((long long)B * p.n_tiles * dm.Hkv);
+    if (n > steps / 4) n = steps / 4;
+    p.n_splits = n_most = (int)(n < 1 ? 1 : (n > 32 ? 32 : n));
   } else {
-    // about 1024 workgroups, ranges of 8 steps at least
-    n = (1024 + pairs - 1) / pairs;
-    most = ((mem_rows + 31) / 32 + (local_rows + 31) / 32 + 7) / 8;
+    // Two workgroups fit a CU.  A workgroup takes about 9 us beside its steps (three loads that wait for one another, then
+    // the joining of four waves), its steps 0.7 us each where it has a CU to itself and 1.2 beside another, and the join of
+    // n parts 3 us and 0.3 for each (8 heads, 8 streams, 512 steps of bank rows and 64 local ones: n = 2 76 us, 4 45,
+    // 6 47, 8 41, 12 46, 16 50; 32 streams, 8 and 32 steps: n = 2 30 us, 4 35, 8 52, 16 97; one stream, 256 and 64: 50, 29,
+    // 23, 19, 17, 15).
+    const long long cost = (mem_rows + 31) / 32 + kLocalCost * ((local_rows + 31) / 32);
+    long long most = (cost + 15) / 16;
+    if (most > 2048 / pairs) most = 2048 / pairs;
+    n_most = (int)(most < 1 ? 1 : (most > 32 ? 32 : most));
+    long long best = -1;
+    for (int n = 1; n <= n_most; ++n) {
+      const long long all = pairs * n, steps = (cost + 4 * n - 1) / (4 * n);
+      const long long t = (all + 511) / 512 * (90 + (all <= 256 ? 7 : 12) * steps) + (n > 1 ? 30 + 3 * n : 0);
+      if (best < 0 || t < best) {
+        best = t;
+        p.n_splits = n;
+      }
+    }
   }
-  if (n > most) n = most;
-  p.n_splits = (int)(n < 1 ? 1 : (n > 32 ? 32 : n));
   const size_t heads = (size_t)B * M * dm.Hq;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -376,9 +398,9 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     at += round_up256(bytes);
     return here;
   };
-  if (p.n_splits > 1) {
-    take(heads * p.n_splits * dm.d * sizeof(float));
-    p.off_ml = take(heads * p.n_splits * sizeof(float2));
+  if (n_most > 1) {
+    take(heads * n_most * dm.d * sizeof(float));
+    p.off_ml = take(heads * n_most * sizeof(float2));
     if (!p.tiled) p.off_tickets = take((size_t)pairs * sizeof(unsigned long long));
   }
   if (p.tiled && mem_rows > 0) {
