@@ -363,14 +363,33 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   p.tiled = M >= 8 && (mem_rows == 0 || shared) ? 1 : 0;
   int n_most;  // splits that the workspace holds: grows with the rows, so that one sized for the longest call serves all
   if (p.tiled) {
-    // 128 columns to a workgroup; up to three workgroups for every CU, ranges of 4 steps at least
+    // 128 columns to a workgroup.  With one, two or three on every CU a step takes 0.80, 0.95 or 1.32 us (d = 64: 0.48, 0.56,
+    // 0.76), a workgroup 6 beside its steps; parts have to be written and joined, 4 us and 0.25 + 0.05 n for every 1000 of
+    // the (token, head) rows, and n rows of d floats at 5 TB/s.  (1000 tokens over 8192 and 1000 rows, 8 heads: n = 1 239
+    // us, 2 164, 3 162, 4 171, 8 183; 128 tokens over 4096: 91, 53, 40, 33, n = 8 27, 16 30; 4 times 509 tokens of 64 dims
+    // over 1000 rows: 26, 37, 38, 40.)
     p.tpw = 32 / dm.r;
     p.n_tiles = (M + 4 * p.tpw - 1) / (4 * p.tpw);
+    const long long tiles = (long long)B * p.n_tiles * dm.Hkv, heads = (long long)B * M * dm.Hq;
     const long long seen = local_rows + 4 * p.tpw;
-    const long long steps = (mem_rows + 31) / 32 + ((seen < Lloc ? seen : Lloc) + 31) / 32;
-    long long n = 768 / ((long long)B * p.n_tiles * dm.Hkv);
-    if (n > steps / 4) n = steps / 4;
-    p.n_splits = n_most = (int)(n < 1 ? 1 : (n > 32 ? 32 : n));
+    const long long all_steps = (mem_rows + 31) / 32 + ((seen < Lloc ? seen : Lloc) + 31) / 32;
+    long long most = all_steps / 4;
+    if (most > 1024 / tiles) most = 1024 / tiles;
+    n_most = (int)(most < 1 ? 1 : (most > 32 ? 32 : most));
+    const int ns_per_step[2][3] = {{480, 560, 760}, {800, 950, 1320}};
+    long long best = -1;
+    for (int n = 1; n <= n_most; ++n) {
+      const long long all = tiles * n, steps = (all_steps + n - 1) / n;
+      const long long per_cu = (all + 255) / 256 < 3 ? (all + 255) / 256 : 3;
+      long long t = steps * ns_per_step[dm.d == 128][per_cu - 1];
+      if (all > 768) t = t * all / 768;
+      t += 6000;
+      if (n > 1) t += 4000 + heads * (250 + 50 * n) / 1000 + heads * n * dm.d * 4 / 5000;
+      if (best < 0 || t < best) {
+        best = t;
+        p.n_splits = n;
+      }
+    }
   } else {
     // Two workgroups fit a CU.  A workgroup takes about 9 us beside its steps (three loads that wait for one another, then
     // the joining of four waves), its steps 0.7 us each where it has a CU to itself and 1.2 beside another, and the join of
@@ -391,7 +410,7 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
       }
     }
   }
-  const size_t heads = (size_t)B * M * dm.Hq;
+  const size_t rows = (size_t)B * M * dm.Hq;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -399,8 +418,8 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     return here;
   };
   if (n_most > 1) {
-    take(heads * n_most * dm.d * sizeof(float));
-    p.off_ml = take(heads * n_most * sizeof(float2));
+    take(rows * n_most * dm.d * sizeof(float));
+    p.off_ml = take(rows * n_most * sizeof(float2));
     if (!p.tiled) p.off_tickets = take((size_t)pairs * sizeof(unsigned long long));
   }
   if (p.tiled && mem_rows > 0) {
