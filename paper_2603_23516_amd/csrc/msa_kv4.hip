@@ -26,8 +26,30 @@ __device__ __forceinline__ int scale_byte(uint32_t amax_bits) {
   return e < 2 ? 2 : (e > 252 ? 252 : e);
 }
 
+// Eight elements of a row of a block -> their codes; the quad's first lane writes the block's scale byte.
+template <int D>
+__device__ __forceinline__ void pack4_eight(const float (&f)[8], uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                            long long row, int lr) {
+  uint32_t amax = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t m = __float_as_uint(f[j]) & 0x7fffffffu;
+    amax = m > amax ? m : amax;
+  }
+  const int e = scale_byte(quad_max_u(amax));
+  const float s = __uint_as_float((uint32_t)e << 23);
+  uint32_t c4 = 0;
+  c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[0], f[1], s, 0);
+  c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[2], f[3], s, 1);
+  c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[4], f[5], s, 2);
+  c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[6], f[7], s, 3);
+  *reinterpret_cast<uint32_t*>(codes + row * (D / 2) + 4 * lr) = c4;
+  if ((lr & 3) == 0) scales[row * (D / 32) + lr / 4] = (uint8_t)e;
+}
+
 // ROT: keys that are not position-encoded yet are turned by their position in the document before they are rounded.
-template <int D, bool ROT>
+// A thread has ROWS rows in flight.
+template <int D, bool ROT, int ROWS, bool STREAM>
 __device__ __forceinline__ void pack4_rows(const uint16_t* __restrict__ X, uint8_t* __restrict__ codes,
                                            uint8_t* __restrict__ scales, const int32_t* __restrict__ lens, int doc_begin,
                                            long long n_rows, int Hkv, int G, const NormTheta& th) {
@@ -35,60 +57,57 @@ __device__ __forceinline__ void pack4_rows(const uint16_t* __restrict__ X, uint8
   constexpr int RPB = 256 / LPR;      // rows per workgroup and turn
   const int lr = threadIdx.x % LPR;
   const long long row0 = (long long)doc_begin * Hkv * G;
-  for (long long r = (long long)blockIdx.x * RPB + threadIdx.x / LPR; r < n_rows; r += (long long)gridDim.x * RPB) {
-    const long long row = row0 + r;
-    bool live = true;
-    int t = 0;
-    if (ROT || lens != nullptr) {
-      const long long slab = row / G;
-      t = (int)(row - slab * G);
-      if (lens != nullptr) {
-        int len = lens[slab / Hkv];
-        len = len < 1 ? 1 : (len > G ? G : len);
-        live = t < len;
+  for (long long r0 = (long long)blockIdx.x * (RPB * ROWS) + threadIdx.x / LPR; r0 < n_rows;
+       r0 += (long long)gridDim.x * (RPB * ROWS)) {
+    uint4 x[ROWS];
+    int t[ROWS];
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+      const long long r = r0 + u * RPB, row = row0 + r;
+      bool live = r < n_rows;
+      t[u] = 0;
+      if (live && (ROT || lens != nullptr)) {
+        const long long slab = row / G;
+        t[u] = (int)(row - slab * G);
+        if (lens != nullptr) {
+          int len = lens[slab / Hkv];
+          len = len < 1 ? 1 : (len > G ? G : len);
+          live = t[u] < len;
+        }
       }
+      x[u] = make_uint4(0, 0, 0, 0);
+      if (live) x[u] = STREAM ? load_stream16(X + row * D + 8 * lr) : *reinterpret_cast<const uint4*>(X + row * D + 8 * lr);
     }
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (live) x = *reinterpret_cast<const uint4*>(X + row * D + 8 * lr);
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    float f[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
-    if (ROT) {
-      const bool second = lr >= LPR / 2;
+    for (int u = 0; u < ROWS; ++u) {
+      const long long r = r0 + u * RPB;
+      if (r >= n_rows) break;  // the same for the lanes of a row
+      const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      float f[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float o = __shfl_xor(f[j], LPR / 2, 64);
-        const float2 c = cis_pos(t, th.th[8 * (lr & (LPR / 2 - 1)) + j]);
-        f[j] = f[j] * c.x + (second ? o : -o) * c.y;
+      for (int j = 0; j < 8; ++j) f[j] = j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+      if (ROT) {
+        const bool second = lr >= LPR / 2;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float o = __shfl_xor(f[j], LPR / 2, 64);
+          const float2 c = cis_pos(t[u], th.th[8 * (lr & (LPR / 2 - 1)) + j]);
+          f[j] = f[j] * c.x + (second ? o : -o) * c.y;
+        }
       }
+      pack4_eight<D>(f, codes, scales, row0 + r, lr);
     }
-    uint32_t amax = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t m = __float_as_uint(f[j]) & 0x7fffffffu;
-      amax = m > amax ? m : amax;
-    }
-    const int e = scale_byte(quad_max_u(amax));
-    const float s = __uint_as_float((uint32_t)e << 23);
-    uint32_t c4 = 0;
-    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[0], f[1], s, 0);
-    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[2], f[3], s, 1);
-    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[4], f[5], s, 2);
-    c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[6], f[7], s, 3);
-    *reinterpret_cast<uint32_t*>(codes + row * (D / 2) + 4 * lr) = c4;
-    if ((lr & 3) == 0) scales[row * (D / 32) + lr / 4] = (uint8_t)e;
   }
 }
 
 // Keys by the first row of workgroups, values by the second; either may be absent.
-template <int D, bool ROT>
+template <int D, bool ROT, int ROWS, bool STREAM>
 __global__ __launch_bounds__(256) void pack4_kernel(Pack4Args a, NormTheta th) {
   const bool values = a.x[0] == nullptr || blockIdx.y == 1;
   if (!values)
-    pack4_rows<D, ROT>(a.x[0], a.codes[0], a.scales[0], a.lens, a.doc_begin, a.n_rows, a.Hkv, a.G, th);
+    pack4_rows<D, ROT, ROWS, STREAM>(a.x[0], a.codes[0], a.scales[0], a.lens, a.doc_begin, a.n_rows, a.Hkv, a.G, th);
   else
-    pack4_rows<D, false>(a.x[1], a.codes[1], a.scales[1], a.lens, a.doc_begin, a.n_rows, a.Hkv, a.G, th);
+    pack4_rows<D, false, ROWS, STREAM>(a.x[1], a.codes[1], a.scales[1], a.lens, a.doc_begin, a.n_rows, a.Hkv, a.G, th);
 }
 
 template <int D>
@@ -108,6 +127,8 @@ __global__ __launch_bounds__(256) void unpack4_kernel(Pack4Args a) {
     *reinterpret_cast<uint4*>(X + row * D + 8 * lr) = fp4x8_to_bf16(c4, s);
   }
 }
+
+constexpr long long kStreamBytes = 128ll << 20;
 
 static unsigned stream_blocks(long long n_rows, int rows_per_block) {
   const long long n = (n_rows + rows_per_block - 1) / rows_per_block;
@@ -132,8 +153,18 @@ int launch_pack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, bool
     const RopeTheta& table = rope_table(dm.base, dm.d);
     for (int u = 0; u < kMaxHalf; ++u) th.th[u] = table.th[u];
   }
-  const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8)), a.x[0] != nullptr && a.x[1] != nullptr ? 2 : 1);
-#define MSA_PACK4(DD, RR) hipLaunchKernelGGL((pack4_kernel<DD, RR>), grid, dim3(256), 0, st, a, th)
+  // From 131072 rows of a tensor on four rows to a thread, which gives fewer waves with more in flight each (262144 rows of 128
+  // dims, packed and unpacked, 58 -> 53 us; 64064 rows 17.4 -> 19.0), from 128 MiB on streaming loads (2 million rows 540 ->
+  // 504 with both).
+  const int n_tensors = a.x[0] != nullptr && a.x[1] != nullptr ? 2 : 1;
+  const bool many = a.n_rows >= 131072, stream = many && a.n_rows * dm.d * 2 * n_tensors >= kStreamBytes;
+  const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8) * (many ? 4 : 1)), n_tensors);
+#define MSA_PACK4(DD, RR)                                                                                \
+  do {                                                                                                   \
+    if (stream) hipLaunchKernelGGL((pack4_kernel<DD, RR, 4, true>), grid, dim3(256), 0, st, a, th);      \
+    else if (many) hipLaunchKernelGGL((pack4_kernel<DD, RR, 4, false>), grid, dim3(256), 0, st, a, th);  \
+    else hipLaunchKernelGGL((pack4_kernel<DD, RR, 1, false>), grid, dim3(256), 0, st, a, th);            \
+  } while (0)
   if (dm.d == 128) {
     if (rotate) MSA_PACK4(128, true); else MSA_PACK4(128, false);
   } else {

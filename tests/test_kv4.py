@@ -134,3 +134,21 @@ def test_keys_turned_by_their_positions(d, G):
     assert float(close.double().mean()) < 1e-3
     y0 = y * s
     assert bool(((got.abs() - y0).abs()[close] <= s[close] * (1 + 2.0 ** -10)).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N, G, d, lens", [(130000, 1, 64, False), (131200, 1, 64, True), (2100, 63, 64, False), (2200, 512, 128, True)])
+def test_many_rows_are_packed_as_few(N, G, d, lens):
+    """Large banks take other loads: a document anywhere in them has the bits it gets alone."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    K = torch.randn((N, 1, G, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    V = torch.randn((N, 1, G, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    n = torch.randint(1, G + 1, (N,), generator=g, device="cuda", dtype=torch.int32) if lens else None
+    cfg = _cfg(N, G, 1, d, lens=n)
+    bank = msa.msa_pack_kv4(cfg, K, V)
+    back = msa.msa_unpack_kv4(cfg, bank)
+    for i in (0, 1, N // 3, N - 2, N - 1):
+        one = _cfg(1, G, 1, d, lens=None if n is None else n[i:i + 1].contiguous())
+        alone = msa.msa_pack_kv4(one, K[i:i + 1], V[i:i + 1])
+        assert all(torch.equal(a[i:i + 1], b) for a, b in zip(bank, alone)), i
+        assert all(torch.equal(a[i:i + 1], b) for a, b in zip(back, msa.msa_unpack_kv4(one, alone))), i

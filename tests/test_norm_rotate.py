@@ -157,3 +157,22 @@ def test_python_refusals():
         msa.msa_norm_rotate(cfg, q[..., ::2], None, None, pos, None, None)
     with pytest.raises(ValueError):
         msa.msa_norm_rotate(cfg, q, q[:, :, :2], None, pos, None, None)              # keys without their cache
+
+
+@pytest.mark.gpu
+def test_a_long_prompt_is_read_with_streaming_loads():
+    """A projection of more than 128 MiB takes other loads: the bits are those of its tokens alone."""
+    M, Hq, Hkv, d = 20000, 16, 8, 128
+    cfg = _cfg(Hq, Hkv, d)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn((1, M, Hq + 2 * Hkv, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(d, generator=g, device="cuda", dtype=torch.bfloat16)
+    pos = torch.arange(M, dtype=torch.int32, device="cuda").reshape(1, M)
+    K, V = (torch.zeros((1, Hkv, M, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = msa.msa_norm_rotate(cfg, x[:, :, :Hq], x[:, :, Hq:Hq + Hkv], x[:, :, Hq + Hkv:], pos, K, V, w, w)
+    for m0 in (0, 7777, M - 5):
+        K1, V1 = (torch.zeros((1, Hkv, 5, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        y = x[:, m0:m0 + 5]
+        q1 = msa.msa_norm_rotate(cfg, y[:, :, :Hq], y[:, :, Hq:Hq + Hkv], y[:, :, Hq + Hkv:], pos[:, m0:m0 + 5].contiguous(), K1, V1, w, w,
+                                 local_pos0=m0)
+        assert torch.equal(q[:, m0:m0 + 5], q1) and torch.equal(K[:, :, m0:m0 + 5], K1) and torch.equal(V[:, :, m0:m0 + 5], V1)
