@@ -397,8 +397,8 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *   q_pos     in   int32 [B][M]
  *   out       out  bf16 [B][M][Hq][d]
  *   lse       out  fp32 [B][M][Hq], may be NULL
- *   workspace      >= msa_sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc); with token_pool = 1 and M >= 8 it holds the
- *                  selected documents in bf16, B * Hkv * k * G * d * 4 bytes
+ *   workspace      >= msa_sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc); where many tokens share a selection
+ *                  (token_pool = 1) it holds the selected documents in bf16, B * Hkv * k * G * d * 4 bytes
  */
 size_t msa_sparse_attend4_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t k, int32_t Lloc);
 int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* K4, const void* K4s,

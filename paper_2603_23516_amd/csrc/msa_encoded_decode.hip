@@ -360,7 +360,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc) {
   EncodedPlan p = {};
   const long long pairs = (long long)B * M * dm.Hkv;
-  p.tiled = M >= 8 && (mem_rows == 0 || shared) ? 1 : 0;
+  // Tokens that share their rows go through the tiled kernel where the single-token kernel would take long over them: its steps
+  // of all tokens (`work`; local ones count kLocalCost) against what the tiled kernel's launches, its thin tiles and the
+  // documents' expansion cost.  us, tiled / one by one, M tokens: 8 heads of 128 over 2048 rows, M = 4 12 / 14, 16 14 / 22;
+  // 8 sequences over 4096 rows, M = 2 40 / 36, 4 40 / 63, 8 31 / 115; heads of 64 that share nothing (r = 1) over 2048 rows,
+  // M = 8 14 / 11, 16 14 / 14; 16 documents of 512, M = 4 40 / 17, 16 39 / 33; 3 times 8 of 64, M = 8 20 / 16, 16 22 / 25.
+  const long long cost = (mem_rows + 31) / 32 + kLocalCost * ((local_rows + 31) / 32), work = pairs * cost;
+  p.tiled = (mem_rows == 0 || shared) && (M >= 32 || (M >= 4 && work >= 20000 + B * dm.Hkv * mem_rows / 4)) ? 1 : 0;
   int n_most;  // splits that the workspace holds: grows with the rows, so that one sized for the longest call serves all
   if (p.tiled) {
     // 128 columns to a workgroup.  With one, two or three on every CU a step takes 0.80, 0.95 or 1.32 us (d = 64: 0.48, 0.56,
@@ -396,7 +402,6 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     // n parts 3 us and 0.3 for each (8 heads, 8 streams, 512 steps of bank rows and 64 local ones: n = 2 76 us, 4 45,
     // 6 47, 8 41, 12 46, 16 50; 32 streams, 8 and 32 steps: n = 2 30 us, 4 35, 8 52, 16 97; one stream, 256 and 64: 50, 29,
     // 23, 19, 17, 15).
-    const long long cost = (mem_rows + 31) / 32 + kLocalCost * ((local_rows + 31) / 32);
     long long most = (cost + 15) / 16;
     if (most > 2048 / pairs) most = 2048 / pairs;
     n_most = (int)(most < 1 ? 1 : (most > 32 ? 32 : most));
