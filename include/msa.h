@@ -32,7 +32,8 @@
  *   - Errors: 0 on success, a negative msa_status otherwise.  Arguments are validated on the host
  *     before anything is enqueued, so an error return (other than MSA_ERR_HIP) means no work was
  *     launched and no GPU is needed to observe it.  No exceptions, no aborts, no printing.
- *   - Inputs are finite by contract.  msa_sparse_attend skips document ids outside [0, N) like -1 pads.
+ *   - Inputs are finite by contract.  msa_sparse_attend and msa_sparse_attend4 skip document ids outside [0, N) like -1
+ *     pads.
  */
 #ifndef MSA_H_
 #define MSA_H_
@@ -364,14 +365,16 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
  *     lse[b][m][h]    = log sum_t exp( ... )        (natural log; -inf and out = 0 if no row is seen, as with q_pos < local_pos0:
  *                                                    the way to mark the padding of a batch)
  * Positions may come in any order; tokens that the caller appends later lie behind q_pos and are not read.  A row up to the
- * largest position of a sequence's tokens holds numbers, seen or not; what rows behind it hold has no effect.
+ * largest position of a sequence's tokens holds numbers, seen or not; what rows behind it hold has no effect, nor has the
+ * query of a token that sees none.  out and lse overlap no input.
  *   q         in   bf16 [B][M][Hq][d]
  *   Kloc,Vloc in   bf16 [B][Hkv][Lloc][d]
  *   window         >= 1; Lloc or more: causal attention;  sinks >= 0
  *   q_pos     in   int32 [B][M]
  *   out       out  bf16 [B][M][Hq][d]
  *   lse       out  fp32 [B][M][Hq], may be NULL
- *   workspace      >= msa_window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks); contents undefined on entry/exit
+ *   workspace      >= msa_window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), which does not fall as Lloc, window
+ *                  or sinks grow; contents undefined on entry/exit
  * Scores, their maximum and sum and the outputs are accumulated in fp32.  With few tokens the softmax weights are carried as
  * bf16 (hi, lo) pairs, with many as bf16.  Reads n_q_heads, n_kv_heads and head_dim of cfg.
  */
@@ -389,7 +392,7 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *     out, lse                     softmax over them with scale 1/sqrt(d), as in msa_sparse_attend
  * Selections, select_scope, token_pool, doc_lens, pads and documents listed twice are read as msa_sparse_attend reads them;
  * any doc_len is served; k * G <= 2^28.  cfg->bank_keys_rotated is not read.  Local rows up to the largest position of a
- * sequence's tokens hold numbers.
+ * sequence's tokens hold numbers.  out and lse overlap no input.
  *   q         in   bf16 [B][M][Hq][d]
  *   K4, K4s, V4, V4s  in  as msa_pack_kv4 writes them
  *   idx       in   int32 [B][M'][S][k]
@@ -397,7 +400,7 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *   q_pos     in   int32 [B][M]
  *   out       out  bf16 [B][M][Hq][d]
  *   lse       out  fp32 [B][M][Hq], may be NULL
- *   workspace      >= msa_sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc); where many tokens share a selection
+ *   workspace      >= msa_sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), which does not fall as k or Lloc grows; where many tokens share a selection
  *                  (token_pool = 1) it holds the selected documents in bf16, B * Hkv * k * G * d * 4 bytes
  */
 size_t msa_sparse_attend4_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t k, int32_t Lloc);

@@ -529,6 +529,14 @@ def sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc):
     return load_library().msa_sparse_attend4_workspace_bytes(ctypes.byref(cfg), B, M, k, Lloc)
 
 
+def _workspace(size, device, stream):
+    """A workspace for one call; a stream other than the current one keeps it until its work is done."""
+    t = torch.empty(max(size, 256), dtype=_U8, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
 def _workspace_at(t, dev):
     if t.dtype is not _U8 or t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"workspace: expected a contiguous tensor of torch.uint8 on cuda:{dev}")
@@ -541,14 +549,15 @@ def msa_window_attend(cfg, q, Kloc, Vloc, q_pos, window, sinks=0, local_pos0=0, 
     (out bf16 like q, lse fp32 [B][M][Hq]): attention over the last `window` tokens and the first `sinks`."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     dev = _gpu(q, "q")
+    if q.dim() != 4 or Kloc.dim() != 4:
+        raise ValueError("msa_window_attend: expected q [B][M][Hq][d] and Kloc [B][Hkv][Lloc][d]")
     B, M, Lloc = q.shape[0], q.shape[1], Kloc.shape[2]
     if out is None:
         out = torch.empty_like(q)
     if lse is None:
         lse = torch.empty((B, M, Hq), dtype=_F32, device=q.device)
     if workspace is None:
-        workspace = torch.empty(max(window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), 256), dtype=_U8,
-                                device=q.device)
+        workspace = _workspace(window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), q.device, stream)
     _call("msa_window_attend", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M,
           _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc"), Lloc,
           local_pos0, window, sinks, _at(q_pos, _I32, (B, M), dev, "q_pos"), _at(out, _BF16, (B, M, Hq, d), dev, "out"),
@@ -561,7 +570,9 @@ def msa_sparse_attend4(cfg, q, bank, idx, Kloc, Vloc, local_pos0, q_pos, out=Non
     idx int32 [B][M'][S][k] as msa_score_topk writes it for cfg -> (out bf16 like q, lse fp32 [B][M][Hq])."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     dev = _gpu(q, "q")
-    B, M, k = q.shape[0], q.shape[1], idx.shape[-1]
+    if q.dim() != 4 or idx.dim() != 4 or (Kloc is not None and Kloc.dim() != 4):
+        raise ValueError("msa_sparse_attend4: expected q [B][M][Hq][d], idx [B][M'][S][k] and Kloc [B][Hkv][Lloc][d]")
+    B, M, k = q.shape[0], q.shape[1], idx.shape[3]
     if (Kloc is None) != (Vloc is None) or any(t is None for t in bank):
         raise ValueError("msa_sparse_attend4: keys come with their values")
     Lloc, Ka, Va = 0, None, None
@@ -573,7 +584,7 @@ def msa_sparse_attend4(cfg, q, bank, idx, Kloc, Vloc, local_pos0, q_pos, out=Non
     if lse is None:
         lse = torch.empty((B, M, Hq), dtype=_F32, device=q.device)
     if workspace is None:
-        workspace = torch.empty(max(sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), 256), dtype=_U8, device=q.device)
+        workspace = _workspace(sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), q.device, stream)
     K4, K4s, V4, V4s = _kv4_at(cfg, bank, dev)
     lists = (B, 1 if cfg.token_pool else M, 1 if cfg.select_scope == MSA_SCOPE_ALL else Hkv, k)
     _call("msa_sparse_attend4", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M, K4, K4s, V4,

@@ -365,9 +365,13 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   // documents' expansion cost.  us, tiled / one by one, M tokens: 8 heads of 128 over 2048 rows, M = 4 12 / 14, 16 14 / 22;
   // 8 sequences over 4096 rows, M = 2 40 / 36, 4 40 / 63, 8 31 / 115; heads of 64 that share nothing (r = 1) over 2048 rows,
   // M = 8 14 / 11, 16 14 / 14; 16 documents of 512, M = 4 40 / 17, 16 39 / 33; 3 times 8 of 64, M = 8 20 / 16, 16 22 / 25.
+  // (More rows never lead back to the single-token kernel.)
   const long long cost = (mem_rows + 31) / 32 + kLocalCost * ((local_rows + 31) / 32), work = pairs * cost;
-  p.tiled = (mem_rows == 0 || shared) && (M >= 32 || (M >= 4 && work >= 20000 + B * dm.Hkv * mem_rows / 4)) ? 1 : 0;
+  p.tiled = (mem_rows == 0 || shared) && (M >= 32 || (M >= (mem_rows > 0 ? 8 : 4) && work >= 20000 + B * dm.Hkv * mem_rows / 4)) ? 1 : 0;
   int n_most;  // splits that the workspace holds: grows with the rows, so that one sized for the longest call serves all
+  long long most1 = (cost + 15) / 16;
+  if (most1 > 2048 / pairs) most1 = 2048 / pairs;
+  const int single_most = (int)(most1 < 1 ? 1 : (most1 > 32 ? 32 : most1));
   if (p.tiled) {
     // 128 columns to a workgroup.  With one, two or three on every CU a step takes 0.80, 0.95 or 1.32 us (d = 64: 0.48, 0.56,
     // 0.76), a workgroup 6 beside its steps; parts have to be written and joined, 4 us and 0.25 + 0.05 n for every 1000 of
@@ -402,9 +406,7 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     // n parts 3 us and 0.3 for each (8 heads, 8 streams, 512 steps of bank rows and 64 local ones: n = 2 76 us, 4 45,
     // 6 47, 8 41, 12 46, 16 50; 32 streams, 8 and 32 steps: n = 2 30 us, 4 35, 8 52, 16 97; one stream, 256 and 64: 50, 29,
     // 23, 19, 17, 15).
-    long long most = (cost + 15) / 16;
-    if (most > 2048 / pairs) most = 2048 / pairs;
-    n_most = (int)(most < 1 ? 1 : (most > 32 ? 32 : most));
+    n_most = single_most;
     long long best = -1;
     for (int n = 1; n <= n_most; ++n) {
       const long long all = pairs * n, steps = (cost + 4 * n - 1) / (4 * n);
@@ -422,17 +424,26 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     at += round_up256(bytes);
     return here;
   };
-  if (n_most > 1) {
-    take(rows * n_most * dm.d * sizeof(float));
-    p.off_ml = take(rows * n_most * sizeof(float2));
-    if (!p.tiled) p.off_tickets = take((size_t)pairs * sizeof(unsigned long long));
+  auto take_parts = [&](int n, bool counted) {  // n parts of every row, and the arrival counters
+    if (n < 2) return;
+    take(rows * n * dm.d * sizeof(float));
+    p.off_ml = take(rows * n * sizeof(float2));
+    if (counted) p.off_tickets = take((size_t)pairs * sizeof(unsigned long long));
+  };
+  size_t single = 0;
+  if (p.tiled && M < 32) {  // what a shorter call, which takes its tokens one by one, asks for
+    take_parts(single_most, true);
+    single = at;
+    at = 0;
   }
+  take_parts(n_most, !p.tiled);
   if (p.tiled && mem_rows > 0) {
     const size_t x = (size_t)B * dm.Hkv * mem_rows * dm.d * 2;
     p.off_kx = take(x);
     p.off_vx = take(x);
     p.off_mem_rows = take((size_t)B * dm.Hkv * sizeof(int));
   }
+  if (at < single) at = single;
   p.ws_bytes = at > 256 ? at : 256;
   return p;
 }

@@ -51,6 +51,12 @@ def test_refused_sizes(lib):
     pooled = _cfg(2048, 512, 32, 8, 128, token_pool=1)
     assert msa.sparse_attend4_workspace_bytes(pooled, 1, 100, 16, 100) >= 8 * 16 * 512 * 128 * 4
     assert msa.sparse_attend4_workspace_bytes(c, 1, 1, 65, 0) == 0
+    for cfg in (c, pooled, _cfg(2048, 1, 32, 8, 128, token_pool=1), _cfg(2048, 8, 8, 1, 64, token_pool=1)):
+        for B, M in ((1, 1), (3, 5), (8, 31), (1, 32), (2, 500), (40, 16), (1, 9)):
+            for k0, k1 in ((1, 64), (3, 3), (64, 64)):      # more documents, a longer local context: never less
+                sizes = [msa.sparse_attend4_workspace_bytes(cfg, B, M, k, L)
+                         for k, L in ((k0, 0), (k0, 10), (min(k0 + 1, k1), 600), (k1, 600), (k1, 4000), (k1, 50000))]
+                assert sizes == sorted(sizes), (B, M, k0)
 
 
 def _make(N, G, Hq, Hkv, d, B, M, L, seed):
@@ -190,3 +196,41 @@ def test_graph_replays(M, pool):
         o, y = msa.msa_sparse_attend4(cfg, q, bank, idx, Kl, Vl, G, q_pos)
         torch.cuda.synchronize()
         assert torch.equal(o, out) and torch.equal(y, lse), i
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M, pool", [(1, 0), (32, 1)])
+def test_offsets_past_32_bits(M, pool):
+    """A bank whose codes alone are 2.3 GB: its last documents are found."""
+    N, G, Hq, Hkv, d, k = 9000, 512, 8, 8, 128, 3
+    cfg = _cfg(N, G, Hq, Hkv, d, token_pool=pool)
+    bank = tuple(torch.zeros_like(t) for t in msa.alloc_kv4(cfg))
+    bank[1].fill_(127), bank[3].fill_(127)
+    (K, V, q, Kl, Vl), _ = _make(4, G, Hq, Hkv, d, 1, M, 8, 11)
+    small = msa.msa_pack_kv4(_cfg(4, G, Hq, Hkv, d), K.cuda(), V.cuda())
+    for t, x in zip(bank, small):
+        t[N - 4:] = x
+    idx = torch.tensor([N - 1, N - 3, N - 4], dtype=torch.int32).reshape(1, 1, 1, k).expand(1, 1, Hkv, k).contiguous()
+    q_pos = torch.full((1, M), G + 7, dtype=torch.int32)
+    out, lse = msa.msa_sparse_attend4(cfg, q.cuda(), bank, idx.cuda(), Kl.cuda(), Vl.cuda(), G, q_pos.cuda())
+    torch.cuda.synchronize()
+    kept = [P.unpack4(small[i].cpu(), small[i + 1].cpu()) for i in (0, 2)]
+    P.sparse_attend4(q.double(), *kept, idx - (N - 4), None, Kl.double(), Vl.double(), q_pos, G).check(out, lse, MANY)
+    back = msa.msa_unpack_kv4(cfg, bank, N - 1, 1)
+    assert torch.equal(back[0][N - 1].double().cpu(), kept[0][3]) and torch.equal(back[1][N - 1].double().cpu(), kept[1][3])
+
+
+@pytest.mark.gpu
+def test_python_refusals():
+    N, G, Hq, Hkv, d, k = 4, 8, 8, 2, 64, 2
+    (K, V, q, Kl, Vl), _ = _make(N, G, Hq, Hkv, d, 2, 3, 9, 0)
+    cfg = _cfg(N, G, Hq, Hkv, d)
+    bank = msa.msa_pack_kv4(cfg, K.cuda(), V.cuda())
+    pos = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    idx = torch.zeros((2, 3, Hkv, k), dtype=torch.int32, device="cuda")
+    good = dict(q=q.cuda(), bank=bank, idx=idx, Kloc=Kl.cuda(), Vloc=Vl.cuda(), local_pos0=G, q_pos=pos)
+    msa.msa_sparse_attend4(cfg, **good)
+    for bad in (dict(q=q), dict(idx=idx[:, :1]), dict(idx=idx[:, :, :1]), dict(idx=idx.long()), dict(bank=bank[::-1]),
+                dict(bank=(None,) + bank[1:]), dict(Kloc=None), dict(q_pos=pos[:1]), dict(Vloc=Kl.cuda()[:, :, 1:])):
+        with pytest.raises(ValueError):
+            msa.msa_sparse_attend4(cfg, **{**good, **bad})

@@ -1,5 +1,6 @@
 """msa_window_attend against the plain definition in 64 bits: windows, first tokens, positions in any order, empty rows."""
 import ctypes
+import itertools
 
 import pytest
 import torch
@@ -48,8 +49,10 @@ def test_workspace_sizes(lib):
     assert msa.window_attend_workspace_bytes(c, 1, 1, 0, 4, 0) == 0
     assert msa.window_attend_workspace_bytes(c, 1, 1, 8, 0, 0) == 0
     # a longer cache or window never asks for less
-    sizes = [msa.window_attend_workspace_bytes(c, 2, 1, L, W, 4) for L, W in ((100, 50), (1000, 50), (1000, 500), (9000, 8000))]
-    assert sizes == sorted(sizes)
+    for cfg, B, M in itertools.product((c, _cfg(8, 1, 64)), (1, 3, 40), (1, 2, 5, 9, 31, 32, 509)):
+        sizes = [msa.window_attend_workspace_bytes(cfg, B, M, L, W, S) for L, W, S in (
+                (1, 1, 0), (100, 50, 0), (100, 50, 40), (1000, 50, 40), (1000, 500, 40), (2500, 2000, 40), (9000, 8000, 40), (70000, 66000, 40))]
+        assert sizes == sorted(sizes), (B, M)
 
 
 def _make(B, M, Hq, Hkv, d, L, seed=0):
@@ -172,3 +175,62 @@ def test_python_refusals():
             msa.msa_window_attend(cfg, **a)
     with pytest.raises(msa.MsaError):
         msa.msa_window_attend(cfg, q, K, V, pos, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 40])
+def test_queries_of_padding_may_be_anything(M):
+    """Tokens that see nothing give zeros and -inf whatever their queries hold, and do not touch their neighbours."""
+    q, K, V = _make(2, M, 4, 2, 64, 60, 9)
+    q_pos = (60 - M + torch.arange(M)).expand(2, M).contiguous().to(torch.int32)
+    q_pos[:, ::2] = -1
+    cfg = _cfg(4, 2, 64)
+    bad = q.clone()
+    bad[:, ::2] = float("nan")
+    a = msa.msa_window_attend(cfg, q.cuda(), K.cuda(), V.cuda(), q_pos.cuda(), 30, sinks=2)
+    b = msa.msa_window_attend(cfg, bad.cuda(), K.cuda(), V.cuda(), q_pos.cuda(), 30, sinks=2)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert float(b[0][:, ::2].abs().max()) == 0.0 and bool(torch.isinf(b[1][:, ::2]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 33])
+def test_offsets_past_32_bits(M):
+    """A cache of 2.2 billion elements: the last rows of the last head are found."""
+    B, Hkv, L, d = 2, 4, 2_150_000, 128
+    cfg = _cfg(8, Hkv, d)
+    K, V = (torch.zeros((B, Hkv, L, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q, Ks, Vs = _make(B, M, 8, Hkv, d, 300, 10)
+    K[:, :, L - 300:], V[:, :, L - 300:] = Ks.cuda(), Vs.cuda()
+    q_pos = (L - M + torch.arange(M)).expand(B, M).contiguous().to(torch.int32)
+    out, lse = msa.msa_window_attend(cfg, q.cuda(), K, V, q_pos.cuda(), 200)
+    torch.cuda.synchronize()
+    P.window_attend(q.double(), Ks.double(), Vs.double(), q_pos - (L - 300), 200, 0, 0).check(out, lse, MANY)
+    del K, V
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    """Calls that run side by side with workspaces of their own, and one whose workspace comes from the binding."""
+    cfg = _cfg(8, 1, 128)
+    sets = [[t.cuda() for t in _make(1, 1, 8, 1, 128, 4000, 20 + i)] for i in range(3)]
+    pos = torch.full((1, 1), 3999, dtype=torch.int32, device="cuda")
+    want = [msa.msa_window_attend(cfg, *s, pos, 4000) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(20):
+        got = [msa.msa_window_attend(cfg, *s, pos, 4000, stream=st) for s, st in zip(sets, streams)]
+        for st in streams:
+            st.synchronize()
+        assert all(torch.equal(a, c) and torch.equal(b, d) for (a, b), (c, d) in zip(want, got))
+
+
+@pytest.mark.gpu
+def test_one_by_one_and_together_agree():
+    """The same tokens below and above the number that goes through the tiled kernel."""
+    q, K, V = _make(1, 32, 8, 2, 64, 500, 30)
+    q_pos = (468 + torch.arange(32)).reshape(1, 32).to(torch.int32)
+    a, la = _check(8, 2, 64, q, K, V, q_pos, 77, 5, 0)
+    b, lb = _check(8, 2, 64, q[:, :31].contiguous(), K, V, q_pos[:, :31].contiguous(), 77, 5, 0)
+    assert float((a[:, :31].float() - b.float()).abs().max()) <= 2.0 ** -5 and float((la[:, :31] - lb).abs().max()) <= 1e-4
