@@ -369,4 +369,15 @@ __device__ __forceinline__ uint32_t arrive_at(unsigned long long* word, unsigned
   }
 }
 
+// Puts the nonce there, with no arrivals, ahead of the arrivals: one participant calls it before its own.  Without it all of
+// them meet a leftover at about the same time, and each takes two or three turns at the word instead of one (32 participants:
+// 9 us).  It ends for the same reason: an exchange fails only because an arrival changed the word.
+__device__ __forceinline__ void expect_arrivals(unsigned long long* word, unsigned long long nonce48) {
+  unsigned long long old = load_dev(word);
+  while ((old >> 16) != nonce48)
+    if (__hip_atomic_compare_exchange_strong(word, &old, nonce48 << 16, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                             __HIP_MEMORY_SCOPE_AGENT))
+      return;
+}
+
 }  // namespace msa

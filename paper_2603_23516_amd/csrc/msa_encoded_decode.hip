@@ -101,6 +101,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   };
   const int s_begin = share(sp), s_end = share(sp + 1);
 
+  unsigned long long* const ticket = a.tickets + (long long)bm * a.Hkv + g;
+  if (a.n_splits > 1 && sp == 0 && tid == 192) expect_arrivals(ticket, a.nonce);  // (a wave that does not number the rows)
+
   // Value rows in LDS: 16-byte piece p of row i lies at place p ^ swz(i), so that neither the writes (16 rows, one piece) nor
   // the transposing reads (four rows, two pieces) meet in a bank.
   unsigned char* const vt = stage[wave];
@@ -318,7 +321,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   if (a.n_splits == 1) return;
   wait_stores_done();
   __syncthreads();
-  unsigned long long* const ticket = a.tickets + (long long)bm * a.Hkv + g;
   if (tid == 0) arrived = arrive_at(ticket, a.nonce);
   __syncthreads();
   if (arrived != (uint32_t)a.n_splits - 1) return;
@@ -404,8 +406,8 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     // Two workgroups fit a CU.  A workgroup takes about 9 us beside its steps (three loads that wait for one another, then
     // the joining of four waves), its steps 0.7 us each where it has a CU to itself and 1.2 beside another, and the join of
     // n parts 3 us and 0.3 for each (8 heads, 8 streams, 512 steps of bank rows and 64 local ones: n = 2 76 us, 4 45,
-    // 6 47, 8 41, 12 46, 16 50; 32 streams, 8 and 32 steps: n = 2 30 us, 4 35, 8 52, 16 97; one stream, 256 and 64: 50, 29,
-    // 23, 19, 17, 15).
+    // 8 41, 12 46, 16 49; 32 streams, 8 and 32 steps: n = 2 29 us, 4 35, 8 52, 16 93; one stream, 256 local steps: n = 4 34, 8
+    // 21, 12 17, 16 15.2, 24 14.4, 32 15.8).
     n_most = single_most;
     long long best = -1;
     for (int n = 1; n <= n_most; ++n) {
