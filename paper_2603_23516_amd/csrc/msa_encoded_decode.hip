@@ -376,10 +376,10 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   const int single_most = (int)(most1 < 1 ? 1 : (most1 > 32 ? 32 : most1));
   if (p.tiled) {
     // 128 columns to a workgroup.  With one, two or three on every CU a step takes 0.80, 0.95 or 1.32 us (d = 64: 0.48, 0.56,
-    // 0.76), a workgroup 6 beside its steps; parts have to be written and joined, 4 us and 0.25 + 0.05 n for every 1000 of
-    // the (token, head) rows, and n rows of d floats at 5 TB/s.  (1000 tokens over 8192 and 1000 rows, 8 heads: n = 1 239
-    // us, 2 164, 3 162, 4 171, 8 183; 128 tokens over 4096: 91, 53, 40, 33, n = 8 27, 16 30; 4 times 509 tokens of 64 dims
-    // over 1000 rows: 26, 37, 38, 40.)
+    // 0.76), a workgroup 6 beside its steps.  Two parts are joined by the last workgroup, 7 us (d = 64: 4);
+    // more by a launch, 4 us and 0.25 + 0.05 n for every 1000 of the (token, head) rows, and n rows of d floats
+    // at 5 TB/s.  (1000 tokens over 8192 and 1000 rows, 8 heads: n = 1 245 us, 2 161, 3 166, 4 171, 8 183; 128 tokens over
+    // 4096: 95, 54, 41, 35, n = 8 28, 16 29; 4 times 509 tokens of 64 dims over 1000 rows: 26, 24, 37, 39.)
     p.tpw = 32 / dm.r;
     p.n_tiles = (M + 4 * p.tpw - 1) / (4 * p.tpw);
     const long long tiles = (long long)B * p.n_tiles * dm.Hkv, heads = (long long)B * M * dm.Hq;
@@ -396,7 +396,10 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
       long long t = steps * ns_per_step[dm.d == 128][per_cu - 1];
       if (all > 768) t = t * all / 768;
       t += 6000;
-      if (n > 1) t += 4000 + heads * (250 + 50 * n) / 1000 + heads * n * dm.d * 4 / 5000;
+      if (n == 2)
+        t += dm.d == 128 ? 7000 : 4000;
+      else if (n > 2)
+        t += 4000 + heads * (250 + 50 * n) / 1000 + heads * n * dm.d * 4 / 5000;
       if (best < 0 || t < best) {
         best = t;
         p.n_splits = n;
@@ -426,19 +429,24 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     at += round_up256(bytes);
     return here;
   };
-  auto take_parts = [&](int n, bool counted) {  // n parts of every row, and the arrival counters
+  auto take_parts = [&](int n, size_t of, size_t floats, size_t sums, size_t counters) {  // n parts of `of`, and the counters
     if (n < 2) return;
-    take(rows * n * dm.d * sizeof(float));
-    p.off_ml = take(rows * n * sizeof(float2));
-    if (counted) p.off_tickets = take((size_t)pairs * sizeof(unsigned long long));
+    take(of * n * floats * sizeof(float));
+    p.off_ml = take(of * n * sums * sizeof(float2));
+    p.off_tickets = take(counters * sizeof(unsigned long long));
   };
   size_t single = 0;
   if (p.tiled && M < 32) {  // what a shorter call, which takes its tokens one by one, asks for
-    take_parts(single_most, true);
+    take_parts(single_most, rows, dm.d, 1, (size_t)pairs);
     single = at;
     at = 0;
   }
-  take_parts(n_most, !p.tiled);
+  if (p.tiled) {
+    const size_t tiles = (size_t)B * p.n_tiles * dm.Hkv;
+    take_parts(n_most, tiles, 128 * (size_t)dm.d, 256, tiles);  // (no fewer than by rows)
+  } else {
+    take_parts(n_most, rows, dm.d, 1, (size_t)pairs);
+  }
   if (p.tiled && mem_rows > 0) {
     const size_t x = (size_t)B * dm.Hkv * mem_rows * dm.d * 2;
     p.off_kx = take(x);
@@ -464,7 +472,8 @@ int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, 
   a.n_splits = pl.n_splits;
   a.part_o = (float*)w;
   a.part_ml = (float2*)(w + pl.off_ml);
-  a.tickets = (unsigned long long*)(w + pl.off_tickets);
+  if (!pl.tiled || pl.n_splits == 2) a.tickets = (unsigned long long*)(w + pl.off_tickets);
+  a.nonce = launch_nonce48();
   if (pl.tiled) {
     TiledArgs ta = {};
     ta.tpw = pl.tpw;
@@ -477,7 +486,6 @@ int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, 
     }
     return launch_encoded_tiled(dm, a, ta, B, st);
   }
-  a.nonce = launch_nonce48();
   const dim3 grid(a.n_splits, dm.Hkv, B * a.M), block(256);
   if (dm.d == 128) {
     if (a.K4 != nullptr) hipLaunchKernelGGL((encoded_decode_kernel<128, true>), grid, block, 0, st, a);

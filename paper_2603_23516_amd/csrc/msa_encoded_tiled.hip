@@ -90,10 +90,12 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
   const int sp = x % a.n_splits;
   x /= a.n_splits;
   const int b = x / ta.n_tiles, tile = ta.n_tiles - 1 - x % ta.n_tiles;
+  if (a.n_splits > 1 && a.tickets != nullptr && sp == 0 && tid == NW * 64 - 1)
+    expect_arrivals(a.tickets + (long long)(b * ta.n_tiles + tile) * a.Hkv + g, a.nonce);
 
   // this lane's column: a (token, head) pair that sees the rows t <= p with t >= lo or t < sinks
-  const int tl = col / r, head = col - tl * r, tok = (tile * NW + wave) * ta.tpw + tl;
-  const bool ok = tl < ta.tpw && tok < a.M;
+  int tl = col / r, head = col - tl * r, tok = (tile * NW + wave) * ta.tpw + tl;
+  bool ok = tl < ta.tpw && tok < a.M;
   int p = -1, pmin = INT32_MAX, pmax = -1, plow = INT32_MAX;  // plow: of the tokens that see anything
   if (ok) {
     const long long pl = (long long)a.q_pos[(long long)b * a.M + tok] - a.pos0;
@@ -161,13 +163,12 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
     vat[t] = TILE + ((vrow * ROW + (((2 * ((lane >> 4) & 1) + ((j16 & 3) >> 1)) ^ swz_v(vrow)) * 16) + 8 * (j16 & 1)) ^ (64 * t));
 
   // A wave's copies of a step: copy j (j < NI: keys, else values) brings 1 KiB to place j of the stage; its lane's 16 bytes come
-  // from row crow at byte cpiece of the row.
-  int crow[NPW], cpiece[NPW];
+  // from byte coff of the step's rows.
+  int coff[NPW];
 #pragma unroll
   for (int i = 0; i < NPW; ++i) {
-    const int j = i * NW + wave, y = (j < NI ? j : j - NI) * 64 + lane;
-    crow[i] = y / NP;
-    cpiece[i] = ((y % NP) ^ (j < NI ? swz_k(crow[i]) : swz_v(crow[i]))) * 16;
+    const int j = i * NW + wave, y = (j < NI ? j : j - NI) * 64 + lane, row = y / NP;
+    coff[i] = row * ROW + ((y % NP) ^ (j < NI ? swz_k(row) : swz_v(row))) * 16;
   }
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + wave * 1024);
 
@@ -201,9 +202,12 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
     for (int i = 0; i < NPW; ++i) {
       const uint16_t* src = n_v;
       if (i * NW + wave < NI) src = n_k;
-      int row = crow[i];
-      if (cnt < 32) row = row < cnt ? row : cnt - 1;
-      copy16_to_lds_async_at(src, row * ROW + cpiece[i], lds0 + INTO * 2 * TILE + i * NW * 1024);
+      int off = coff[i];
+      if (cnt < 32) {  // rows that do not exist: the last one that does
+        const int last = (cnt - 1) * ROW + (off & (ROW - 1));
+        off = off < last ? off : last;
+      }
+      copy16_to_lds_async_at(src, off, lds0 + INTO * 2 * TILE + i * NW * 1024);
     }
     n_t0 += 32;
     n_k += 32 * D;
@@ -282,24 +286,28 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
       for (int t = 0; t < NT; ++t) o[t] *= alpha;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
-    uint32_t pw[8];
+    // contraction slot j of slice sg and half hf is key 16 sg + (j % 4) + 8 (j / 4) + 4 hf: the lane's own registers; half of
+    // the weights at a time, so that the products of the first half run beside the exponentials of the second
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i], a.qscale, -m_use));
-      const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i + 1], a.qscale, -m_use));
-      l_run += p0 + p1;
-      pw[i] = pack_bf16(p0, p1);
-    }
-    const bf16x8_t pb[2] = {as_bf16x8(make_uint4(pw[0], pw[1], pw[2], pw[3])), as_bf16x8(make_uint4(pw[4], pw[5], pw[6], pw[7]))};
-    // contraction slot j of slice sg and half hf is key 16 sg + (j % 4) + 8 (j / 4) + 4 hf: the lane's own registers
+    for (int sg = 0; sg < 2; ++sg) {
+      uint32_t pw[4];
 #pragma unroll
-    for (int sg = 0; sg < 2; ++sg)
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * sg + 2 * i], a.qscale, -m_use));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * sg + 2 * i + 1], a.qscale, -m_use));
+        l_run += p0 + p1;
+        pw[i] = pack_bf16(p0, p1);
+      }
+      const bf16x8_t pb = as_bf16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+      // (the compiler left to itself puts all sixteen exponentials first: one workgroup on a CU 260 us for 238)
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const s16x4_t v0 = lds_read_tr16(st + vat[t] + 16 * sg * ROW), v1 = lds_read_tr16(st + vat[t] + (16 * sg + 8) * ROW);
         const bf16x8_t av = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[t] = mfma32e(av, pb[sg], o[t]);
+        o[t] = mfma32e(av, pb, o[t]);
       }
+    }
   };
   if (sb < se) issue(std::integral_constant<int, 0>());
   if (sb + 1 < se) issue(std::integral_constant<int, 1>());
@@ -311,20 +319,70 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
 
   const uint32_t u = __float_as_uint(l_run);
   const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+
+  // ---- the splits' results ----------------------------------------------------------------------------------------
+  // Two of them: a part is stored as the registers hold it, each store 512 bytes in a row, past the caches, and the workgroup
+  // that arrives last adds the other's to its own.  More are stored by (token, head) row for a launch that joins them: here one
+  // part after another comes past the caches at 3 us each (128 tokens over 4096 rows in 8 parts 35 us, by a launch 27; 1000
+  // tokens over 9192 in 2 parts 161, by a launch 168; 4096 tokens of 64 dims in 2 parts 55, 76).
+  if (a.n_splits > 1 && a.tickets != nullptr) {
+    constexpr int PAIRS = NT * 8;  // pairs of floats of a thread
+    const long long part0 = ((long long)(b * ta.n_tiles + tile) * a.Hkv + g) * a.n_splits;
+    unsigned long long* const po = reinterpret_cast<unsigned long long*>(a.part_o) + part0 * (PAIRS * 256);
+    unsigned long long* const pm = reinterpret_cast<unsigned long long*>(a.part_ml) + part0 * 256;
+    {
+      unsigned long long* const mine = po + (long long)sp * (PAIRS * 256);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          store_dev(&mine[(8 * t + i) * 256 + tid],
+                    ((unsigned long long)__float_as_uint(o[t][2 * i + 1]) << 32) | __float_as_uint(o[t][2 * i]));
+      store_dev(&pm[sp * 256 + tid], ((unsigned long long)__float_as_uint(l) << 32) | __float_as_uint(m_run));
+    }
+    wait_stores_done();
+    __syncthreads();
+    unsigned long long* const ticket = a.tickets + (long long)(b * ta.n_tiles + tile) * a.Hkv + g;
+    if (tid == 0) pmin_s[0] = (int)arrive_at(ticket, a.nonce);
+    __syncthreads();
+    if (pmin_s[0] != a.n_splits - 1) return;
+    if (tid == 0) store_dev(ticket, 0ull);
+    {
+      // Products and sums rounded one by one: the result does not depend on which of the two was the last.
+#pragma clang fp contract(off)
+      const int other = 1 - sp;
+      const unsigned long long ml = load_dev(&pm[other * 256 + tid]);
+      const float mi = __uint_as_float((uint32_t)ml), m = fmaxf(m_run, mi);
+      const float f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m);
+      const float fi = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m);
+      m_run = m;
+      l = l * f + __uint_as_float((uint32_t)(ml >> 32)) * fi;
+      const unsigned long long* const theirs = po + (long long)other * (PAIRS * 256);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        unsigned long long v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = load_dev(&theirs[(8 * t + i) * 256 + tid]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          o[t][2 * i] = o[t][2 * i] * f + __uint_as_float((uint32_t)v[i]) * fi;
+          o[t][2 * i + 1] = o[t][2 * i + 1] * f + __uint_as_float((uint32_t)(v[i] >> 32)) * fi;
+        }
+      }
+    }
+  }
+  {  // which column this is, again: kept through the loop it would be registers that the loop does not have
+    int c = col;
+    asm volatile("" : "+v"(c));
+    tl = c / r;
+    head = c - tl * r;
+    tok = (tile * NW + wave) * ta.tpw + tl;
+    ok = tl < ta.tpw && tok < a.M;
+  }
   if (!ok) return;
   const long long qh = ((long long)b * a.M + tok) * a.Hq + g * r + head;
-  if (a.n_splits == 1) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<uint2*>(a.out + qh * D + 32 * t + 8 * i + 4 * hf) =
-            make_uint2(pack_bf16(o[t][4 * i] * inv, o[t][4 * i + 1] * inv),
-                       pack_bf16(o[t][4 * i + 2] * inv, o[t][4 * i + 3] * inv));
-    if (hf == 0 && a.lse != nullptr) a.lse[qh] = l > 0.f ? (m_run + log2f(l)) * 0.6931471805599453f : -INFINITY;
-  } else {
+  if (a.n_splits > 1 && a.tickets == nullptr) {
     const long long ph = qh * a.n_splits + sp;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -333,7 +391,17 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
         *reinterpret_cast<f32x4_t*>(a.part_o + ph * D + 32 * t + 8 * i + 4 * hf) =
             (f32x4_t){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
     if (hf == 0) a.part_ml[ph] = make_float2(m_run, l);
+    return;
   }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<uint2*>(a.out + qh * D + 32 * t + 8 * i + 4 * hf) =
+          make_uint2(pack_bf16(o[t][4 * i] * inv, o[t][4 * i + 1] * inv),
+                     pack_bf16(o[t][4 * i + 2] * inv, o[t][4 * i + 3] * inv));
+  if (hf == 0 && a.lse != nullptr) a.lse[qh] = l > 0.f ? (m_run + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 int launch_encoded_tiled(const Dims& dm, const EncodedArgs& a, TiledArgs ta, int B, hipStream_t st) {
@@ -351,7 +419,7 @@ int launch_encoded_tiled(const Dims& dm, const EncodedArgs& a, TiledArgs ta, int
   else
     hipLaunchKernelGGL(encoded_tiled_kernel<64>, grid, dim3(kTiledWaves * 64), 0, st, a, ta);
   if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
-  if (a.n_splits > 1)
+  if (a.n_splits > 1 && a.tickets == nullptr)
     return launch_merge2(dm.d, a.part_o, a.part_ml, a.n_splits, a.part_o, a.part_ml, 0, a.out, a.lse, 0,
                          (long long)B * a.M * dm.Hq, st);
   return MSA_OK;

@@ -136,14 +136,15 @@ def test_tokens_do_not_depend_on_their_neighbours():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M, L", [(1, 2000), (12, 700)])
-def test_graph_replays_and_streams(M, L):
-    """A captured call, replayed on new inputs with other work between, on a stream of its own, with split rows (tickets)."""
-    cfg = _cfg(8, 1, 128)
-    q, K, V = (t.cuda() for t in _make(1, M, 8, 1, 128, L, 7))
+@pytest.mark.parametrize("M, L, Hq, Hkv", [(1, 2000, 8, 1), (12, 700, 8, 1), (40, 3000, 8, 1), (256, 2100, 64, 8)])
+def test_graph_replays_and_streams(M, L, Hq, Hkv):
+    """A captured call, replayed on new inputs with other work between, on a stream of its own, with split rows: one token,
+    tokens one by one, tiles whose many parts a launch joins, tiles whose few parts the last workgroup joins."""
+    cfg = _cfg(Hq, Hkv, 128)
+    q, K, V = (t.cuda() for t in _make(1, M, Hq, Hkv, 128, L, 7))
     q_pos = (L - M + torch.arange(M)).reshape(1, M).to(torch.int32).cuda()
     ws = torch.full((msa.window_attend_workspace_bytes(cfg, 1, M, L, L, 0),), 0xFF, dtype=torch.uint8, device="cuda")
-    out, lse = torch.empty_like(q), torch.empty((1, M, 8), dtype=torch.float32, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((1, M, Hq), dtype=torch.float32, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     graph = torch.cuda.CUDAGraph()
@@ -234,3 +235,34 @@ def test_one_by_one_and_together_agree():
     a, la = _check(8, 2, 64, q, K, V, q_pos, 77, 5, 0)
     b, lb = _check(8, 2, 64, q[:, :31].contiguous(), K, V, q_pos[:, :31].contiguous(), 77, 5, 0)
     assert float((a[:, :31].float() - b.float()).abs().max()) <= 2.0 ** -5 and float((la[:, :31] - lb).abs().max()) <= 1e-4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B, M, Hq, Hkv, d, L, W, S", [
+    (1, 256, 64, 8, 128, 2100, 2100, 0),       # two parts to a tile
+    (4, 509, 16, 8, 64, 1500, 1000, 16),       # two, of 64 dims
+    (1, 40, 8, 1, 128, 3000, 2500, 3),         # many, joined by a launch
+    (1, 700, 24, 8, 64, 900, 900, 0),          # none: r = 3
+])
+def test_many_tokens_at_random_places(B, M, Hq, Hkv, d, L, W, S):
+    """Chunks of prompts large enough for every way of sharing their rows out; tokens at random places in 64 bits."""
+    q, K, V = _make(B, M, Hq, Hkv, d, L, M)
+    last = torch.tensor([[L - 1 - 97 * b] for b in range(B)])
+    q_pos = (last - M + 1 + torch.arange(M)).to(torch.int32)
+    args = (_cfg(Hq, Hkv, d), q.cuda(), K.cuda(), V.cuda(), q_pos.cuda(), W)
+    out, lse = msa.msa_window_attend(*args, sinks=S)
+    for _ in range(3):        # whichever workgroup is the last to join the parts: the same bits
+        again = msa.msa_window_attend(*args, sinks=S)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    g = torch.Generator().manual_seed(1)
+    n = 60
+    at = torch.stack([torch.randint(0, B, (n,), generator=g), torch.randint(0, M, (n,), generator=g)], 1).tolist() + [[0, 0], [B - 1, M - 1]]
+    ref = P.Attended((len(at), Hq), d)
+    t = torch.arange(L)
+    for i, (b, m) in enumerate(at):
+        p = int(q_pos[b, m])
+        seen = (t <= p) & ((p - t < W) | (t < S))
+        for h in range(Hq):
+            ref.put((i, h), P.attend(q[b, m, h].double(), K[b, h * Hkv // Hq].double(), V[b, h * Hkv // Hq].double(), seen))
+    pick = tuple(torch.tensor(at).T)
+    ref.check(out.cpu()[pick], lse.cpu()[pick], MANY)
