@@ -7,8 +7,10 @@
 // to nearest, ties to even), the same on every machine.  e stays in 2 .. 252, where every value is a normal bf16 number;
 // beyond 2^125 * 6 values saturate.
 //
-// Both are streams: 2 bytes read and 0.53 written per element, or the other way round.  A lane takes eight elements (one 16-byte
-// access in bf16, 4 bytes of codes); the block's maximum comes from the quad of lanes that share it.
+// Both are streams: 2 bytes read and 0.53 written per element, or the other way round; bound by HBM (2 million rows of 128 dims, K and
+// V, 1.36 GB: packed in 220 us, 6.2 TB/s, unpacked in 257, 5.3 TB/s).  Rows that are unpacked are stored with the streaming hint
+// (262144 rows packed and unpacked 56.8 -> 52.5 us, 64064 rows 18.1 -> 16.4).  A lane takes eight elements (one 16-byte access in
+// bf16, 4 bytes of codes); the block's maximum comes from the quad of lanes that share it.
 #include "msa_attend.h"
 
 namespace msa {
@@ -27,7 +29,7 @@ __device__ __forceinline__ int scale_byte(uint32_t amax_bits) {
 }
 
 // Eight elements of a row of a block -> their codes; the quad's first lane writes the block's scale byte.
-template <int D>
+template <int D, bool STREAM>
 __device__ __forceinline__ void pack4_eight(const float (&f)[8], uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                             long long row, int lr) {
   uint32_t amax = 0;
@@ -43,13 +45,19 @@ __device__ __forceinline__ void pack4_eight(const float (&f)[8], uint8_t* __rest
   c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[2], f[3], s, 1);
   c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[4], f[5], s, 2);
   c4 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c4, f[6], f[7], s, 3);
-  *reinterpret_cast<uint32_t*>(codes + row * (D / 2) + 4 * lr) = c4;
+  uint32_t* const to = reinterpret_cast<uint32_t*>(codes + row * (D / 2) + 4 * lr);
+  if (STREAM)
+    __builtin_nontemporal_store(c4, to);
+  else
+    *to = c4;
   if ((lr & 3) == 0) scales[row * (D / 32) + lr / 4] = (uint8_t)e;
 }
 
-// ROT: keys that are not position-encoded yet are turned by their position in the document before they are rounded.
-// A thread has ROWS rows in flight.
-template <int D, bool ROT, int ROWS, bool STREAM>
+// ROT: keys that are not position-encoded yet are turned by their position in the document before they are rounded.  The angles
+// cost more than the bytes (each element its own: 2 million rows of keys and values 380 us, of one position in four documents or
+// heads 237, nothing turned 220).
+// A thread has ROWS rows in flight.  STREAM: 1 streaming loads, 2 streaming stores of the codes as well.
+template <int D, bool ROT, int ROWS, int STREAM>
 __device__ __forceinline__ void pack4_rows(const uint16_t* __restrict__ X, uint8_t* __restrict__ codes,
                                            uint8_t* __restrict__ scales, const int32_t* __restrict__ lens, int doc_begin,
                                            long long n_rows, int Hkv, int G, const NormTheta& th) {
@@ -57,51 +65,60 @@ __device__ __forceinline__ void pack4_rows(const uint16_t* __restrict__ X, uint8
   constexpr int RPB = 256 / LPR;      // rows per workgroup and turn
   const int lr = threadIdx.x % LPR;
   const long long row0 = (long long)doc_begin * Hkv * G;
-  for (long long r0 = (long long)blockIdx.x * (RPB * ROWS) + threadIdx.x / LPR; r0 < n_rows;
-       r0 += (long long)gridDim.x * (RPB * ROWS)) {
+  const long long turns = ROT ? (n_rows / G + ROWS - 1) / ROWS * G : (n_rows + ROWS - 1) / ROWS;
+  for (long long i = (long long)blockIdx.x * RPB + threadIdx.x / LPR; i < (turns + RPB - 1) / RPB * RPB;
+       i += (long long)gridDim.x * RPB) {
+    // rows of this turn: RPB apart, or, to be turned, of one position in ROWS (document, head) pairs
+    const long long r0 = ROT ? i / G * ROWS * G + i % G : i / RPB * (RPB * ROWS) + i % RPB;
+    const long long apart = ROT ? G : RPB;
     uint4 x[ROWS];
-    int t[ROWS];
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
-      const long long r = r0 + u * RPB, row = row0 + r;
+      const long long r = r0 + u * apart, row = row0 + r;
       bool live = r < n_rows;
-      t[u] = 0;
-      if (live && (ROT || lens != nullptr)) {
+      if (live && lens != nullptr) {
         const long long slab = row / G;
-        t[u] = (int)(row - slab * G);
-        if (lens != nullptr) {
-          int len = lens[slab / Hkv];
-          len = len < 1 ? 1 : (len > G ? G : len);
-          live = t[u] < len;
-        }
+        int len = lens[slab / Hkv];
+        len = len < 1 ? 1 : (len > G ? G : len);
+        live = row - slab * G < len;
       }
       x[u] = make_uint4(0, 0, 0, 0);
       if (live) x[u] = STREAM ? load_stream16(X + row * D + 8 * lr) : *reinterpret_cast<const uint4*>(X + row * D + 8 * lr);
     }
+    float2 c[ROT ? 8 : 1];
+    const bool second = lr >= LPR / 2;
+    if (ROT) {  // a lane works out four of its eight angles, the one that holds the partners the others
+      const int p = (int)(i % G), u0 = 8 * (lr & (LPR / 2 - 1));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 m = cis_pos(p, th.th[u0 + j + (second ? 4 : 0)]);
+        const float2 o = make_float2(__shfl_xor(m.x, LPR / 2, 64), __shfl_xor(m.y, LPR / 2, 64));
+        c[j] = second ? o : m;
+        c[j + 4] = second ? m : o;
+      }
+    }
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
-      const long long r = r0 + u * RPB;
+      const long long r = r0 + u * apart;
       if (r >= n_rows) break;  // the same for the lanes of a row
       const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
       float f[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
       if (ROT) {
-        const bool second = lr >= LPR / 2;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float o = __shfl_xor(f[j], LPR / 2, 64);
-          const float2 c = cis_pos(t[u], th.th[8 * (lr & (LPR / 2 - 1)) + j]);
-          f[j] = f[j] * c.x + (second ? o : -o) * c.y;
+          f[j] = fmaf(f[j], c[j].x, (second ? o : -o) * c[j].y);  // (spelt out: the same bits from every variant)
         }
       }
-      pack4_eight<D>(f, codes, scales, row0 + r, lr);
+      pack4_eight<D, (STREAM > 1)>(f, codes, scales, row0 + r, lr);
     }
   }
 }
 
 // Keys by the first row of workgroups, values by the second; either may be absent.
-template <int D, bool ROT, int ROWS, bool STREAM>
+template <int D, bool ROT, int ROWS, int STREAM>
 __global__ __launch_bounds__(256) void pack4_kernel(Pack4Args a, NormTheta th) {
   const bool values = a.x[0] == nullptr || blockIdx.y == 1;
   if (!values)
@@ -124,11 +141,11 @@ __global__ __launch_bounds__(256) void unpack4_kernel(Pack4Args a) {
     const long long row = row0 + r;
     const uint32_t c4 = *reinterpret_cast<const uint32_t*>(codes + row * (D / 2) + 4 * lr);
     const float s = __uint_as_float((uint32_t)scales[row * (D / 32) + lr / 4] << 23);
-    *reinterpret_cast<uint4*>(X + row * D + 8 * lr) = fp4x8_to_bf16(c4, s);
+    store_stream16(X + row * D + 8 * lr, fp4x8_to_bf16(c4, s));
   }
 }
 
-constexpr long long kStreamBytes = 128ll << 20;
+constexpr long long kStreamBytes = 128ll << 20, kStreamCodesBytes = 1ll << 30;
 
 static unsigned stream_blocks(long long n_rows, int rows_per_block) {
   const long long n = (n_rows + rows_per_block - 1) / rows_per_block;
@@ -155,21 +172,30 @@ int launch_pack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, bool
   }
   // From 131072 rows of a tensor on four rows to a thread, which gives fewer waves with more in flight each (262144 rows of 128
   // dims, packed and unpacked, 58 -> 53 us; 64064 rows 17.4 -> 19.0), from 128 MiB on streaming loads (2 million rows 540 ->
-  // 504 with both).
+  // 504 with both), and streaming stores where the caches do not hold the codes for the next reader either, 1 GiB of rows on
+  // (2 million rows 496 -> 479; 262144 rows 52.6 -> 60.7).  Keys to be turned have four rows to a thread at any size, which share
+  // their angles (one row to a thread, 64064 rows of keys and values 15.4 us for 13.4).
   const int n_tensors = a.x[0] != nullptr && a.x[1] != nullptr ? 2 : 1;
-  const bool many = a.n_rows >= 131072, stream = many && a.n_rows * dm.d * 2 * n_tensors >= kStreamBytes;
+  const bool many = rotate || a.n_rows >= 131072;
+  const long long bytes = a.n_rows * dm.d * 2 * n_tensors;
   const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8) * (many ? 4 : 1)), n_tensors);
-#define MSA_PACK4(DD, RR)                                                                                \
-  do {                                                                                                   \
-    if (stream) hipLaunchKernelGGL((pack4_kernel<DD, RR, 4, true>), grid, dim3(256), 0, st, a, th);      \
-    else if (many) hipLaunchKernelGGL((pack4_kernel<DD, RR, 4, false>), grid, dim3(256), 0, st, a, th);  \
-    else hipLaunchKernelGGL((pack4_kernel<DD, RR, 1, false>), grid, dim3(256), 0, st, a, th);            \
+#define MSA_PACK4(DD, RR, ROWS, SS) hipLaunchKernelGGL((pack4_kernel<DD, RR, ROWS, SS>), grid, dim3(256), 0, st, a, th)
+#define MSA_PACK4_MANY(DD, RR)                                 \
+  do {                                                         \
+    if (bytes < kStreamBytes) MSA_PACK4(DD, RR, 4, 0);           \
+    else if (bytes < kStreamCodesBytes) MSA_PACK4(DD, RR, 4, 1); \
+    else MSA_PACK4(DD, RR, 4, 2);                              \
   } while (0)
   if (dm.d == 128) {
-    if (rotate) MSA_PACK4(128, true); else MSA_PACK4(128, false);
+    if (rotate) MSA_PACK4_MANY(128, true);
+    else if (many) MSA_PACK4_MANY(128, false);
+    else MSA_PACK4(128, false, 1, 0);
   } else {
-    if (rotate) MSA_PACK4(64, true); else MSA_PACK4(64, false);
+    if (rotate) MSA_PACK4_MANY(64, true);
+    else if (many) MSA_PACK4_MANY(64, false);
+    else MSA_PACK4(64, false, 1, 0);
   }
+#undef MSA_PACK4_MANY
 #undef MSA_PACK4
   return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
 }

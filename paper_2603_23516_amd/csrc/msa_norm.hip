@@ -2,8 +2,10 @@
 //     y = x * rsqrt(mean_u x_u^2 + eps) * w          per head, in fp32
 //     (y_u, y_{u + d/2}) turned by p * base^(-2u/d)    p the token's position
 // rounded to bf16 once, queries to a dense tensor, keys and values into the rows of the local cache that msa_sparse_attend,
-// msa_window_attend and msa_sparse_attend4 read.  Every element is read once and written once: bound by HBM for a prompt, by
-// the latency of a load, the angles and a store for a few tokens.
+// msa_window_attend and msa_sparse_attend4 read.  Every element is read once and written once: bound by HBM for a prompt
+// (16384 tokens of 48 heads of 128, 403 MB in and out: 75 us, 5.4 TB/s), by the latency of a load, the angles and a store
+// for a few tokens (8: 4.2 us).  Stores carry the streaming hint at every size: kept in the L2 they displace what is still to
+// be read (16384 tokens 85.5 us for 74.7, 4096 25.5 for 17.8).
 //
 // A row of d elements is held by d/16 lanes, eight elements at u0 = 8 l and their partners at u0 + d/2, so that a rotation
 // needs no other lane and both loads are 16 bytes; a wave takes 64 / (d/16) heads of one token at a time.  A lane's eight
@@ -55,8 +57,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormArgs a, NormTheta 
     const uint4 x1 = STREAM ? load_stream16(src) : *reinterpret_cast<const uint4*>(src);
     const uint4 x2 = STREAM ? load_stream16(src + HALF) : *reinterpret_cast<const uint4*>(src + HALF);
     if (kind == 2) {
-      *reinterpret_cast<uint4*>(dst) = x1;
-      *reinterpret_cast<uint4*>(dst + HALF) = x2;
+      store_stream16(dst, x1);
+      store_stream16(dst + HALF, x2);
       continue;
     }
     const uint32_t w1[4] = {x1.x, x1.y, x1.z, x1.w}, w2[4] = {x2.x, x2.y, x2.z, x2.w};
@@ -91,8 +93,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormArgs a, NormTheta 
       y1[j] = pack_bf16(p0 * c0.x - q0 * c0.y, p1 * c1.x - q1 * c1.y);
       y2[j] = pack_bf16(q0 * c0.x + p0 * c0.y, q1 * c1.x + p1 * c1.y);
     }
-    *reinterpret_cast<uint4*>(dst) = make_uint4(y1[0], y1[1], y1[2], y1[3]);
-    *reinterpret_cast<uint4*>(dst + HALF) = make_uint4(y2[0], y2[1], y2[2], y2[3]);
+    store_stream16(dst, make_uint4(y1[0], y1[1], y1[2], y1[3]));
+    store_stream16(dst + HALF, make_uint4(y2[0], y2[1], y2[2], y2[3]));
   }
 }
 
@@ -109,8 +111,9 @@ int launch_norm_rotate(const Dims& dm, NormArgs a, hipStream_t st) {
   const RopeTheta& table = rope_table(dm.base, dm.d);
   for (int u = 0; u < kMaxHalf; ++u) th.th[u] = table.th[u];
   const long long blocks = (a.BM * a.shares + 3) / 4;
-  // Projections that the caches do not hold: streaming loads (16384 tokens of 48 heads of 128, 201 MB: 85 -> 66 us, 6.1 TB/s
-  // in and out; 12288 54.4 -> 52.5; 8192, 101 MB: 32.4 -> 36).
+  // Projections that the caches do not hold: streaming loads.  us for 48 heads of 128, with plain loads / streaming ones, inputs
+  // changing from call to call and, in brackets, right behind the product that wrote the projection: 16384 tokens (201 MB) 81.7 / 74.7
+  // [85.6 / 70.0], 12288 63.4 / 57.5 [65.7 / 54.5], 8192 (101 MB) 43.9 / 39.6 [34.4 / 34.6], 4096 17.8 / 22.0 [19.7 / 20.0].
   const int heads = (a.q != nullptr ? dm.Hq : 0) + (a.k != nullptr ? dm.Hkv : 0) + (a.v != nullptr ? dm.Hkv : 0);
   const bool stream = a.BM * heads * dm.d * 2 >= (128ll << 20);
 #define MSA_NORM(DD, SS) hipLaunchKernelGGL((norm_rotate_kernel<DD, SS>), dim3((unsigned)blocks), dim3(256), 0, st, a, th)

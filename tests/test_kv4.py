@@ -152,3 +152,16 @@ def test_many_rows_are_packed_as_few(N, G, d, lens):
         alone = msa.msa_pack_kv4(one, K[i:i + 1], V[i:i + 1])
         assert all(torch.equal(a[i:i + 1], b) for a, b in zip(bank, alone)), i
         assert all(torch.equal(a[i:i + 1], b) for a, b in zip(back, msa.msa_unpack_kv4(one, alone))), i
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N, Hkv, G, d", [(70, 3, 700, 64), (131, 1, 1001, 128), (2, 1, 66000, 64), (23000, 3, 2, 128), (140001, 1, 1, 64)])
+def test_many_turned_keys_are_packed_as_few(N, Hkv, G, d):
+    """The angles of a position are shared by several documents and heads: each has the bits it gets alone, the last ones too."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    K = torch.randn((N, Hkv, G, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    n = torch.randint(1, G + 1, (N,), generator=g, device="cuda", dtype=torch.int32)
+    K4, K4s, _, _ = msa.msa_pack_kv4(_cfg(N, G, Hkv, d, rotated=0, lens=n), K, None)
+    for i in (0, 1, N // 2, N - 2, N - 1):
+        a4, a4s, _, _ = msa.msa_pack_kv4(_cfg(1, G, Hkv, d, rotated=0, lens=n[i:i + 1].contiguous()), K[i:i + 1], None)
+        assert torch.equal(K4[i:i + 1], a4) and torch.equal(K4s[i:i + 1], a4s), i
