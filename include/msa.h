@@ -321,7 +321,7 @@ int msa_layers_step(const msa_config_t* cfg, const msa_config_t* attend_cfg, con
  * Lloc = G) Kloc, Vloc are a bank.  A token of negative position is padding: nothing of it is written.  A position
  * outside [local_pos0, local_pos0 + Lloc) has no row in the cache: its query alone is written.  Rows that no token of the
  * call is at keep what they held.  Tokens of one sequence have positions of their own; of a row that two of them claim the
- * contents are undefined (that row's alone).  Reads n_q_heads, n_kv_heads, head_dim and rope_base of cfg.
+ * contents are undefined (that row's alone).  B * M <= 2^25.  Reads n_q_heads, n_kv_heads, head_dim and rope_base of cfg.
  *   q, k, v   in   bf16, heads and dims dense ([Hq][d], [Hkv][d]), token (b, m) at (b*M + m) * stride elements: a fused
  *                  projection is read where it lies.  Strides are multiples of 8, at least the heads' elements.
  *                  q may be NULL with q_out (no queries), k with Kloc, v with Vloc; not all three
@@ -375,6 +375,8 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
  *   lse       out  fp32 [B][M][Hq], may be NULL
  *   workspace      >= msa_window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), which does not fall as Lloc, window
  *                  or sinks grow; contents undefined on entry/exit
+ * B <= 65535; B * M <= 65535 for M < 32, from there on as many tokens as make 2^24 tiles of 128 (token, head) pairs of a KV
+ * head; Lloc <= 2^28.
  * Scores, their maximum and sum and the outputs are accumulated in fp32.  With few tokens the softmax weights are carried as
  * bf16 (hi, lo) pairs, with many as bf16.  Reads n_q_heads, n_kv_heads and head_dim of cfg.
  */
@@ -391,7 +393,8 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *                                  [0, N), and every local row t < Lloc with local_pos0 + t <= q_pos[b][m]
  *     out, lse                     softmax over them with scale 1/sqrt(d), as in msa_sparse_attend
  * Selections, select_scope, token_pool, doc_lens, pads and documents listed twice are read as msa_sparse_attend reads them;
- * any doc_len is served; k * G <= 2^28.  cfg->bank_keys_rotated is not read.  Local rows up to the largest position of a
+ * any doc_len is served; k * G <= 2^28, Lloc <= 2^28, and as many tokens as msa_window_attend takes where token_pool = 1, else
+ * B * M <= 65535.  cfg->bank_keys_rotated is not read.  Local rows up to the largest position of a
  * sequence's tokens hold numbers.  out and lse overlap no input.
  *   q         in   bf16 [B][M][Hq][d]
  *   K4, K4s, V4, V4s  in  as msa_pack_kv4 writes them

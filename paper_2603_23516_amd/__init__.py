@@ -394,9 +394,18 @@ def _gpu(t, name):
     return dev
 
 
+def _i32(x, name):
+    """x, where an int32_t holds it (ctypes would cut it off)."""
+    if -2 ** 31 <= x < 2 ** 31:
+        return x
+    raise ValueError(f"{name}: {x} does not fit 32 bits")
+
+
 def _call(name, dev, stream, cfg, *args):
     """The entry point `name` on `stream` (None: the tensors' device's current one), with that device as the current one."""
     fn = getattr(_lib or load_library(), name)
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"{name}: a stream of cuda:{stream.device_index} for tensors on cuda:{dev}")
     raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
     if dev == torch.cuda.current_device():
         rc = fn(cfg, *args, raw)
@@ -451,7 +460,7 @@ def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None,
     _call("msa_norm_rotate", dev, stream, ctypes.byref(cfg), qa, qs, ka, ks, va, vs,
           None if q_weight is None else _at(q_weight, _BF16, (d,), dev, "q_weight"),
           None if k_weight is None else _at(k_weight, _BF16, (d,), dev, "k_weight"), eps, 1 if rotate else 0,
-          _at(pos, _I32, (B, M), dev, "pos"), B, M, qo, Ka, Va, Lloc, local_pos0)
+          _at(pos, _I32, (B, M), dev, "pos"), B, M, qo, Ka, Va, Lloc, _i32(local_pos0, "local_pos0"))
     return q_out
 
 
@@ -463,6 +472,8 @@ def alloc_kv4(cfg, device="cuda"):
 
 def _kv4_at(cfg, bank, dev):
     N, Hkv, G, d = cfg.n_docs, cfg.n_kv_heads, cfg.doc_len, cfg.head_dim
+    if cfg.doc_lens_tensor is not None and cfg.doc_lens_tensor.get_device() != dev:
+        raise ValueError(f"doc_lens: on {cfg.doc_lens_tensor.device}, the bank on cuda:{dev}")
     codes, scales = (N, Hkv, G, d // 2), (N, Hkv, G, d // 32)
     return [None if t is None else _at(t, _U8, s, dev, n)
             for t, s, n in zip(bank, (codes, scales, codes, scales), ("K4", "K4s", "V4", "V4s"))]
@@ -490,7 +501,8 @@ def msa_pack_kv4(cfg, K, V, doc_begin=0, doc_count=None, bank=None, stream=None)
         V4 = V4s = None
     else:
         Va = _at(V, _BF16, shape, dev, "V")
-    _call("msa_pack_kv4", dev, stream, ctypes.byref(cfg), Ka, Va, doc_begin, doc_count, K4, K4s, V4, V4s)
+    _call("msa_pack_kv4", dev, stream, ctypes.byref(cfg), Ka, Va, _i32(doc_begin, "doc_begin"),
+          _i32(doc_count, "doc_count"), K4, K4s, V4, V4s)
     return bank
 
 
@@ -517,24 +529,31 @@ def msa_unpack_kv4(cfg, bank, doc_begin=0, doc_count=None, K=None, V=None, strea
     else:
         V = torch.empty(shape, dtype=_BF16, device=src.device) if V is None else V
         Va = _at(V, _BF16, shape, dev, "V")
-    _call("msa_unpack_kv4", dev, stream, ctypes.byref(cfg), *at, doc_begin, doc_count, Ka, Va)
+    _call("msa_unpack_kv4", dev, stream, ctypes.byref(cfg), *at, _i32(doc_begin, "doc_begin"), _i32(doc_count, "doc_count"),
+          Ka, Va)
     return K, V
 
 
+_MOST = 2 ** 31 - 1  # as many rows as there can be: a longer window, or more first tokens, see the same
+
+
 def window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks=0):
-    return load_library().msa_window_attend_workspace_bytes(ctypes.byref(cfg), B, M, Lloc, window, sinks)
+    return load_library().msa_window_attend_workspace_bytes(ctypes.byref(cfg), _i32(B, "B"), _i32(M, "M"), _i32(Lloc, "Lloc"),
+                                                            _i32(min(window, _MOST), "window"),
+                                                            _i32(min(sinks, _MOST), "sinks"))
 
 
 def sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc):
-    return load_library().msa_sparse_attend4_workspace_bytes(ctypes.byref(cfg), B, M, k, Lloc)
+    return load_library().msa_sparse_attend4_workspace_bytes(ctypes.byref(cfg), _i32(B, "B"), _i32(M, "M"), _i32(k, "k"),
+                                                             _i32(Lloc, "Lloc"))
 
 
 def _workspace(size, device, stream):
-    """A workspace for one call; a stream other than the current one keeps it until its work is done."""
-    t = torch.empty(max(size, 256), dtype=_U8, device=device)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+    """A workspace for one call, of the memory of the stream that it is used on."""
+    if stream is None:
+        return torch.empty(max(size, 256), dtype=_U8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(max(size, 256), dtype=_U8, device=device)
 
 
 def _workspace_at(t, dev):
@@ -549,6 +568,7 @@ def msa_window_attend(cfg, q, Kloc, Vloc, q_pos, window, sinks=0, local_pos0=0, 
     (out bf16 like q, lse fp32 [B][M][Hq]): attention over the last `window` tokens and the first `sinks`."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     dev = _gpu(q, "q")
+    window, sinks = _i32(min(window, _MOST), "window"), _i32(min(sinks, _MOST), "sinks")
     if q.dim() != 4 or Kloc.dim() != 4:
         raise ValueError("msa_window_attend: expected q [B][M][Hq][d] and Kloc [B][Hkv][Lloc][d]")
     B, M, Lloc = q.shape[0], q.shape[1], Kloc.shape[2]
@@ -560,7 +580,8 @@ def msa_window_attend(cfg, q, Kloc, Vloc, q_pos, window, sinks=0, local_pos0=0, 
         workspace = _workspace(window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), q.device, stream)
     _call("msa_window_attend", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M,
           _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc"), Lloc,
-          local_pos0, window, sinks, _at(q_pos, _I32, (B, M), dev, "q_pos"), _at(out, _BF16, (B, M, Hq, d), dev, "out"),
+          _i32(local_pos0, "local_pos0"), window, sinks, _at(q_pos, _I32, (B, M), dev, "q_pos"),
+          _at(out, _BF16, (B, M, Hq, d), dev, "out"),
           _at(lse, _F32, (B, M, Hq), dev, "lse"), _workspace_at(workspace, dev), workspace.numel())
     return out, lse
 
@@ -588,7 +609,7 @@ def msa_sparse_attend4(cfg, q, bank, idx, Kloc, Vloc, local_pos0, q_pos, out=Non
     K4, K4s, V4, V4s = _kv4_at(cfg, bank, dev)
     lists = (B, 1 if cfg.token_pool else M, 1 if cfg.select_scope == MSA_SCOPE_ALL else Hkv, k)
     _call("msa_sparse_attend4", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M, K4, K4s, V4,
-          V4s, _at(idx, _I32, lists, dev, "idx"), k, Ka, Va, Lloc, local_pos0, _at(q_pos, _I32, (B, M), dev, "q_pos"),
-          _at(out, _BF16, (B, M, Hq, d), dev, "out"), _at(lse, _F32, (B, M, Hq), dev, "lse"),
-          _workspace_at(workspace, dev), workspace.numel())
+          V4s, _at(idx, _I32, lists, dev, "idx"), k, Ka, Va, Lloc, _i32(local_pos0, "local_pos0"),
+          _at(q_pos, _I32, (B, M), dev, "q_pos"), _at(out, _BF16, (B, M, Hq, d), dev, "out"),
+          _at(lse, _F32, (B, M, Hq), dev, "lse"), _workspace_at(workspace, dev), workspace.numel())
     return out, lse

@@ -392,7 +392,7 @@ int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, co
   const int64_t nq = (int64_t)dm.Hq * dm.d, nk = (int64_t)dm.Hkv * dm.d;
   if ((q != nullptr && q_stride < nq) || (k != nullptr && k_stride < nk) || (v != nullptr && v_stride < nk))
     return MSA_ERR_INVALID_ARG;
-  if ((int64_t)B * M > (1 << 28) || (int64_t)local_pos0 + Lloc > INT32_MAX) return MSA_ERR_UNSUPPORTED;
+  if ((int64_t)B * M > (1 << 25) || (int64_t)local_pos0 + Lloc > INT32_MAX) return MSA_ERR_UNSUPPORTED;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_weight) || misaligned(k_weight) ||
       misaligned(q_out) || misaligned(Kloc) || misaligned(Vloc) || misaligned4(pos) ||
       (q != nullptr && q_stride % 8 != 0) || (k != nullptr && k_stride % 8 != 0) || (v != nullptr && v_stride % 8 != 0))
@@ -451,12 +451,19 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
   return launch_unpack4(dm, x, doc_begin, doc_count, (hipStream_t)stream);
 }
 
+// Launches of the kernels over position-encoded keys: one workgroup per token in the grid's third dimension, or tiles in its
+// first, whose threads count to 2^32.
+static bool encoded_grid_ok(const Dims& dm, int32_t B, int32_t M, const EncodedPlan& pl) {
+  if (!pl.tiled) return (int64_t)B * M <= 65535;
+  return B <= 65535 && (int64_t)B * pl.n_tiles * pl.n_splits * dm.Hkv < (1 << 24);
+}
+
 static int plan_window(const Dims& dm, int32_t B, int32_t M, int32_t Lloc, int32_t window, int32_t sinks, EncodedPlan* pl) {
   if (B < 1 || M < 1 || Lloc < 1 || window < 1 || sinks < 0) return MSA_ERR_INVALID_ARG;
-  if ((int64_t)B * M > 65535 || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
+  if ((int64_t)B * M > (1 << 25) || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
   const long long seen = (long long)window + sinks;
   *pl = plan_encoded(dm, B, M, 0, false, seen < Lloc ? seen : Lloc, Lloc);
-  return MSA_OK;
+  return encoded_grid_ok(dm, B, M, *pl) ? MSA_OK : MSA_ERR_UNSUPPORTED;
 }
 
 size_t msa_window_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
@@ -500,10 +507,10 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
 
 static int plan_attend4(const Dims& dm, int32_t B, int32_t M, int32_t k, int32_t Lloc, EncodedPlan* pl) {
   if (B < 1 || M < 1 || k < 1 || Lloc < 0) return MSA_ERR_INVALID_ARG;
-  if (k > MSA_MAX_TOPK || (int64_t)B * M > 65535 || (int64_t)k * dm.G > (1 << 28) || Lloc > (1 << 28))
+  if (k > MSA_MAX_TOPK || (int64_t)B * M > (1 << 25) || (int64_t)k * dm.G > (1 << 28) || Lloc > (1 << 28))
     return MSA_ERR_UNSUPPORTED;
   *pl = plan_encoded(dm, B, M, (long long)k * dm.G, dm.token_pool == 1, Lloc, Lloc);
-  return MSA_OK;
+  return encoded_grid_ok(dm, B, M, *pl) ? MSA_OK : MSA_ERR_UNSUPPORTED;
 }
 
 size_t msa_sparse_attend4_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t k, int32_t Lloc) {

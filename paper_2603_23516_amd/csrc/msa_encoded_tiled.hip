@@ -103,7 +103,8 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
     pmin = pmax = p;
     if (p >= 0) plow = p;
   }
-  const int lo = p - a.window + 1;
+  int lo = p - a.window + 1;
+  if (lo < 0) lo = 0;  // (differences from it stay in 32 bits)
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) {
     const int u = __shfl_xor(pmin, off, 64), v = __shfl_xor(pmax, off, 64), w = __shfl_xor(plow, off, 64);

@@ -108,6 +108,11 @@ def test_pieces_and_halves():
     msa.msa_pack_kv4(cfg, K, None, 0, 1, bank)
     msa.msa_pack_kv4(cfg, K, None, 3, 2, bank)
     msa.msa_pack_kv4(cfg, K, V, 5, 0, bank)          # no documents
+    for begin, count in ((2 ** 32, None), (0, 2 ** 32), (2 ** 32, 0)):
+        with pytest.raises(ValueError):
+            msa.msa_pack_kv4(cfg, K, V, begin, count, bank)
+        with pytest.raises(ValueError):
+            msa.msa_unpack_kv4(cfg, bank, begin, count)
     assert all(torch.equal(a, b) for a, b in zip(bank, whole))
     out = torch.full_like(K, 5.0)
     got, none = msa.msa_unpack_kv4(cfg, (whole[0], whole[1], None, None), 4, 1, K=out)

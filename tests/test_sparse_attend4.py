@@ -231,6 +231,21 @@ def test_python_refusals():
     good = dict(q=q.cuda(), bank=bank, idx=idx, Kloc=Kl.cuda(), Vloc=Vl.cuda(), local_pos0=G, q_pos=pos)
     msa.msa_sparse_attend4(cfg, **good)
     for bad in (dict(q=q), dict(idx=idx[:, :1]), dict(idx=idx[:, :, :1]), dict(idx=idx.long()), dict(bank=bank[::-1]),
-                dict(bank=(None,) + bank[1:]), dict(Kloc=None), dict(q_pos=pos[:1]), dict(Vloc=Kl.cuda()[:, :, 1:])):
+                dict(bank=(None,) + bank[1:]), dict(Kloc=None), dict(q_pos=pos[:1]), dict(Vloc=Kl.cuda()[:, :, 1:]),
+                dict(local_pos0=2 ** 32 + G)):
         with pytest.raises(ValueError):
             msa.msa_sparse_attend4(cfg, **{**good, **bad})
+
+
+@pytest.mark.gpu
+def test_a_question_of_more_than_65535_tokens():
+    N, G, d, M = 6, 8, 64, 66001
+    (K, V, q, Kl, Vl), _ = _make(N, G, 2, 1, d, 1, M, 20, 0)
+    cfg = msa.MsaConfig(N, G, 1, 2, 1, d, 1e4, token_pool=1)
+    bank = msa.msa_pack_kv4(cfg.replace(bank_keys_rotated=1), K.cuda(), V.cuda())
+    idx = torch.tensor([4, -1, 2], dtype=torch.int32).reshape(1, 1, 1, 3)
+    q_pos = (G + torch.arange(M, dtype=torch.int32) % 23).reshape(1, M)
+    out, lse = msa.msa_sparse_attend4(cfg, q.cuda(), bank, idx.cuda(), Kl.cuda(), Vl.cuda(), G, q_pos.cuda())
+    at = [0, 1, 40000, 65535, 65536, M - 1]
+    kept = [P.unpack4(bank[i].cpu(), bank[i + 1].cpu()) for i in (0, 2)]
+    P.sparse_attend4(q[:, at].double(), *kept, idx, None, Kl.double(), Vl.double(), q_pos[:, at], G).check(out[:, at], lse[:, at], MANY)

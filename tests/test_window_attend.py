@@ -32,7 +32,8 @@ def _call(lib, cfg, **kw):
 @pytest.mark.parametrize("kw, status", [
     (dict(q=None), -1), (dict(K=None), -1), (dict(V=None), -1), (dict(q_pos=None), -1), (dict(out=None), -1), (dict(ws=None), -1),
     (dict(B=0), -1), (dict(M=0), -1), (dict(L=0), -1), (dict(W=0), -1), (dict(S=-1), -1), (dict(pos0=-1), -1),
-    (dict(B=256, M=256), -2), (dict(L=(1 << 28) + 1), -2), (dict(bytes=255), -3),
+    (dict(B=65536), -2), (dict(B=1 << 13, M=1 << 13), -2),
+    (dict(B=65536, M=32), -2), (dict(L=(1 << 28) + 1), -2), (dict(bytes=255), -3),
     (dict(q=ctypes.c_void_p(0x10008)), -4), (dict(K=ctypes.c_void_p(0x10002)), -4), (dict(q_pos=ctypes.c_void_p(0x10002)), -4),
     (dict(lse=ctypes.c_void_p(0x10002)), -4), (dict(ws=ctypes.c_void_p(0x10010 + 4)), -4),
 ])
@@ -48,6 +49,10 @@ def test_workspace_sizes(lib):
         assert _call(lib, c, B=B, M=M, L=L, W=W, S=S, bytes=n - 1) == msa.MSA_ERR_WORKSPACE
     assert msa.window_attend_workspace_bytes(c, 1, 1, 0, 4, 0) == 0
     assert msa.window_attend_workspace_bytes(c, 1, 1, 8, 0, 0) == 0
+    assert msa.window_attend_workspace_bytes(c, 1, 70000, 8, 2 ** 40, 2 ** 40) == msa.window_attend_workspace_bytes(c, 1, 70000, 8, 8, 0)
+    for bad in (dict(M=2 ** 32 + 1), dict(Lloc=2 ** 31), dict(window=-2 ** 40), dict(sinks=-2 ** 33)):
+        with pytest.raises(ValueError):
+            msa.window_attend_workspace_bytes(c, **{**dict(B=1, M=1, Lloc=8, window=4, sinks=0), **bad})
     # a longer cache or window never asks for less
     for cfg, B, M in itertools.product((c, _cfg(8, 1, 64)), (1, 3, 40), (1, 2, 5, 9, 31, 32, 509)):
         sizes = [msa.window_attend_workspace_bytes(cfg, B, M, L, W, S) for L, W, S in (
@@ -266,3 +271,39 @@ def test_many_tokens_at_random_places(B, M, Hq, Hkv, d, L, W, S):
             ref.put((i, h), P.attend(q[b, m, h].double(), K[b, h * Hkv // Hq].double(), V[b, h * Hkv // Hq].double(), seen))
     pick = tuple(torch.tensor(at).T)
     ref.check(out.cpu()[pick], lse.cpu()[pick], MANY)
+
+
+def _some_tokens(out, lse, q, K, V, q_pos, W, S, at):
+    ref = P.Attended((len(at), q.shape[2]), q.shape[3])
+    t = torch.arange(K.shape[2])
+    for i, m in enumerate(at):
+        p = int(q_pos[0, m])
+        seen = (t <= p) & ((p - t < W) | (t < S))
+        for h in range(q.shape[2]):
+            ref.put((i, h), P.attend(q[0, m, h].double(), K[0, 0, seen].double(), V[0, 0, seen].double(), seen[seen]))
+    ref.check(out[0, at].cpu(), lse[0, at].cpu(), MANY)
+
+
+@pytest.mark.gpu
+def test_a_prompt_of_more_than_65535_tokens():
+    M, W, S = 70001, 300, 5
+    q, K, V = _make(1, M, 2, 1, 64, M, 40)
+    q_pos = torch.arange(M, dtype=torch.int32).reshape(1, M)
+    out, lse = msa.msa_window_attend(_cfg(2, 1, 64), q.cuda(), K.cuda(), V.cuda(), q_pos.cuda(), W, sinks=S)
+    _some_tokens(out, lse, q, K, V, q_pos, W, S, [0, 1, 299, 300, 306, 40000, 65534, 65535, 65536, 65600, M - 65, M - 1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [2, 40])
+def test_sizes_past_32_bits(M):
+    """A window, or a number of first tokens, past 32 bits sees everything; what would be cut off is refused."""
+    cfg = _cfg(2, 1, 64)
+    q, K, V = (t.cuda() for t in _make(1, M, 2, 1, 64, 90, 41))
+    pos = (90 - M + torch.arange(M)).reshape(1, M).to(torch.int32).cuda()
+    want = msa.msa_window_attend(cfg, q, K, V, pos, 90)
+    for W, S in ((2 ** 31, 0), (2 ** 32 + 5, 0), (3, 2 ** 32), (2 ** 31 - 1, 0)):
+        got = msa.msa_window_attend(cfg, q, K, V, pos, W, sinks=S)
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    for bad in (dict(local_pos0=2 ** 32), dict(window=-2 ** 32 + 9), dict(sinks=-2 ** 32)):
+        with pytest.raises(ValueError):
+            msa.msa_window_attend(cfg, q, K, V, pos, **{**dict(window=9), **bad})
