@@ -13,6 +13,11 @@
  *                           concatenates as printed (attended with bank_keys_rotated = 1)
  *   msa_fetch_selected      the host-DRAM tier of Section 3.4.2: gathers the selected documents from a
  *                           pinned host bank into a device staging bank
+ * and what stands next to them in a model's layers:
+ *   msa_norm_rotate         head norms and rotation of a layer's projections, keys and values into the local cache
+ *   msa_window_attend       attention over the local cache (window and first tokens), for layers that do not route
+ *   msa_pack_kv4            offline: a bank in four bits, 0.27 of its bytes (msa_unpack_kv4 back)
+ *   msa_sparse_attend4      msa_sparse_attend over that bank
  *
  * Notation: N documents, G tokens per document, P chunk size, C = G/P chunks per document,
  * Hq query heads, Hkv key/value heads, r = Hq/Hkv, d head dimension, B sequences, M query tokens per
