@@ -416,6 +416,17 @@ def _call(name, dev, stream, cfg, *args):
         raise MsaError(rc, name)
 
 
+def _new(shape, dtype, device, stream):
+    """A tensor that a call on `stream` (None: the current one) fills.  On another stream it is of that stream's memory, where
+    nothing of the current one is pending, and what the current stream does with it is done before it is given out again."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _tokens_at(t, B, M, heads, d, dev, name):
     """(address, elements from one token to the next) of a tensor [B][M][heads][d]; a view of a fused projection is taken as
     it lies."""
@@ -446,7 +457,7 @@ def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None,
     if q is not None:
         qa, qs = _tokens_at(q, B, M, Hq, d, dev, "q")
         if q_out is None:
-            q_out = torch.empty((B, M, Hq, d), dtype=_BF16, device=q.device)
+            q_out = _new((B, M, Hq, d), _BF16, q.device, stream)
         qo = _at(q_out, _BF16, (B, M, Hq, d), dev, "q_out")
     if k is not None:
         ka, ks = _tokens_at(k, B, M, Hkv, d, dev, "k")
@@ -464,10 +475,11 @@ def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None,
     return q_out
 
 
-def alloc_kv4(cfg, device="cuda"):
-    """(K4, K4s, V4, V4s) of a bank in four bits: codes uint8 [N][Hkv][G][d/2], scale bytes uint8 [N][Hkv][G][d/32]."""
+def alloc_kv4(cfg, device="cuda", stream=None):
+    """(K4, K4s, V4, V4s) of a bank in four bits: codes uint8 [N][Hkv][G][d/2], scale bytes uint8 [N][Hkv][G][d/32].  stream:
+    the one that fills it, where that is not the current one."""
     rows = (cfg.n_docs, cfg.n_kv_heads, cfg.doc_len)
-    return tuple(torch.empty(rows + (cfg.head_dim // n,), dtype=_U8, device=device) for n in (2, 32, 2, 32))
+    return tuple(_new(rows + (cfg.head_dim // n,), _U8, device, stream) for n in (2, 32, 2, 32))
 
 
 def _kv4_at(cfg, bank, dev):
@@ -490,7 +502,7 @@ def msa_pack_kv4(cfg, K, V, doc_begin=0, doc_count=None, bank=None, stream=None)
     if doc_count is None:
         doc_count = shape[0] - doc_begin
     if bank is None:
-        bank = alloc_kv4(cfg, src.device)
+        bank = alloc_kv4(cfg, src.device, stream)
     K4, K4s, V4, V4s = _kv4_at(cfg, bank, dev)
     Ka = Va = None
     if K is None:
@@ -522,12 +534,12 @@ def msa_unpack_kv4(cfg, bank, doc_begin=0, doc_count=None, K=None, V=None, strea
     if K4 is None:
         K = None
     else:
-        K = torch.empty(shape, dtype=_BF16, device=src.device) if K is None else K
+        K = _new(shape, _BF16, src.device, stream) if K is None else K
         Ka = _at(K, _BF16, shape, dev, "K")
     if V4 is None:
         V = None
     else:
-        V = torch.empty(shape, dtype=_BF16, device=src.device) if V is None else V
+        V = _new(shape, _BF16, src.device, stream) if V is None else V
         Va = _at(V, _BF16, shape, dev, "V")
     _call("msa_unpack_kv4", dev, stream, ctypes.byref(cfg), *at, _i32(doc_begin, "doc_begin"), _i32(doc_count, "doc_count"),
           Ka, Va)
@@ -548,14 +560,6 @@ def sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc):
                                                              _i32(Lloc, "Lloc"))
 
 
-def _workspace(size, device, stream):
-    """A workspace for one call, of the memory of the stream that it is used on."""
-    if stream is None:
-        return torch.empty(max(size, 256), dtype=_U8, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(max(size, 256), dtype=_U8, device=device)
-
-
 def _workspace_at(t, dev):
     if t.dtype is not _U8 or t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"workspace: expected a contiguous tensor of torch.uint8 on cuda:{dev}")
@@ -573,11 +577,11 @@ def msa_window_attend(cfg, q, Kloc, Vloc, q_pos, window, sinks=0, local_pos0=0, 
         raise ValueError("msa_window_attend: expected q [B][M][Hq][d] and Kloc [B][Hkv][Lloc][d]")
     B, M, Lloc = q.shape[0], q.shape[1], Kloc.shape[2]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new((B, M, Hq, d), _BF16, q.device, stream)
     if lse is None:
-        lse = torch.empty((B, M, Hq), dtype=_F32, device=q.device)
+        lse = _new((B, M, Hq), _F32, q.device, stream)
     if workspace is None:
-        workspace = _workspace(window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), q.device, stream)
+        workspace = _new(max(window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), 256), _U8, q.device, stream)
     _call("msa_window_attend", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M,
           _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc"), Lloc,
           _i32(local_pos0, "local_pos0"), window, sinks, _at(q_pos, _I32, (B, M), dev, "q_pos"),
@@ -601,11 +605,11 @@ def msa_sparse_attend4(cfg, q, bank, idx, Kloc, Vloc, local_pos0, q_pos, out=Non
         Lloc = Kloc.shape[2]
         Ka, Va = _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc")
     if out is None:
-        out = torch.empty_like(q)
+        out = _new((B, M, Hq, d), _BF16, q.device, stream)
     if lse is None:
-        lse = torch.empty((B, M, Hq), dtype=_F32, device=q.device)
+        lse = _new((B, M, Hq), _F32, q.device, stream)
     if workspace is None:
-        workspace = _workspace(sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), q.device, stream)
+        workspace = _new(max(sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), 256), _U8, q.device, stream)
     K4, K4s, V4, V4s = _kv4_at(cfg, bank, dev)
     lists = (B, 1 if cfg.token_pool else M, 1 if cfg.select_scope == MSA_SCOPE_ALL else Hkv, k)
     _call("msa_sparse_attend4", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M, K4, K4s, V4,

@@ -249,3 +249,38 @@ def test_a_question_of_more_than_65535_tokens():
     at = [0, 1, 40000, 65535, 65536, M - 1]
     kept = [P.unpack4(bank[i].cpu(), bank[i + 1].cpu()) for i in (0, 2)]
     P.sparse_attend4(q[:, at].double(), *kept, idx, None, Kl.double(), Vl.double(), q_pos[:, at], G).check(out[:, at], lse[:, at], MANY)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", ["norm", "window", "attend4", "pack", "unpack"])
+def test_results_on_another_stream_take_no_memory_in_use(what):
+    """What the current stream still has to read, though its tensors are gone, is not handed to a call on another stream."""
+    N, G, Hq, Hkv, d, B, M = 16, 64, 8, 2, 64, 2, 64
+    (K, V, q, Kl, Vl), _ = _make(N, G, Hq, Hkv, d, B, M, M, 21)
+    K, V, q, Kl, Vl = (t.cuda() for t in (K, V, q, Kl, Vl))
+    cfg = _cfg(N, G, Hq, Hkv, d)
+    bank = msa.msa_pack_kv4(cfg, K, V)
+    pos = torch.arange(M, dtype=torch.int32, device="cuda").repeat(B, 1)
+    idx = torch.zeros((B, M, Hkv, 2), dtype=torch.int32, device="cuda")
+    kt, vt = Kl.transpose(1, 2).contiguous(), Vl.transpose(1, 2).contiguous()
+    Kn, Vn = torch.zeros_like(Kl), torch.zeros_like(Vl)
+    calls = dict(norm=lambda s: msa.msa_norm_rotate(cfg, q, kt, vt, pos, Kn, Vn, stream=s),
+                 window=lambda s: msa.msa_window_attend(cfg, q, Kl, Vl, pos, 20, stream=s),
+                 attend4=lambda s: msa.msa_sparse_attend4(cfg, q, bank, idx, Kl, Vl, 0, pos, stream=s),
+                 pack=lambda s: msa.msa_pack_kv4(cfg, K, V, stream=s), unpack=lambda s: msa.msa_unpack_kv4(cfg, bank, stream=s))
+    want = calls[what](None)
+    want = [want] if torch.is_tensor(want) else list(want)
+    sizes = [t.numel() * t.element_size() for t in want]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        held = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in sizes]
+        torch.cuda._sleep(20_000_000)
+        kept = [t.clone() for t in held]
+        del held
+        got = calls[what](side)
+        got = [got] if torch.is_tensor(got) else list(got)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(bool((t == 7).all()) for t in kept)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
