@@ -170,15 +170,16 @@ int launch_pack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, bool
     const RopeTheta& table = rope_table(dm.base, dm.d);
     for (int u = 0; u < kMaxHalf; ++u) th.th[u] = table.th[u];
   }
-  // From 131072 rows of a tensor on four rows to a thread, which gives fewer waves with more in flight each (262144 rows of 128
-  // dims, packed and unpacked, 58 -> 53 us; 64064 rows 17.4 -> 19.0), from 128 MiB on streaming loads (2 million rows 540 ->
-  // 504 with both), and streaming stores where the caches do not hold the codes for the next reader either, 1 GiB of rows on
-  // (2 million rows 496 -> 479; 262144 rows 52.6 -> 60.7).  Keys to be turned have four rows to a thread at any size, which share
+  // Two rows to a thread (against one, packed and unpacked: 128000 rows of 128 dims 30.8 -> 28.4 us, 64064 17.1 -> 16.6), from
+  // 131072 rows of a tensor on four, which gives fewer waves with more in flight each (against one: 262144 rows 58 -> 53;
+  // 64064 rows 17.4 -> 19.0), from 128 MiB on streaming loads (2 million rows 540 -> 504 with both), and streaming stores where
+  // the caches do not hold the codes for the next reader either, 1 GiB of rows on (2 million rows 496 -> 479; 262144 rows
+  // 52.6 -> 60.7).  Keys to be turned have four rows to a thread at any size, which share
   // their angles (one row to a thread, 64064 rows of keys and values 15.4 us for 13.4).
   const int n_tensors = a.x[0] != nullptr && a.x[1] != nullptr ? 2 : 1;
   const bool many = rotate || a.n_rows >= 131072;
   const long long bytes = a.n_rows * dm.d * 2 * n_tensors;
-  const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8) * (many ? 4 : 1)), n_tensors);
+  const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8) * (many ? 4 : 2)), n_tensors);
 #define MSA_PACK4(DD, RR, ROWS, SS) hipLaunchKernelGGL((pack4_kernel<DD, RR, ROWS, SS>), grid, dim3(256), 0, st, a, th)
 #define MSA_PACK4_MANY(DD, RR)                                 \
   do {                                                         \
@@ -189,11 +190,11 @@ int launch_pack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, bool
   if (dm.d == 128) {
     if (rotate) MSA_PACK4_MANY(128, true);
     else if (many) MSA_PACK4_MANY(128, false);
-    else MSA_PACK4(128, false, 1, 0);
+    else MSA_PACK4(128, false, 2, 0);
   } else {
     if (rotate) MSA_PACK4_MANY(64, true);
     else if (many) MSA_PACK4_MANY(64, false);
-    else MSA_PACK4(64, false, 1, 0);
+    else MSA_PACK4(64, false, 2, 0);
   }
 #undef MSA_PACK4_MANY
 #undef MSA_PACK4
