@@ -1,6 +1,7 @@
 """msa_window_attend against the plain definition in 64 bits: windows, first tokens, positions in any order, empty rows."""
 import ctypes
 import itertools
+import threading
 
 import pytest
 import torch
@@ -307,3 +308,59 @@ def test_sizes_past_32_bits(M):
     for bad in (dict(local_pos0=2 ** 32), dict(window=-2 ** 32 + 9), dict(sinks=-2 ** 32)):
         with pytest.raises(ValueError):
             msa.msa_window_attend(cfg, q, K, V, pos, **{**dict(window=9), **bad})
+
+
+@pytest.mark.gpu
+def test_two_graphs_share_a_workspace():
+    """Graphs of different layouts of one workspace, replayed in turn, with eager calls through it in between."""
+    cfg = _cfg(32, 8, 128)
+    sets = []
+    for M, L in ((1, 3000), (256, 2100), (48, 3000), (2, 1500)):      # parts of single tokens, of tiles (two, more), again
+        q, K, V = (t.cuda() for t in _make(1, M, 32, 8, 128, L, 50 + M))
+        sets.append((q, K, V, (L - M + torch.arange(M)).reshape(1, M).to(torch.int32).cuda(), L))
+    want = [msa.msa_window_attend(cfg, *s) for s in sets]
+    size = max(msa.window_attend_workspace_bytes(cfg, 1, s[0].shape[1], s[4], s[4]) for s in sets)
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+    outs = [(torch.empty_like(a), torch.empty_like(b)) for a, b in want]
+    torch.cuda.synchronize()
+    side, graphs = torch.cuda.Stream(), []
+    for s, (o, l) in zip(sets, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            msa.msa_window_attend(cfg, *s, out=o, lse=l, workspace=ws, stream=side)
+    for turn in range(4):
+        for i in (0, 1, 2, 3, 1, 0):
+            for t in outs[i]:
+                t.fill_(3.0)
+            graphs[i].replay()
+            again = msa.msa_window_attend(cfg, *sets[(i + turn) % 4], workspace=ws)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i])), (turn, i)
+            assert all(torch.equal(a, b) for a, b in zip(again, want[(i + turn) % 4])), (turn, i)
+
+
+@pytest.mark.gpu
+def test_calls_from_two_threads():
+    cfg = _cfg(8, 2, 64)
+    sets = []
+    for i, M in enumerate((1, 100)):
+        q, K, V = (t.cuda() for t in _make(1, M, 8, 2, 64, 1000, 60 + i))
+        sets.append((q, K, V, (1000 - M + torch.arange(M)).reshape(1, M).to(torch.int32).cuda(), 1000))
+    want = [msa.msa_window_attend(cfg, *s) for s in sets]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        for _ in range(50):
+            got = msa.msa_window_attend(cfg, *sets[i], stream=stream)
+            stream.synchronize()
+            if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in (0, 1, 0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
