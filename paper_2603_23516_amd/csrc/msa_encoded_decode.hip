@@ -373,9 +373,11 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   // documents' expansion cost.  us, tiled / one by one, M tokens: 8 heads of 128 over 2048 rows, M = 4 12 / 14, 16 14 / 22;
   // 8 sequences over 4096 rows, M = 2 40 / 36, 4 40 / 63, 8 31 / 115; heads of 64 that share nothing (r = 1) over 2048 rows,
   // M = 8 14 / 11, 16 14 / 14; 16 documents of 512, M = 4 40 / 17, 16 39 / 33; 3 times 8 of 64, M = 8 20 / 16, 16 22 / 25.
-  // (More rows never lead back to the single-token kernel.)
-  const long long cost = (mem_rows + 31) / 32 + kLocalCost * ((local_rows + 31) / 32), work = pairs * cost;
-  p.tiled = (mem_rows == 0 || shared) && (M >= 32 || (M >= (mem_rows > 0 ? 8 : 4) && work >= 20000 + B * dm.Hkv * mem_rows / 4)) ? 1 : 0;
+  // (More rows never lead back to the single-token kernel: both sides count them in whole steps, M of them on the left and 8 on
+  // the right, which applies from M = 8 on.)
+  const long long steps_mem = (mem_rows + 31) / 32, cost = steps_mem + kLocalCost * ((local_rows + 31) / 32);
+  const long long work = pairs * cost, least = 20000 + 8 * pairs / M * steps_mem;
+  p.tiled = (mem_rows == 0 || shared) && (M >= 32 || (M >= (mem_rows > 0 ? 8 : 4) && work >= least)) ? 1 : 0;
   int n_most;  // splits that the workspace holds: grows with the rows, so that one sized for the longest call serves all
   long long most1 = (cost + 15) / 16;
   if (most1 > 2048 / pairs) most1 = 2048 / pairs;

@@ -1,6 +1,7 @@
 """msa_sparse_attend4 against the plain definition in 64 bits over what the packed bank stands for, alone and at the end of the
 chain that leads to it."""
 import ctypes
+import itertools
 
 import pytest
 import torch
@@ -57,6 +58,21 @@ def test_refused_sizes(lib):
                 sizes = [msa.sparse_attend4_workspace_bytes(cfg, B, M, k, L)
                          for k, L in ((k0, 0), (k0, 10), (min(k0 + 1, k1), 600), (k1, 600), (k1, 4000), (k1, 50000))]
                 assert sizes == sorted(sizes), (B, M, k0)
+
+
+@pytest.mark.parametrize("G", [1, 3, 8, 20, 33, 512])
+@pytest.mark.parametrize("Hq, Hkv, d", [(32, 8, 128), (8, 1, 64), (8, 8, 64)])
+def test_more_documents_never_ask_for_less(G, Hq, Hkv, d):
+    """Every k at a fixed local context, and lengths around the border between the two kernels at a fixed k: what serves the
+    largest call serves the smaller ones."""
+    cfg = _cfg(2048, G, Hq, Hkv, d, token_pool=1)
+    for B, M in itertools.product((1, 3, 8, 64, 400), (1, 7, 8, 9, 16, 31, 32, 40)):
+        for L in (0, 1, 100, 1111, 3328, 9000):
+            sizes = [msa.sparse_attend4_workspace_bytes(cfg, B, M, k, L) for k in range(1, 65)]
+            assert sizes == sorted(sizes), (B, M, L)
+        for k in (1, 2, 31, 64):
+            sizes = [msa.sparse_attend4_workspace_bytes(cfg, B, M, k, L) for L in range(0, 3600, 16)]
+            assert sizes == sorted(sizes), (B, M, k)
 
 
 def _make(N, G, Hq, Hkv, d, B, M, L, seed):
