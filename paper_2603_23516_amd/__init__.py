@@ -450,6 +450,8 @@ def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None,
     src = q if q is not None else k if k is not None else v
     if src is None or src.dim() != 4:
         raise ValueError("msa_norm_rotate: expected q, k or v as [B][M][heads][d]")
+    if (Kloc is not None and Kloc.dim() != 4) or (Vloc is not None and Vloc.dim() != 4):
+        raise ValueError("msa_norm_rotate: expected Kloc and Vloc as [B][Hkv][Lloc][d]")
     dev = _gpu(src, "msa_norm_rotate")
     B, M = src.shape[:2]
     qa = ka = va = qo = Ka = Va = None

@@ -176,3 +176,13 @@ def test_a_long_prompt_is_read_with_streaming_loads():
         q1 = msa.msa_norm_rotate(cfg, y[:, :, :Hq], y[:, :, Hq:Hq + Hkv], y[:, :, Hq + Hkv:], pos[:, m0:m0 + 5].contiguous(), K1, V1, w, w,
                                  local_pos0=m0)
         assert torch.equal(q[:, m0:m0 + 5], q1) and torch.equal(K[:, :, m0:m0 + 5], K1) and torch.equal(V[:, :, m0:m0 + 5], V1)
+
+
+@pytest.mark.parametrize("Kloc, Vloc", [((2, 64), (1, 2, 4, 64)), ((1, 2, 4, 64), (4, 64)), ((64,), None), (None, (8, 64)), ((1, 1, 2, 4, 64), None)])
+def test_caches_of_other_ranks(Kloc, Vloc):
+    """Refused like a cache of another shape, before anything else is read of them."""
+    cfg = _cfg()
+    kv = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16)
+    K, V = (None if s is None else torch.zeros(s, dtype=torch.bfloat16) for s in (Kloc, Vloc))
+    with pytest.raises(ValueError, match="Kloc and Vloc"):
+        msa.msa_norm_rotate(cfg, None, None if K is None else kv, None if V is None else kv, torch.zeros((1, 1), dtype=torch.int32), K, V)
