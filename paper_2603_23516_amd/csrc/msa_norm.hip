@@ -15,8 +15,21 @@
 
 namespace msa {
 
+// The sum of a head's squares, in every lane that holds a part of it.
+template <int LPH>
+__device__ __forceinline__ float head_sum_of_squares(const float (&f1)[8], const float (&f2)[8]) {
+  float ss = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ss += f1[e] * f1[e] + f2[e] * f2[e];
+  ss += dpp_f<kDppXor1>(ss);
+  ss += dpp_f<kDppXor2>(ss);
+  if (LPH == 8) ss += dpp_f<kDppHalfMirror>(ss);
+  return ss;
+}
+
+// (Eight waves to a SIMD: the path of large squares would make it seven.)
 template <int D, bool STREAM>
-__global__ __launch_bounds__(256) void norm_rotate_kernel(NormArgs a, NormTheta th) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(8))) void norm_rotate_kernel(NormArgs a, NormTheta th) {
   constexpr int HALF = D / 2;
   constexpr int LPH = D / 16;    // lanes per head
   constexpr int HPW = 64 / LPH;  // heads per wave and turn
@@ -70,13 +83,19 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormArgs a, NormTheta 
     }
     const uint16_t* wt = kind == 0 ? a.qw : a.kw;
     if (wt != nullptr) {
-      float ss = 0.f;
+      float ss = head_sum_of_squares<LPH>(f1, f2), eps = a.eps;
+      if (__ballot(ss == INFINITY) != 0) {  // elements of 2^60 and more, whose squares fp32 does not hold: 2^-70 of them
+        const float c = ss == INFINITY ? 0x1p-70f : 1.f;  // (the lanes of a head agree)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss += f1[e] * f1[e] + f2[e] * f2[e];
-      ss += dpp_f<kDppXor1>(ss);
-      ss += dpp_f<kDppXor2>(ss);
-      if (LPH == 8) ss += dpp_f<kDppHalfMirror>(ss);
-      const float rs = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+        for (int e = 0; e < 8; ++e) {
+          f1[e] *= c;
+          f2[e] *= c;
+        }
+        ss = head_sum_of_squares<LPH>(f1, f2);
+        eps *= c;
+        eps *= c;
+      }
+      const float rs = 1.0f / sqrtf(ss * (1.0f / D) + eps);
       const uint4 g1 = *reinterpret_cast<const uint4*>(wt + 8 * l), g2 = *reinterpret_cast<const uint4*>(wt + HALF + 8 * l);
       const uint32_t v1[4] = {g1.x, g1.y, g1.z, g1.w}, v2[4] = {g2.x, g2.y, g2.z, g2.w};
 #pragma unroll

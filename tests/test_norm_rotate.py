@@ -186,3 +186,34 @@ def test_caches_of_other_ranks(Kloc, Vloc):
     K, V = (None if s is None else torch.zeros(s, dtype=torch.bfloat16) for s in (Kloc, Vloc))
     with pytest.raises(ValueError, match="Kloc and Vloc"):
         msa.msa_norm_rotate(cfg, None, None if K is None else kv, None if V is None else kv, torch.zeros((1, 1), dtype=torch.int32), K, V)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("top", [2.0 ** 58, 2.0 ** 61, 1e30, 3.38e38])
+@pytest.mark.parametrize("eps", [1e-6, 1e38])
+def test_squares_past_fp32(d, top, eps):
+    """Finite elements whose squares fp32 does not hold, all of a head or one of it, beside heads of ordinary size.  The bound: one
+    rounding to bf16, and in fp32 at most 32 roundings of the pair's magnitude; nothing here underflows (2^-80 at least)."""
+    B, M, Hq, Hkv = 1, 5, 8, 2
+    g = torch.Generator().manual_seed(d)
+    x = torch.randn((B, M, Hq + 2 * Hkv, d), generator=g).clamp(-4, 4)
+    x = torch.where(x.abs() < 0.01, 0.01, x)
+    x[:, ::2, :, :] *= top / 4
+    x[:, 1] *= top * 2.0 ** -40
+    x[:, 1, :, d // 3] = -top
+    x[:, 3, ::2] *= top / 4
+    x = x.to(torch.bfloat16)
+    assert bool(x.isfinite().all())
+    w = [(1 + 0.2 * torch.randn(d, generator=g)).to(torch.bfloat16) for _ in range(2)]
+    pos = torch.arange(M, dtype=torch.int32).reshape(B, M)
+    K, V = (torch.zeros((B, Hkv, M, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    xd = x.cuda()
+    q = msa.msa_norm_rotate(_cfg(Hq, Hkv, d), xd[:, :, :Hq], xd[:, :, Hq:Hq + Hkv], xd[:, :, Hq + Hkv:], pos.cuda(), K, V,
+                            w[0].cuda(), w[1].cuda(), eps=eps)
+    eps = float(torch.tensor(eps, dtype=torch.float32))
+    for got, src, wt in ((q, x[:, :, :Hq], w[0]), (K.transpose(1, 2), x[:, :, Hq:Hq + Hkv], w[1])):
+        y = P.norm(src.double(), wt.double(), eps)
+        want, size = P.rotate(y, pos[:, :, None].expand(y.shape[:-1]), 1e4), y.abs() + y.abs().roll(d // 2, -1)
+        err = (got.double().cpu() - want).abs() - (HALF_BF16 * want.abs() + 32 * 2.0 ** -24 * size)
+        assert float(err.max()) <= 0, float(err.max())
