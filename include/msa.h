@@ -380,8 +380,8 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
  *   lse       out  fp32 [B][M][Hq], may be NULL
  *   workspace      >= msa_window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks), which does not fall as Lloc, window
  *                  or sinks grow; contents undefined on entry/exit
- * B <= 65535; B * M <= 65535 for M < 32, from there on as many tokens as make 2^24 tiles of 128 (token, head) pairs of a KV
- * head; Lloc <= 2^28.
+ * B, n_kv_heads <= 65535; B * M <= 65535 for M < 32, from there on as many tokens as make 2^24 tiles of 128 (token, head)
+ * pairs of a KV head; Lloc <= 2^28.
  * Scores, their maximum and sum and the outputs are accumulated in fp32.  With few tokens the softmax weights are carried as
  * bf16 (hi, lo) pairs, with many as bf16.  Reads n_q_heads, n_kv_heads and head_dim of cfg.
  */

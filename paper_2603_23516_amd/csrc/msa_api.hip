@@ -451,19 +451,17 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
   return launch_unpack4(dm, x, doc_begin, doc_count, (hipStream_t)stream);
 }
 
-// Launches of the kernels over position-encoded keys: one workgroup per token in the grid's third dimension, or tiles in its
-// first, whose threads count to 2^32.
-static bool encoded_grid_ok(const Dims& dm, int32_t B, int32_t M, const EncodedPlan& pl) {
-  if (!pl.tiled) return (int64_t)B * M <= 65535;
-  return B <= 65535 && (int64_t)B * pl.n_tiles * pl.n_splits * dm.Hkv < (1 << 24);
+// Sequences and KV heads are dimensions of the grids of the kernels over position-encoded keys.
+static bool encoded_sizes_ok(const Dims& dm, int32_t B, int32_t M) {
+  return B <= 65535 && dm.Hkv <= 65535 && (int64_t)B * M <= (1 << 25);
 }
 
 static int plan_window(const Dims& dm, int32_t B, int32_t M, int32_t Lloc, int32_t window, int32_t sinks, EncodedPlan* pl) {
   if (B < 1 || M < 1 || Lloc < 1 || window < 1 || sinks < 0) return MSA_ERR_INVALID_ARG;
-  if ((int64_t)B * M > (1 << 25) || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
+  if (!encoded_sizes_ok(dm, B, M) || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
   const long long seen = (long long)window + sinks;
   *pl = plan_encoded(dm, B, M, 0, false, seen < Lloc ? seen : Lloc, Lloc);
-  return encoded_grid_ok(dm, B, M, *pl) ? MSA_OK : MSA_ERR_UNSUPPORTED;
+  return pl->ws_bytes != 0 ? MSA_OK : MSA_ERR_UNSUPPORTED;
 }
 
 size_t msa_window_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
@@ -507,10 +505,10 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
 
 static int plan_attend4(const Dims& dm, int32_t B, int32_t M, int32_t k, int32_t Lloc, EncodedPlan* pl) {
   if (B < 1 || M < 1 || k < 1 || Lloc < 0) return MSA_ERR_INVALID_ARG;
-  if (k > MSA_MAX_TOPK || (int64_t)B * M > (1 << 25) || (int64_t)k * dm.G > (1 << 28) || Lloc > (1 << 28))
+  if (k > MSA_MAX_TOPK || !encoded_sizes_ok(dm, B, M) || (int64_t)k * dm.G > (1 << 28) || Lloc > (1 << 28))
     return MSA_ERR_UNSUPPORTED;
   *pl = plan_encoded(dm, B, M, (long long)k * dm.G, dm.token_pool == 1, Lloc, Lloc);
-  return encoded_grid_ok(dm, B, M, *pl) ? MSA_OK : MSA_ERR_UNSUPPORTED;
+  return pl->ws_bytes != 0 ? MSA_OK : MSA_ERR_UNSUPPORTED;
 }
 
 size_t msa_sparse_attend4_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t k, int32_t Lloc) {

@@ -39,7 +39,8 @@ struct EncodedPlan {
   size_t ws_bytes;
 };
 // mem_rows: k G, 0 without a bank; shared: the tokens of a sequence have their bank rows in common; local_rows: rows of the
-// cache that a token can see.
+// cache that a token can see.  ws_bytes is 0 where the grid does not hold the call: one workgroup per token in its third
+// dimension, or tiles in its first, whose threads count to 2^32.
 EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc);
 int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, void* ws, hipStream_t st);
 int launch_encoded_tiled(const Dims& dm, const EncodedArgs& a, TiledArgs ta, int B, hipStream_t st);

@@ -391,6 +391,7 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     p.tpw = 32 / dm.r;
     p.n_tiles = (M + 4 * p.tpw - 1) / (4 * p.tpw);
     const long long tiles = (long long)B * p.n_tiles * dm.Hkv, heads = (long long)B * M * dm.Hq;
+    if (tiles >= 1 << 24) return p;  // (parts: 1024 workgroups in all at most)
     const long long seen = local_rows + 4 * p.tpw;
     const long long all_steps = (mem_rows + 31) / 32 + ((seen < Lloc ? seen : Lloc) + 31) / 32;
     long long most = all_steps / 4;
@@ -419,6 +420,7 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
     // n parts 3 us and 0.3 for each (8 heads, 8 streams, 512 steps of bank rows and 64 local ones: n = 2 76 us, 4 45,
     // 8 41, 12 46, 16 49; 32 streams, 8 and 32 steps: n = 2 29 us, 4 35, 8 52, 16 93; one stream, 256 local steps: n = 4 34, 8
     // 21, 12 17, 16 15.2, 24 14.4, 32 15.8).
+    if ((long long)B * M > 65535) return p;
     n_most = single_most;
     long long best = -1;
     for (int n = 1; n <= n_most; ++n) {
