@@ -46,8 +46,9 @@ int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, 
 int launch_encoded_tiled(const Dims& dm, const EncodedArgs& a, TiledArgs ta, int B, hipStream_t st);
 
 // The rows of a selection numbered through, by the 64 lanes of one wave: pre[j] rows lie in front of slot j's document, which
-// lane j gets back; pads, ids outside the bank and rows past a document's end are left out.  pre has MSA_MAX_TOPK + 1 entries.
-__device__ __forceinline__ int number_rows(const EncodedArgs& a, int b, long long bm, int g, int lane, int* pre) {
+// lane j gets back, `before` with pre[lane]; pads, ids outside the bank and rows past a document's end are left out.  pre has
+// MSA_MAX_TOPK + 1 entries.
+__device__ __forceinline__ int number_rows(const EncodedArgs& a, int b, long long bm, int g, int lane, int* pre, int& before) {
   int doc = -1, len = 0;
   if (lane < a.k) {
     doc = a.idx[((a.idx_rows_per_b == 1 ? b : bm) * a.idx_sel + (a.idx_sel == 1 ? 0 : g)) * a.k + lane];
@@ -67,6 +68,7 @@ __device__ __forceinline__ int number_rows(const EncodedArgs& a, int b, long lon
   }
   pre[lane + 1] = sum;
   if (lane == 0) pre[0] = 0;
+  before = sum - len;
   return doc;
 }
 

@@ -92,8 +92,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   int rows_mem = 0;
   if (BANK4) {
     if (wave == 0) {
-      const int doc = number_rows(a, b, bm, g, lane, pre);
-      base[lane] = ((long long)doc * a.Hkv + g) * a.G - pre[lane];
+      int before;  // (from the register: pre[lane] is another lane's to write, and nothing waits for it here)
+      const int doc = number_rows(a, b, bm, g, lane, pre, before);
+      base[lane] = ((long long)doc * a.Hkv + g) * a.G - before;
     }
     lds_barrier();
     rows_mem = __builtin_amdgcn_readfirstlane(pre[MSA_MAX_TOPK]);

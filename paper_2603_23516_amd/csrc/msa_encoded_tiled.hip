@@ -46,7 +46,8 @@ __global__ __launch_bounds__(256) void expand4_kernel(EncodedArgs a, uint16_t* _
   constexpr int LPR = D / 8, RPB = 256 / LPR;
   __shared__ int pre[MSA_MAX_TOPK + 1], docs[MSA_MAX_TOPK];
   const int tid = threadIdx.x, g = blockIdx.y, b = blockIdx.z;
-  if (tid < 64) docs[tid] = number_rows(a, b, b, g, tid, pre);
+  int before;
+  if (tid < 64) docs[tid] = number_rows(a, b, b, g, tid, pre, before);
   __syncthreads();
   const int rows = pre[MSA_MAX_TOPK];
   const long long pair = (long long)b * a.Hkv + g;
