@@ -1,6 +1,7 @@
 // Test-only probes of the device helpers in paper_2603_23516_amd/csrc/msa_device.h: the MFMA operand
 // layout, the DPP group maximum, bf16 packing and the ordered selection keys.  One wavefront each.
 #include "../../paper_2603_23516_amd/csrc/msa_device.h"
+#include "../../paper_2603_23516_amd/csrc/msa_encoded.h"
 
 using namespace msa;
 
@@ -103,4 +104,16 @@ extern "C" void probe_pack(const void* in, void* out, void* hi, void* lo, int n)
 extern "C" void probe_keys(const void* score, const void* doc, void* key, void* sb, void* db, int n) {
   hipLaunchKernelGGL(probe_keys_kernel, dim3((n + 255) / 256), dim3(256), 0, 0, (const float*)score,
                      (const uint32_t*)doc, (unsigned long long*)key, (float*)sb, (uint32_t*)db, n);
+}
+
+// The plan of a call over position-encoded keys (the library's own function): parts per pair or tile, negative where the tokens
+// go through the tiled kernel, 0 where no grid holds the call.
+extern "C" int probe_encoded_plan(int Hq, int Hkv, int d, int B, int M, long long mem_rows, int shared, long long local_rows, int Lloc) {
+  Dims dm{};
+  dm.Hq = Hq;
+  dm.Hkv = Hkv;
+  dm.r = Hq / Hkv;
+  dm.d = d;
+  const EncodedPlan p = plan_encoded(dm, B, M, mem_rows, shared != 0, local_rows, Lloc);
+  return p.ws_bytes == 0 ? 0 : (p.tiled ? -p.n_splits : p.n_splits);
 }
