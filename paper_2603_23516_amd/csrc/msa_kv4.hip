@@ -145,7 +145,7 @@ __global__ __launch_bounds__(256) void unpack4_kernel(Pack4Args a) {
   }
 }
 
-constexpr long long kStreamBytes = 128ll << 20, kStreamCodesBytes = 1ll << 30;
+constexpr long long kStreamBytes = 128ll << 20, kStreamCodes = 256ll << 20;
 
 static unsigned stream_blocks(long long n_rows, int rows_per_block) {
   const long long n = (n_rows + rows_per_block - 1) / rows_per_block;
@@ -172,19 +172,22 @@ int launch_pack4(const Dims& dm, Pack4Args x, int doc_begin, int doc_count, bool
   }
   // Two rows to a thread (against one, packed and unpacked: 128000 rows of 128 dims 30.8 -> 28.4 us, 64064 17.1 -> 16.6), from
   // 131072 rows of a tensor on four, which gives fewer waves with more in flight each (against one: 262144 rows 58 -> 53;
-  // 64064 rows 17.4 -> 19.0), from 128 MiB on streaming loads (2 million rows 540 -> 504 with both), and streaming stores where
-  // the caches do not hold the codes for the next reader either, 1 GiB of rows on (2 million rows 496 -> 479; 262144 rows
-  // 52.6 -> 60.7).  Keys to be turned have four rows to a thread at any size, which share
-  // their angles (one row to a thread, 64064 rows of keys and values 15.4 us for 13.4).
+  // 64064 rows 17.4 -> 19.0), from 128 MiB on streaming loads (2 million rows 540 -> 504 with both), and streaming stores of
+  // codes that the 256 MiB behind the L2s do not hold for the next reader either.  Packed and unpacked with plain stores /
+  // streaming ones, 8 heads of 128: 384 documents of 512 rows (204 MiB of codes) 345 / 348, 448 (238) 384 / 414, 480 (255)
+  // 423 / 444, 496 (264) 463 / 459, 512 (272) 495 / 475, 640 (340) 635 / 611; 64 dims: 960 documents (255) 409 / 442, 1024
+  // (272) 500 / 475.  (Packing alone gains from 192 documents on, 88 / 82, 512 245 / 221, but what is packed is read.)  Keys to
+  // be turned have four rows to a thread at any size, which share their angles (one row to a thread, 64064 rows of keys and
+  // values 15.4 us for 13.4).
   const int n_tensors = a.x[0] != nullptr && a.x[1] != nullptr ? 2 : 1;
   const bool many = rotate || a.n_rows >= 131072;
-  const long long bytes = a.n_rows * dm.d * 2 * n_tensors;
+  const long long bytes = a.n_rows * dm.d * 2 * n_tensors, codes = a.n_rows * (dm.d / 2 + dm.d / 32) * n_tensors;
   const dim3 grid(stream_blocks(a.n_rows, 256 / (dm.d / 8) * (many ? 4 : 2)), n_tensors);
 #define MSA_PACK4(DD, RR, ROWS, SS) hipLaunchKernelGGL((pack4_kernel<DD, RR, ROWS, SS>), grid, dim3(256), 0, st, a, th)
 #define MSA_PACK4_MANY(DD, RR)                                 \
   do {                                                         \
-    if (bytes < kStreamBytes) MSA_PACK4(DD, RR, 4, 0);           \
-    else if (bytes < kStreamCodesBytes) MSA_PACK4(DD, RR, 4, 1); \
+    if (bytes < kStreamBytes) MSA_PACK4(DD, RR, 4, 0);         \
+    else if (codes < kStreamCodes) MSA_PACK4(DD, RR, 4, 1);    \
     else MSA_PACK4(DD, RR, 4, 2);                              \
   } while (0)
   if (dm.d == 128) {

@@ -170,3 +170,20 @@ def test_many_turned_keys_are_packed_as_few(N, Hkv, G, d):
     for i in (0, 1, N // 2, N - 2, N - 1):
         a4, a4s, _, _ = msa.msa_pack_kv4(_cfg(1, G, Hkv, d, rotated=0, lens=n[i:i + 1].contiguous()), K[i:i + 1], None)
         assert torch.equal(K4[i:i + 1], a4) and torch.equal(K4s[i:i + 1], a4s), i
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rotated, d, N, lens", [(1, 128, 4001, False), (0, 128, 3900, True), (1, 64, 7999, True), (0, 64, 7801, False)])
+def test_codes_past_the_caches_are_packed_as_few(rotated, d, N, lens):
+    """More than 256 MiB of codes are stored in another way: a document has the bits it gets alone, the last one too."""
+    G = 512
+    assert 2 * N * G * (d // 2 + d // 32) >= 256 << 20
+    g = torch.Generator(device="cuda").manual_seed(N)
+    K, V = (torch.randn((N, 1, G, d), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    n = torch.randint(1, G + 1, (N,), generator=g, device="cuda", dtype=torch.int32) if lens else None
+    bank = msa.msa_pack_kv4(_cfg(N, G, 1, d, rotated, n), K, V)
+    for i in (0, 1, 2, 3, N // 3, N // 2, N - 2, N - 1):
+        alone = msa.msa_pack_kv4(_cfg(1, G, 1, d, rotated, None if n is None else n[i:i + 1].contiguous()), K[i:i + 1], V[i:i + 1])
+        assert all(torch.equal(a[i:i + 1], b) for a, b in zip(bank, alone)), i
+    del bank, K, V
+    torch.cuda.empty_cache()
