@@ -179,9 +179,9 @@ class _Four:
         near = (Kl, Vl) if Kl.shape[2] else (None, None)
         return msa.msa_sparse_attend4(self.cfg, q, self.bank, idx, *near, self.pos0, q_pos, **kw)
 
-    def check(self, out, lse, weights, n=24):
+    def check(self, out, lse, weights, n=24, without=None):
         Hq, Hkv, d, B, M, k, G, L, scope, _ = self.case
-        at, r = _places(self.g, B, M, n), Hq // Hkv
+        at, r = [x for x in _places(self.g, B, M, n) if without is None or not without[x]], Hq // Hkv
         ref = P.Attended((len(at), Hq), d)
         for i, (b, m) in enumerate(at):
             near = torch.arange(L) + self.pos0 <= int(self.q_pos[b, m])
@@ -216,6 +216,21 @@ def test_selections_of_their_own_keep_pairs(plan, M):
     assert _attend4_parts(plan, *case[:8], pool=0) > 0
     f = _Four(case, pool=0)
     f.check(*f.call(workspace=f.ws), PAIRS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", [c for c in ATTEND4 if c[4] in (8, 9, 300, 700)], ids=str)
+def test_queries_that_are_no_numbers_stay_by_themselves(case):
+    """The padding of a batch holds anything; where its tokens see shared documents their own outputs do too, and no others."""
+    f = _Four(case)
+    B, M = case[3], case[4]
+    bad = torch.rand((B, M), generator=f.g) < 0.4
+    bad[0, 0], bad[-1, -1] = True, True
+    bad[0, 1] = bad[-1, 0] = bad[0, M - 1] = False
+    f.dev[0][bad.cuda()] = float("nan")
+    out, lse = f.call(workspace=f.ws)
+    assert bool(out.cpu()[~bad].isfinite().all()) and not bool(lse.cpu()[~bad].isnan().any())
+    f.check(out, lse, PAIRS if case[9] > 0 else SINGLE, without=bad)
 
 
 @pytest.mark.gpu
@@ -271,3 +286,57 @@ def test_single_token_offsets_past_32_bits():
     out, lse = msa.msa_sparse_attend4(cfg, q1.cuda(), bank, idx.cuda(), Kl.cuda(), Vl.cuda(), G, q_pos.cuda())
     kept = [P.unpack4(small[i].cpu(), small[i + 1].cpu()) for i in (0, 2)]
     P.sparse_attend4(q1.double(), *kept, idx - (N - 4), None, Kl.double(), Vl.double(), q_pos, G).check(out, lse, PAIRS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d, M", [(64, 1), (128, 2), (64, 5)])
+def test_a_captured_decode_step(d, M):
+    """One step of a program -- norms and append, a local layer, a routed layer, and the new document packed and unpacked -- captured
+    once and replayed for token after token, positions and projections changing between: the bits of the same steps run eagerly."""
+    B, Hq, Hkv, N, G, L, k = 3, 8, 2, 12, 24, 64, 4
+    g = torch.Generator().manual_seed(d + M)
+    cfg = msa.MsaConfig(N, G, 1, Hq, Hkv, d, 1e4, bank_keys_rotated=1, token_pool=int(M > 1))
+    K, V = (_normal(g, N, Hkv, G, d).cuda() for _ in range(2))
+    bank = msa.msa_pack_kv4(cfg, K, V)
+    idx = torch.randint(-1, N, (B, 1, Hkv, k), generator=g, dtype=torch.int32).cuda()
+    w = [(1 + 0.2 * torch.randn(d, generator=g)).to(torch.bfloat16).cuda() for _ in range(2)]
+    fused = torch.empty((B, M, Hq + 2 * Hkv, d), dtype=torch.bfloat16, device="cuda")
+    pos = torch.empty((B, M), dtype=torch.int32, device="cuda")
+
+    class Step:
+        def __init__(self):
+            self.Kl, self.Vl = (torch.full((B, Hkv, L, d), 0.5, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            self.q, self.a, self.b = (torch.empty((B, M, Hq, d), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+            self.la, self.lb = (torch.empty((B, M, Hq), dtype=torch.float32, device="cuda") for _ in range(2))
+            self.bank, self.back = tuple(t.clone() for t in bank), [torch.zeros_like(K) for _ in range(2)]
+            self.wa = torch.full((msa.window_attend_workspace_bytes(cfg, B, M, L, 20, 3),), 0xA5, dtype=torch.uint8, device="cuda")
+            self.wb = torch.full((msa.sparse_attend4_workspace_bytes(cfg, B, M, k, L),), 0xA5, dtype=torch.uint8, device="cuda")
+
+        def run(self):
+            msa.msa_norm_rotate(cfg, fused[:, :, :Hq], fused[:, :, Hq:Hq + Hkv], fused[:, :, Hq + Hkv:], pos, self.Kl, self.Vl, *w,
+                                local_pos0=G, q_out=self.q)
+            msa.msa_pack_kv4(cfg, K, V, N - 2, 2, self.bank)
+            msa.msa_window_attend(cfg, self.q, self.Kl, self.Vl, pos, 20, sinks=3, local_pos0=G, out=self.a, lse=self.la, workspace=self.wa)
+            msa.msa_sparse_attend4(cfg, self.q, self.bank, idx, self.Kl, self.Vl, G, pos, out=self.b, lse=self.lb, workspace=self.wb)
+            msa.msa_unpack_kv4(cfg, self.bank, N - 2, 2, *self.back)
+
+        def results(self):
+            return [self.Kl, self.Vl, self.q, self.a, self.la, self.b, self.lb, *self.bank, *self.back]
+
+    def feed(step):
+        fused.copy_(_normal(g, *fused.shape))
+        pos.copy_((G + step * M + torch.arange(M)).expand(B, M) - torch.arange(B)[:, None] * (step > 1))
+        K[N - 2:].copy_(_normal(g, 2, Hkv, G, d))
+
+    feed(0)
+    Step().run()                               # (warm)
+    torch.cuda.synchronize()
+    played, eager, graph = Step(), Step(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        played.run()
+    for step in range(6):
+        feed(step)
+        graph.replay()
+        eager.run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(played.results(), eager.results())), step
