@@ -367,8 +367,8 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
  * is the token at position local_pos0 + t; with p = q_pos[b][m] - local_pos0 token (b, m) sees the rows
  *     t <= p, t < Lloc, and (p - t < window or t < sinks)
  *     out[b][m][h][:] = softmax_t( q[b][m][h][:] . Kloc[b][g][t][:] / sqrt(d) ) . Vloc[b][g][t][:]
- *     lse[b][m][h]    = log sum_t exp( ... )        (natural log; -inf and out = 0 if no row is seen, as with q_pos < local_pos0:
- *                                                    the way to mark the padding of a batch)
+ *     lse[b][m][h]    = log sum_t exp( ... )        (natural log; -inf and out = 0 if no row is seen, as with q_pos <
+ *                                                    local_pos0: the way to mark the padding of a batch)
  * Positions may come in any order; tokens that the caller appends later lie behind q_pos and are not read.  A row up to the
  * largest position of a sequence's tokens holds numbers, seen or not; what rows behind it hold has no effect, nor has the
  * query of a token that sees none.  out and lse overlap no input.
@@ -382,8 +382,10 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
  *                  or sinks grow; contents undefined on entry/exit
  * B, n_kv_heads <= 65535; B * M <= 65535 for M < 32, from there on as many tokens as make 2^24 tiles of 128 (token, head)
  * pairs of a KV head; Lloc <= 2^28.
- * Scores, their maximum and sum and the outputs are accumulated in fp32.  With few tokens the softmax weights are carried as
- * bf16 (hi, lo) pairs, with many as bf16.  Reads n_q_heads, n_kv_heads and head_dim of cfg.
+ * Scores (within fp32's range), their maximum and sum and the outputs are accumulated in fp32.  Where a token is taken by itself
+ * the softmax weights are carried as bf16 (hi, lo) pairs; where tokens are taken together, from 32 of them on and from 4 where
+ * that is faster, as bf16: an output is then off by up to 2^-8 of the weighted mean of |v| more than its own rounding.
+ * Reads n_q_heads, n_kv_heads and head_dim of cfg.
  */
 size_t msa_window_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
                                          int32_t sinks);
@@ -398,9 +400,11 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *                                  [0, N), and every local row t < Lloc with local_pos0 + t <= q_pos[b][m]
  *     out, lse                     softmax over them with scale 1/sqrt(d), as in msa_sparse_attend
  * Selections, select_scope, token_pool, doc_lens, pads and documents listed twice are read as msa_sparse_attend reads them;
- * any doc_len is served; k * G <= 2^28, Lloc <= 2^28, and as many tokens as msa_window_attend takes where token_pool = 1, else
- * B * M <= 65535.  cfg->bank_keys_rotated is not read.  Local rows up to the largest position of a
+ * any doc_len is served; k * G <= 2^28, Lloc <= 2^28, B and n_kv_heads <= 65535, and as many tokens as msa_window_attend takes
+ * where token_pool = 1, else B * M <= 65535.  cfg->bank_keys_rotated is not read.  Local rows up to the largest position of a
  * sequence's tokens hold numbers.  out and lse overlap no input.
+ * Softmax weights as in msa_window_attend: pairs, but with token_pool = 1 bf16 from 32 tokens on, and from 8 where that is faster
+ * (msa_sparse_attend carries pairs everywhere).
  *   q         in   bf16 [B][M][Hq][d]
  *   K4, K4s, V4, V4s  in  as msa_pack_kv4 writes them
  *   idx       in   int32 [B][M'][S][k]
@@ -408,8 +412,9 @@ int msa_window_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *   q_pos     in   int32 [B][M]
  *   out       out  bf16 [B][M][Hq][d]
  *   lse       out  fp32 [B][M][Hq], may be NULL
- *   workspace      >= msa_sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), which does not fall as k or Lloc grows; where many tokens share a selection
- *                  (token_pool = 1) it holds the selected documents in bf16, B * Hkv * k * G * d * 4 bytes
+ *   workspace      >= msa_sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc), which does not fall as k or Lloc grows; where many
+ *                  tokens share a selection (token_pool = 1) it holds the selected documents in bf16, B * Hkv * k * G * d * 4
+ *                  bytes
  */
 size_t msa_sparse_attend4_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t k, int32_t Lloc);
 int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* K4, const void* K4s,

@@ -15,9 +15,11 @@ struct EncodedArgs {
   const int32_t* q_pos;    // [BM]
   uint16_t* out;           // [BM][Hq][D]
   float* lse;              // [BM][Hq] or null
-  float* part_o;           // [BM][Hq][n_splits][D] unnormalised partial outputs, where n_splits > 1 (tiled kernel with
-  float2* part_ml;         // [BM][Hq][n_splits]    (running max in log2 units, sum)      tickets: by workgroup, as registers hold them)
-  unsigned long long* tickets;  // arrival counters, one per (token, KV head) or, of two parts, (tile, KV head); null: a launch joins them
+  float* part_o;           // [BM][Hq][n_splits][D] unnormalised partial outputs, where n_splits > 1
+  float2* part_ml;         // [BM][Hq][n_splits]    (running max in log2 units, sum); tiled kernel with tickets: both by workgroup,
+                           // as registers hold them
+  unsigned long long* tickets;  // arrival counters, one per (token, KV head) or, of two parts, (tile, KV head); null: a launch
+                                // joins the parts
   unsigned long long nonce;
   int M, Hq, Hkv, r, G, k, N, Lloc, pos0, window, sinks;
   int idx_sel, idx_rows_per_b, n_splits;

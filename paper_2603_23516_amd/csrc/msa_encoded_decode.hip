@@ -14,9 +14,9 @@
 // by v_cvt_scalef32_pk_bf16_fp4, which applies the block's scale; the query's dims are laid out to match.
 // The workgroup that arrives last at a pair merges its splits.
 //
-// Bound by HBM: 40 tokens that see 4100 rows of 8 heads of 128 (672 MB) 103 us, 6.5 TB/s; 40 tokens of 16 documents in four bits and
-// 1800 rows in bf16 (474 MB) 75 us, 6.3 TB/s; 8 tokens of 32 documents (210 MB) 40 us, of which about 9 are the first loads and
-// the joins.  One token of 64 dims over 32 + 256 rows 5.8: the loads that wait for one another.  Two waves to a SIMD
+// Bound by HBM: 40 tokens that see 4100 rows of 8 heads of 128 (672 MB) 103 us, 6.5 TB/s; 40 tokens of 16 documents in four
+// bits and 1800 rows in bf16 (474 MB) 75 us, 6.3 TB/s; 8 tokens of 32 documents (210 MB) 40 us, of which about 9 are the first
+// loads and the joins.  One token of 64 dims over 32 + 256 rows 5.8: the loads that wait for one another.  Two waves to a SIMD
 // (registers for two sets of loads); eight waves to a workgroup, a second set for local rows, sixteen
 // parts at a time in the join and a launch of its own for it gave nothing or were slower.
 #include "msa_encoded.h"
@@ -371,9 +371,19 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   const long long pairs = (long long)B * M * dm.Hkv;
   // Tokens that share their rows go through the tiled kernel where the single-token kernel would take long over them: its steps
   // of all tokens (`work`; local ones count kLocalCost) against what the tiled kernel's launches, its thin tiles and the
-  // documents' expansion cost.  us, tiled / one by one, M tokens: 8 heads of 128 over 2048 rows, M = 4 12 / 14, 16 14 / 22;
-  // 8 sequences over 4096 rows, M = 2 40 / 36, 4 40 / 63, 8 31 / 115; heads of 64 that share nothing (r = 1) over 2048 rows,
-  // M = 8 14 / 11, 16 14 / 14; 16 documents of 512, M = 4 40 / 17, 16 39 / 33; 3 times 8 of 64, M = 8 20 / 16, 16 22 / 25.
+  // documents' expansion cost.  us in a graph, tiled / one by one, M tokens; 8 KV heads of 128, r = 4, if nothing else is said:
+  //   a window of 2048                               M = 8 17 / 14, 12 18 / 19, 16 18 / 21, 24 19 / 35
+  //   2 sequences, 4096                              M = 3 24 / 20, 4 24 / 22, 6 24 / 30, 8 24 / 35
+  //   8 sequences, 4096                              M = 2 48 / 39, 3 49 / 66, 4 50 / 65, 6 39 / 97, 8 40 / 118
+  //   32768                                          M = 2 54 / 38, 3 57 / 58, 4 57 / 68
+  //   4 sequences, 512, 4 KV heads, r = 8            M = 16 16 / 12, 24 16 / 19
+  //   2048, 64 dims, r = 1                           M = 12 14 / 12, 16 14 / 13, 24 14 / 20
+  //   16 documents of 512, 512 local rows            M = 12 37 / 29, 16 38 / 34, 24 39 / 53
+  //   8 sequences, 16 documents of 512, 2048 local   M = 6 145 / 116, 8 145 / 130, 12 148 / 210
+  //   3 sequences, 8 documents of 64, 512 local      M = 8 21 / 17, 12 22 / 25, 16 22 / 25
+  //   8 sequences, 32 documents of 8, 2048 local     M = 6 31 / 66, 8 31 / 66, 16 35 / 129
+  // The border is off by up to an eighth on its tiled side and a fifth on the other; 3 tokens of many sequences, and 3 to 7 tokens
+  // with few documents beside a long context, go one by one though tiles would take half to four fifths of the time.
   // (More rows never lead back to the single-token kernel: both sides count them in whole steps, M of them on the left and 8 on
   // the right, which applies from M = 8 on.)
   const long long steps_mem = (mem_rows + 31) / 32, cost = steps_mem + kLocalCost * ((local_rows + 31) / 32);

@@ -8,15 +8,20 @@
 //             16-byte pieces placed so that the reads below meet no bank twice
 //   scores    S^T[32 keys][32 cols] = K q^T with v_mfma_f32_32x32x16_bf16; the queries stay in registers
 //   softmax   online, per column (16 keys in a lane, the other 16 in lane ^ 32)
-//   product   O^T[dd][col] += V^T[dd][key] P^T[key][col], the weights in bf16 (each is off by 2^-8 of itself
-//             at most, either way, and the output by what that comes to; their sum is taken before the rounding), V^T by transposing LDS reads
+//   product   O^T[dd][col] += V^T[dd][key] P^T[key][col], the weights in bf16, V^T by transposing LDS reads
+// A weight in bf16 is off by 2^-8 of itself at most, either way, and the output by what that comes to; their sum is taken before
+// the rounding.  As (hi, lo) pairs, as the single-token kernel carries them at no cost, they would take the second product twice:
+// relative error against 64 bits 0.0023 -> 0.0017 (what rounding the output costs by itself), window_prefill 407 -> 535 us,
+// window_chunk_64 25 -> 28, attend4_question 168 -> 211.
 // Masks are worked out only in steps that some column of the wave does not see whole; steps that a wave does not see at all
 // are passed over.
 //
-// 8192 tokens of 32 / 8 heads of 128, window 4096 (413 GFLOP) 391 to 430 us by card, 0.96 to 1.05 PFLOP/s, where a product of
-// 8192^3 by the library runs at 1.21.  The matrix pipe is busy 58 % of the time and the vector ALU 61 %: maximum,
-// exponentials and rounding of 32 x 32 weights take 7.3 instructions per product, the two meet in one issue slot, and the chip
-// lowers its clock to 1.7 .. 1.9 GHz under both.  Three workgroups of four waves on a CU, 32 columns to a wave, was the best shape;
+// 8192 tokens of 32 / 8 heads of 128, window 4096 (413 GFLOP) 391 to 430 us by card with other work between the calls, 0.96 to
+// 1.05 PFLOP/s, and up to 494 us, 0.84, back to back on a card that has warmed up; a product of 8192^3 by the library runs at 1.21.
+// The matrix pipe is busy 58 % of the time and the vector ALU 61 %: maximum, exponentials and rounding of 32 x 32 weights take 7.3
+// instructions per product, the two meet in one issue slot, and the chip lowers its clock to 1.7 .. 1.9 GHz under both.  1000
+// tokens over 16 documents of 512 rows: 165 to 184 us behind 11 of expansion.  Three workgroups of four waves on a CU, 32 columns
+// to a wave, was the best shape;
 // each at its time, against what it would have replaced: 64 columns to a wave, half of the LDS reads, 859 us for 492; eight
 // waves to a workgroup 565 for 492; the scores a step ahead of their weights 457 for 392; a raised wave priority around
 // the products slower.

@@ -7,10 +7,10 @@
 // to nearest, ties to even), the same on every machine.  e stays in 2 .. 252, where every value is a normal bf16 number;
 // beyond 2^125 * 6 values saturate.
 //
-// Both are streams: 2 bytes read and 0.53 written per element, or the other way round; bound by HBM (2 million rows of 128 dims, K and
-// V, 1.36 GB: packed in 220 us, 6.2 TB/s, unpacked in 257, 5.3 TB/s).  Rows that are unpacked are stored with the streaming hint
-// (262144 rows packed and unpacked 56.8 -> 52.5 us, 64064 rows 18.1 -> 16.4).  A lane takes eight elements (one 16-byte access in
-// bf16, 4 bytes of codes); the block's maximum comes from the quad of lanes that share it.
+// Both are streams: 2 bytes read and 0.53 written per element, or the other way round; bound by HBM (2 million rows of 128
+// dims, K and V, 1.36 GB: packed in 221 us, 6.2 TB/s, unpacked in 257, 5.3 TB/s).  Rows that are unpacked are stored with the
+// streaming hint (262144 rows packed and unpacked 56.8 -> 52.5 us, 64064 rows 18.1 -> 16.4).  A lane takes eight elements (one
+// 16-byte access in bf16, 4 bytes of codes); the block's maximum comes from the quad of lanes that share it.
 #include "msa_attend.h"
 
 namespace msa {
@@ -53,9 +53,9 @@ __device__ __forceinline__ void pack4_eight(const float (&f)[8], uint8_t* __rest
   if ((lr & 3) == 0) scales[row * (D / 32) + lr / 4] = (uint8_t)e;
 }
 
-// ROT: keys that are not position-encoded yet are turned by their position in the document before they are rounded.  The angles
-// cost more than the bytes (each element its own: 2 million rows of keys and values 380 us, of one position in four documents or
-// heads 237, nothing turned 220).
+// ROT: keys that are not position-encoded yet are turned by their position in the document before they are rounded.  The
+// angles cost more than the bytes (2 million rows of keys and values, each row with angles of its own 380 us, rows of one
+// position in four documents or heads together 236 to 264, nothing turned 221).
 // A thread has ROWS rows in flight.  STREAM: 1 streaming loads, 2 streaming stores of the codes as well.
 template <int D, bool ROT, int ROWS, int STREAM>
 __device__ __forceinline__ void pack4_rows(const uint16_t* __restrict__ X, uint8_t* __restrict__ codes,

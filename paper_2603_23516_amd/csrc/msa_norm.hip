@@ -131,8 +131,9 @@ int launch_norm_rotate(const Dims& dm, NormArgs a, hipStream_t st) {
   for (int u = 0; u < kMaxHalf; ++u) th.th[u] = table.th[u];
   const long long blocks = (a.BM * a.shares + 3) / 4;
   // Projections that the caches do not hold: streaming loads.  us for 48 heads of 128, with plain loads / streaming ones, inputs
-  // changing from call to call and, in brackets, right behind the product that wrote the projection: 16384 tokens (201 MB) 81.7 / 74.7
-  // [85.6 / 70.0], 12288 63.4 / 57.5 [65.7 / 54.5], 8192 (101 MB) 43.9 / 39.6 [34.4 / 34.6], 4096 17.8 / 22.0 [19.7 / 20.0].
+  // changing from call to call and, in brackets, right behind the product that wrote the projection: 16384 tokens (201 MB)
+  // 81.7 / 74.7 [85.6 / 70.0], 12288 63.4 / 57.5 [65.7 / 54.5], 8192 (101 MB) 43.9 / 39.6 [34.4 / 34.6], 4096 17.8 / 22.0
+  // [19.7 / 20.0].
   const int heads = (a.q != nullptr ? dm.Hq : 0) + (a.k != nullptr ? dm.Hkv : 0) + (a.v != nullptr ? dm.Hkv : 0);
   const bool stream = a.BM * heads * dm.d * 2 >= (128ll << 20);
 #define MSA_NORM(DD, SS) hipLaunchKernelGGL((norm_rotate_kernel<DD, SS>), dim3((unsigned)blocks), dim3(256), 0, st, a, th)
