@@ -18,6 +18,11 @@
  *   msa_window_attend       attention over the local cache (window and first tokens), for layers that do not route
  *   msa_pack_kv4            offline: a bank in four bits, 0.27 of its bytes (msa_unpack_kv4 back)
  *   msa_sparse_attend4      msa_sparse_attend over that bank
+ * and for a local cache that is served from for long:
+ *   msa_norm_rotate_axes    msa_norm_rotate with positions of several axes and rows told apart from positions
+ *   msa_prefix_attend       attention of a batch over a prefix that its sequences share and over their own caches
+ *   msa_attend_mass         the attention weight that every row of the cache receives
+ *   msa_evict               the rows that weigh most kept, the others dropped
  *
  * Notation: N documents, G tokens per document, P chunk size, C = G/P chunks per document,
  * Hq query heads, Hkv key/value heads, r = Hq/Hkv, d head dimension, B sequences, M query tokens per
@@ -64,6 +69,7 @@ typedef enum msa_status {
 enum { MSA_SIM_DOT = 0, MSA_SIM_COS = 1 };
 enum { MSA_SCOPE_GROUP = 0, MSA_SCOPE_ALL = 1 };
 enum { MSA_MAX_TOPK = 64 };
+enum { MSA_MAX_AXES = 4 };
 
 typedef struct msa_config {
   int32_t n_docs;       /* N >= 1                                                                  */
@@ -421,6 +427,103 @@ int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_
                        const void* V4, const void* V4s, const int32_t* idx, int32_t k, const void* Kloc, const void* Vloc,
                        int32_t Lloc, int32_t local_pos0, const int32_t* q_pos, void* out, float* lse, void* workspace,
                        size_t workspace_bytes, msa_stream_t stream);
+
+/*
+ * msa_norm_rotate for positions of several axes (time, height and width of images and video beside text), and for a cache
+ * whose rows are told apart from positions: after msa_evict, or where tokens share a position.  As msa_norm_rotate, but
+ *     pair (u, u + d/2) of a head is turned by pos[b][m][axes[u]] * base^(-2u/d)
+ *     key and value go into row rows[b][m], or without rows into row pos[b][m][0] - local_pos0
+ * A token whose first position is negative is padding, nothing of it is written (its other positions are not read); the other
+ * tokens' positions may have any sign on the further axes.  A row outside [0, Lloc) is none: the query alone is written.  Of a
+ * row that two tokens claim the contents are undefined.
+ *   pos       in   int32 [B][M][n_axes], 1 <= n_axes <= MSA_MAX_AXES
+ *   axes      in   HOST int32 [d/2], each in [0, n_axes); read before the call returns
+ *   rows      in   int32 [B][M], may be NULL
+ */
+int msa_norm_rotate_axes(const msa_config_t* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                         int32_t rotate, const int32_t* pos, int32_t n_axes, const int32_t* axes, const int32_t* rows,
+                         int32_t B, int32_t M, void* q_out, void* Kloc, void* Vloc, int32_t Lloc, int32_t local_pos0,
+                         msa_stream_t stream);
+
+/*
+ * Attention of a batch whose sequences share a prefix (an instruction, a document): one softmax over the prefix' rows, which
+ * are held and read once for all, and the rows of a sequence's own cache.  Queries and keys carry their positions.  Token
+ * (b, m) sees
+ *     prefix rows t < prefix_lens[b] (clamped to [0, Lpre]; all Lpre with prefix_lens == NULL)
+ *     cache rows t < Lloc with local_pos0 + t <= q_pos[b][m]
+ *     out[b][m][h][:] = softmax( q[b][m][h][:] . key / sqrt(d) ) . value
+ *     lse[b][m][h]    = log sum exp( ... )       (natural log; -inf and out = 0 if nothing is seen)
+ * so a token with q_pos < local_pos0 (padding of a batch) sees the prefix alone.  Of the prefix the rows up to the largest of
+ * prefix_lens hold numbers, of a cache the rows up to the largest position of its tokens; rows behind them have no effect.
+ * out and lse overlap no input.
+ *   q           in   bf16 [B][M][Hq][d]
+ *   Kpre, Vpre  in   bf16 [Hkv][Lpre][d]; may be NULL iff Lpre == 0
+ *   prefix_lens in   int32 [B], may be NULL
+ *   Kloc, Vloc  in   bf16 [B][Hkv][Lloc][d]; may be NULL iff Lloc == 0 (not both lengths are 0)
+ *   q_pos       in   int32 [B][M]
+ *   out         out  bf16 [B][M][Hq][d]
+ *   lse         out  fp32 [B][M][Hq], may be NULL
+ *   workspace        >= msa_prefix_attend_workspace_bytes(cfg, B, M, Lpre, Lloc), which does not fall as Lpre or Lloc grows;
+ *                    contents undefined on entry/exit
+ * B, n_kv_heads <= 65535, B * M <= 2^25, Lpre, Lloc <= 2^28.  Scores, their maximum and sum and the outputs are accumulated in
+ * fp32; the softmax weights are rounded to bf16 for the second product (2^-8 relative).
+ */
+size_t msa_prefix_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lpre, int32_t Lloc);
+int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kpre, const void* Vpre,
+                      int32_t Lpre, const int32_t* prefix_lens, const void* Kloc, const void* Vloc, int32_t Lloc,
+                      int32_t local_pos0, const int32_t* q_pos, void* out, float* lse, void* workspace,
+                      size_t workspace_bytes, msa_stream_t stream);
+
+/*
+ * The attention weight that every row of the local cache receives from the tokens of a call, added to what it has: what
+ * msa_evict goes by.  Token (b, m) sees the rows that msa_window_attend shows it for this window, sinks, local_pos0 and q_pos
+ * (window = Lloc or more: the cache rows that msa_prefix_attend and msa_sparse_attend4 show it), and with lse as the attention
+ * over them, and over whatever else was in its softmax, left it
+ *     mass_out[b][g][t] = decay * mass[b][g][t] + sum over the tokens m that see row t and the heads h of group g of
+ *                         exp( q[b][m][h][:] . Kloc[b][g][t][:] / sqrt(d) - lse[b][m][h] )
+ * in fp32.  decay == 0, or mass == NULL: nothing of mass is read.  Every entry of mass_out is written, those of rows that no
+ * token sees with decay * mass, 0 without it; in place with decay == 1 they are left as they are.  A token whose lse is -inf
+ * (it saw nothing) adds nothing.  The same bits from call to call.  mass_out is mass itself or overlaps no input.
+ *   q         in   bf16 [B][M][Hq][d]
+ *   Kloc      in   bf16 [B][Hkv][Lloc][d]; rows up to the largest position of a sequence's tokens hold numbers
+ *   q_pos     in   int32 [B][M]
+ *   lse       in   fp32 [B][M][Hq]
+ *   mass      in   fp32 [B][Hkv][Lloc], may be NULL
+ *   decay          0 to 1
+ *   mass_out  out  fp32 [B][Hkv][Lloc]
+ *   workspace      >= msa_attend_mass_workspace_bytes(cfg, B, M, Lloc, window, sinks); contents undefined on entry/exit
+ * B, n_kv_heads <= 65535, B * M <= 2^25, Lloc <= 2^28.
+ */
+size_t msa_attend_mass_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
+                                       int32_t sinks);
+int msa_attend_mass(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kloc, int32_t Lloc,
+                    int32_t local_pos0, int32_t window, int32_t sinks, const int32_t* q_pos, const float* lse,
+                    const float* mass, float decay, float* mass_out, void* workspace, size_t workspace_bytes,
+                    msa_stream_t stream);
+
+/*
+ * The local cache cut down to `keep` rows per (sequence, KV head), each head by weights of its own.  Sequence b holds rows
+ * 0 .. n - 1, n = lens[b] (clamped to [0, Lloc]).  Where n <= keep all of them stay.  Else the first `sinks` rows stay, the last
+ * `recent` ones, and of the rows between them the keep - sinks - recent that weigh most (of equal weights the lowest row; -0 and
+ * 0 are equal; what is no number weighs least, less than -inf).  Rows keep their order: with rows[b][g][0] < rows[b][g][1] < ...
+ *     Kout[b][g][j][:] = Kloc[b][g][rows[b][g][j]][:], Vout and mass_out alike,      j < min(n, keep)
+ *     rows[b][g][j]    = -1 for j >= n
+ *     mass_out[b][g][j] = 0 for j >= min(n, keep): a row that is appended there begins without weight
+ * Rows of Kout and Vout from min(n, keep) on are left as they are.  The caller's new lengths are min(lens, keep).
+ *   Kloc,Vloc   in   bf16 [B][Hkv][Lloc][d]
+ *   mass        in   fp32 [B][Hkv][Lloc]
+ *   lens        in   int32 [B]
+ *   keep             1 to Lout; sinks + recent <= keep
+ *   Kout, Vout  out  bf16 [B][Hkv][Lout][d]
+ *   mass_out    out  fp32 [B][Hkv][Lout]
+ *   rows        out  int32 [B][Hkv][keep]
+ * In place where Kout, Vout and mass_out are Kloc, Vloc and mass (all three, Lout == Lloc); else the outputs overlap no input.
+ * B * n_kv_heads <= 2^16, Lloc, Lout <= 2^28, B * n_kv_heads * keep <= 2^29.
+ */
+int msa_evict(const msa_config_t* cfg, const void* Kloc, const void* Vloc, const float* mass, const int32_t* lens, int32_t B,
+              int32_t Lloc, int32_t keep, int32_t sinks, int32_t recent, void* Kout, void* Vout, float* mass_out,
+              int32_t Lout, int32_t* rows, msa_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -14,6 +14,7 @@ LIB_PATH = os.path.join(_HERE, "libmsa.so")
 MSA_SIM_DOT, MSA_SIM_COS = 0, 1
 MSA_SCOPE_GROUP, MSA_SCOPE_ALL = 0, 1
 MSA_MAX_TOPK = 64
+MSA_MAX_AXES = 4
 MSA_OK, MSA_ERR_INVALID_ARG, MSA_ERR_UNSUPPORTED, MSA_ERR_WORKSPACE, MSA_ERR_MISALIGNED, MSA_ERR_HIP = \
     0, -1, -2, -3, -4, -5
 
@@ -23,7 +24,9 @@ EXPORTS = ("msa_version", "msa_status_string", "msa_routing_keys_bytes", "msa_in
            "msa_sparse_attend", "msa_fetch_slots", "msa_fetch_selected",
            "msa_noalloc_scratch_bytes", "msa_score_topk_noalloc", "msa_layers_step", "msa_norm_rotate", "msa_pack_kv4",
            "msa_unpack_kv4", "msa_window_attend_workspace_bytes", "msa_window_attend",
-           "msa_sparse_attend4_workspace_bytes", "msa_sparse_attend4")
+           "msa_sparse_attend4_workspace_bytes", "msa_sparse_attend4", "msa_norm_rotate_axes",
+           "msa_prefix_attend_workspace_bytes", "msa_prefix_attend", "msa_attend_mass_workspace_bytes", "msa_attend_mass",
+           "msa_evict")
 
 
 class MsaConfig(ctypes.Structure):
@@ -150,6 +153,19 @@ def load_library():
     lib.msa_sparse_attend4_workspace_bytes.argtypes = [cfgp] + [i32] * 4
     lib.msa_sparse_attend4.restype = ctypes.c_int
     lib.msa_sparse_attend4.argtypes = [cfgp, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.msa_norm_rotate_axes.restype = ctypes.c_int
+    lib.msa_norm_rotate_axes.argtypes = [cfgp, vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_float, i32, vp, i32, vp, vp, i32,
+                                         i32, vp, vp, vp, i32, i32, vp]
+    lib.msa_prefix_attend_workspace_bytes.restype = sz
+    lib.msa_prefix_attend_workspace_bytes.argtypes = [cfgp] + [i32] * 4
+    lib.msa_prefix_attend.restype = ctypes.c_int
+    lib.msa_prefix_attend.argtypes = [cfgp, vp, i32, i32, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.msa_attend_mass_workspace_bytes.restype = sz
+    lib.msa_attend_mass_workspace_bytes.argtypes = [cfgp] + [i32] * 5
+    lib.msa_attend_mass.restype = ctypes.c_int
+    lib.msa_attend_mass.argtypes = [cfgp, vp, i32, i32, vp] + [i32] * 4 + [vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+    lib.msa_evict.restype = ctypes.c_int
+    lib.msa_evict.argtypes = [cfgp, vp, vp, vp, vp] + [i32] * 5 + [vp, vp, vp, i32, vp, vp]
     _lib = lib
     return lib
 
@@ -439,20 +455,18 @@ def _tokens_at(t, B, M, heads, d, dev, name):
                      f"same distance apart, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()}, {t.device}")
 
 
-def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None, eps=1e-6, rotate=True, local_pos0=0,
-                    q_out=None, stream=None):
-    """q bf16 [B][M][Hq][d], k, v bf16 [B][M][Hkv][d] (views of a fused projection are read where they lie), pos int32
-    [B][M] -> q_out bf16 [B][M][Hq][d]; keys and values go into rows pos - local_pos0 of Kloc, Vloc bf16
-    [B][Hkv][Lloc][d].  q, or k with Kloc, or v with Vloc, may be None.  Weights bf16 [d], None for no norm."""
+def _norm_tensors(cfg, name, q, k, v, Kloc, Vloc, q_weight, k_weight, q_out, stream):
+    """What msa_norm_rotate and msa_norm_rotate_axes check alike -> (device, B, M, q_out, the arguments up to the weights, q_out,
+    Kloc, Vloc, Lloc)."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     if (k is None) != (Kloc is None) or (v is None) != (Vloc is None) or (q is None and q_out is not None):
-        raise ValueError("msa_norm_rotate: k comes with Kloc, v with Vloc, q_out with q")
+        raise ValueError(f"{name}: k comes with Kloc, v with Vloc, q_out with q")
     src = q if q is not None else k if k is not None else v
     if src is None or src.dim() != 4:
-        raise ValueError("msa_norm_rotate: expected q, k or v as [B][M][heads][d]")
+        raise ValueError(f"{name}: expected q, k or v as [B][M][heads][d]")
     if (Kloc is not None and Kloc.dim() != 4) or (Vloc is not None and Vloc.dim() != 4):
-        raise ValueError("msa_norm_rotate: expected Kloc and Vloc as [B][Hkv][Lloc][d]")
-    dev = _gpu(src, "msa_norm_rotate")
+        raise ValueError(f"{name}: expected Kloc and Vloc as [B][Hkv][Lloc][d]")
+    dev = _gpu(src, name)
     B, M = src.shape[:2]
     qa = ka = va = qo = Ka = Va = None
     qs = ks = vs = Lloc = 0
@@ -470,10 +484,55 @@ def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None,
         if k is None:
             Lloc = Vloc.shape[2]
         Va = _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc")
-    _call("msa_norm_rotate", dev, stream, ctypes.byref(cfg), qa, qs, ka, ks, va, vs,
-          None if q_weight is None else _at(q_weight, _BF16, (d,), dev, "q_weight"),
-          None if k_weight is None else _at(k_weight, _BF16, (d,), dev, "k_weight"), eps, 1 if rotate else 0,
+    return dev, B, M, q_out, (qa, qs, ka, ks, va, vs, None if q_weight is None else _at(q_weight, _BF16, (d,), dev, "q_weight"),
+                              None if k_weight is None else _at(k_weight, _BF16, (d,), dev, "k_weight")), qo, Ka, Va, Lloc
+
+
+def msa_norm_rotate(cfg, q, k, v, pos, Kloc, Vloc, q_weight=None, k_weight=None, eps=1e-6, rotate=True, local_pos0=0,
+                    q_out=None, stream=None):
+    """q bf16 [B][M][Hq][d], k, v bf16 [B][M][Hkv][d] (views of a fused projection are read where they lie), pos int32
+    [B][M] -> q_out bf16 [B][M][Hq][d]; keys and values go into rows pos - local_pos0 of Kloc, Vloc bf16
+    [B][Hkv][Lloc][d].  q, or k with Kloc, or v with Vloc, may be None.  Weights bf16 [d], None for no norm."""
+    dev, B, M, q_out, tokens, qo, Ka, Va, Lloc = _norm_tensors(cfg, "msa_norm_rotate", q, k, v, Kloc, Vloc, q_weight, k_weight,
+                                                               q_out, stream)
+    _call("msa_norm_rotate", dev, stream, ctypes.byref(cfg), *tokens, eps, 1 if rotate else 0,
           _at(pos, _I32, (B, M), dev, "pos"), B, M, qo, Ka, Va, Lloc, _i32(local_pos0, "local_pos0"))
+    return q_out
+
+
+_axes_arrays = {}
+
+
+def _axes_array(axes, half):
+    """A host array of the axis of every pair; the last ones asked for are kept (a model has one, and building it takes longer
+    than the call)."""
+    key = tuple(axes)
+    arr = _axes_arrays.get(key)
+    if arr is None:
+        if not all(isinstance(x, int) and 0 <= x < MSA_MAX_AXES for x in key):
+            raise ValueError(f"axes: expected integers in [0, {MSA_MAX_AXES}), got {key}")
+        if len(_axes_arrays) >= 64:
+            _axes_arrays.clear()
+        arr = _axes_arrays[key] = (ctypes.c_int32 * len(key))(*key)
+    if len(key) != half:
+        raise ValueError(f"axes: expected the axis of every one of {half} pairs, got {len(key)}")
+    return arr
+
+
+def msa_norm_rotate_axes(cfg, q, k, v, pos, axes, Kloc, Vloc, rows=None, q_weight=None, k_weight=None, eps=1e-6, rotate=True,
+                         local_pos0=0, q_out=None, stream=None):
+    """msa_norm_rotate with positions of several axes: pos int32 [B][M][A], pair u of a head turned by the position of axis
+    axes[u] (d/2 integers).  Keys and values go into rows rows[b][m] (int32 [B][M]) of Kloc, Vloc, None: pos[b][m][0] -
+    local_pos0."""
+    if pos.dim() != 3:
+        raise ValueError("msa_norm_rotate_axes: expected pos [B][M][A]")
+    A = pos.shape[2]
+    dev, B, M, q_out, tokens, qo, Ka, Va, Lloc = _norm_tensors(cfg, "msa_norm_rotate_axes", q, k, v, Kloc, Vloc, q_weight,
+                                                               k_weight, q_out, stream)
+    _call("msa_norm_rotate_axes", dev, stream, ctypes.byref(cfg), *tokens, eps, 1 if rotate else 0,
+          _at(pos, _I32, (B, M, A), dev, "pos"), A, _axes_array(axes, cfg.head_dim // 2),
+          None if rows is None else _at(rows, _I32, (B, M), dev, "rows"), B, M, qo, Ka, Va, Lloc,
+          _i32(local_pos0, "local_pos0"))
     return q_out
 
 
@@ -619,3 +678,95 @@ def msa_sparse_attend4(cfg, q, bank, idx, Kloc, Vloc, local_pos0, q_pos, out=Non
           _at(q_pos, _I32, (B, M), dev, "q_pos"), _at(out, _BF16, (B, M, Hq, d), dev, "out"),
           _at(lse, _F32, (B, M, Hq), dev, "lse"), _workspace_at(workspace, dev), workspace.numel())
     return out, lse
+
+
+# ---- a local cache that is served from for long --------------------------------------------------------------------------
+def prefix_attend_workspace_bytes(cfg, B, M, Lpre, Lloc):
+    return load_library().msa_prefix_attend_workspace_bytes(ctypes.byref(cfg), _i32(B, "B"), _i32(M, "M"), _i32(Lpre, "Lpre"),
+                                                            _i32(Lloc, "Lloc"))
+
+
+def msa_prefix_attend(cfg, q, Kpre, Vpre, Kloc, Vloc, q_pos, local_pos0=0, prefix_lens=None, out=None, lse=None,
+                      workspace=None, stream=None):
+    """q bf16 [B][M][Hq][d], Kpre, Vpre bf16 [Hkv][Lpre][d] shared by the sequences, Kloc, Vloc bf16 [B][Hkv][Lloc][d] their own
+    caches (either pair may be None), q_pos int32 [B][M] -> (out bf16 like q, lse fp32 [B][M][Hq]): attention over the prefix
+    (prefix_lens int32 [B]: so many rows of it) and the cache rows up to q_pos - local_pos0.  Queries and keys carry their
+    positions."""
+    Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    dev = _gpu(q, "q")
+    if q.dim() != 4 or (Kpre is not None and Kpre.dim() != 3) or (Kloc is not None and Kloc.dim() != 4):
+        raise ValueError("msa_prefix_attend: expected q [B][M][Hq][d], Kpre [Hkv][Lpre][d] and Kloc [B][Hkv][Lloc][d]")
+    if (Kpre is None) != (Vpre is None) or (Kloc is None) != (Vloc is None):
+        raise ValueError("msa_prefix_attend: keys come with their values")
+    B, M = q.shape[:2]
+    Lpre, Kp, Vp, Lloc, Ka, Va = 0, None, None, 0, None, None
+    if Kpre is not None:
+        Lpre = Kpre.shape[1]
+        Kp, Vp = _at(Kpre, _BF16, (Hkv, Lpre, d), dev, "Kpre"), _at(Vpre, _BF16, (Hkv, Lpre, d), dev, "Vpre")
+    if Kloc is not None:
+        Lloc = Kloc.shape[2]
+        Ka, Va = _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc")
+    if out is None:
+        out = _new((B, M, Hq, d), _BF16, q.device, stream)
+    if lse is None:
+        lse = _new((B, M, Hq), _F32, q.device, stream)
+    if workspace is None:
+        workspace = _new(max(prefix_attend_workspace_bytes(cfg, B, M, Lpre, Lloc), 256), _U8, q.device, stream)
+    _call("msa_prefix_attend", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M, Kp, Vp, Lpre,
+          None if prefix_lens is None else _at(prefix_lens, _I32, (B,), dev, "prefix_lens"), Ka, Va, Lloc,
+          _i32(local_pos0, "local_pos0"), _at(q_pos, _I32, (B, M), dev, "q_pos"), _at(out, _BF16, (B, M, Hq, d), dev, "out"),
+          _at(lse, _F32, (B, M, Hq), dev, "lse"), _workspace_at(workspace, dev), workspace.numel())
+    return out, lse
+
+
+def attend_mass_workspace_bytes(cfg, B, M, Lloc, window, sinks=0):
+    return load_library().msa_attend_mass_workspace_bytes(ctypes.byref(cfg), _i32(B, "B"), _i32(M, "M"), _i32(Lloc, "Lloc"),
+                                                          _i32(min(window, _MOST), "window"),
+                                                          _i32(min(sinks, _MOST), "sinks"))
+
+
+def msa_attend_mass(cfg, q, Kloc, lse, q_pos, window, sinks=0, local_pos0=0, mass=None, decay=1.0, out=None, workspace=None,
+                    stream=None):
+    """q bf16 [B][M][Hq][d], Kloc bf16 [B][Hkv][Lloc][d], lse fp32 [B][M][Hq] as an attention over them left it, q_pos int32
+    [B][M] -> out fp32 [B][Hkv][Lloc] = decay * mass + the attention weights that every row receives (window, sinks: of
+    msa_window_attend).  out may be mass."""
+    Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    dev = _gpu(q, "q")
+    window, sinks = _i32(min(window, _MOST), "window"), _i32(min(sinks, _MOST), "sinks")
+    if q.dim() != 4 or Kloc.dim() != 4:
+        raise ValueError("msa_attend_mass: expected q [B][M][Hq][d] and Kloc [B][Hkv][Lloc][d]")
+    B, M, Lloc = q.shape[0], q.shape[1], Kloc.shape[2]
+    if out is None:
+        out = _new((B, Hkv, Lloc), _F32, q.device, stream)
+    if workspace is None:
+        workspace = _new(max(attend_mass_workspace_bytes(cfg, B, M, Lloc, window, sinks), 256), _U8, q.device, stream)
+    _call("msa_attend_mass", dev, stream, ctypes.byref(cfg), _at(q, _BF16, (B, M, Hq, d), dev, "q"), B, M,
+          _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"), Lloc, _i32(local_pos0, "local_pos0"), window, sinks,
+          _at(q_pos, _I32, (B, M), dev, "q_pos"), _at(lse, _F32, (B, M, Hq), dev, "lse"),
+          None if mass is None else _at(mass, _F32, (B, Hkv, Lloc), dev, "mass"), decay,
+          _at(out, _F32, (B, Hkv, Lloc), dev, "out"), _workspace_at(workspace, dev), workspace.numel())
+    return out
+
+
+def msa_evict(cfg, Kloc, Vloc, mass, lens, keep, sinks=0, recent=0, Kout=None, Vout=None, mass_out=None, rows=None, stream=None):
+    """Kloc, Vloc bf16 [B][Hkv][Lloc][d] with lens int32 [B] rows each, mass fp32 [B][Hkv][Lloc]: per KV head the first `sinks`
+    rows, the last `recent` and the heaviest of the others stay, `keep` in all -> (Kout, Vout, mass_out, rows int32
+    [B][Hkv][keep]).  In place without Kout, Vout and mass_out, which come together ([B][Hkv][Lout]..., Lout >= keep)."""
+    Hkv, d = cfg.n_kv_heads, cfg.head_dim
+    dev = _gpu(Kloc, "Kloc")
+    if Kloc.dim() != 4 or (Kout is not None and Kout.dim() != 4):
+        raise ValueError("msa_evict: expected Kloc and Kout as [B][Hkv][Lloc][d]")
+    if (Kout is None) != (Vout is None) or (Kout is None) != (mass_out is None):
+        raise ValueError("msa_evict: Kout, Vout and mass_out come together")
+    if Kout is None:
+        Kout, Vout, mass_out = Kloc, Vloc, mass
+    B, Lloc, Lout = Kloc.shape[0], Kloc.shape[2], Kout.shape[2]
+    keep = _i32(keep, "keep")
+    if rows is None:
+        rows = _new((B, Hkv, max(keep, 0)), _I32, Kloc.device, stream)
+    _call("msa_evict", dev, stream, ctypes.byref(cfg), _at(Kloc, _BF16, (B, Hkv, Lloc, d), dev, "Kloc"),
+          _at(Vloc, _BF16, (B, Hkv, Lloc, d), dev, "Vloc"), _at(mass, _F32, (B, Hkv, Lloc), dev, "mass"),
+          _at(lens, _I32, (B,), dev, "lens"), B, Lloc, keep, _i32(sinks, "sinks"), _i32(recent, "recent"),
+          _at(Kout, _BF16, (B, Hkv, Lout, d), dev, "Kout"), _at(Vout, _BF16, (B, Hkv, Lout, d), dev, "Vout"),
+          _at(mass_out, _F32, (B, Hkv, Lout), dev, "mass_out"), Lout, _at(rows, _I32, (B, Hkv, max(keep, 0)), dev, "rows"))
+    return Kout, Vout, mass_out, rows

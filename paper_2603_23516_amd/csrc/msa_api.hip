@@ -1,6 +1,7 @@
 // C-ABI layer: argument validation (host only, before anything is enqueued), work plans, launches.
 #include "msa_encoded.h"
 #include "msa_host.h"
+#include "msa_prefix.h"
 
 #include <chrono>
 #include <mutex>
@@ -377,11 +378,12 @@ int msa_layers_step(const msa_config_t* cfg, const msa_config_t* attend_cfg, con
   return rc;
 }
 
-int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
-                    const void* v, int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
-                    int32_t rotate, const int32_t* pos, int32_t B, int32_t M, void* q_out, void* Kloc, void* Vloc,
-                    int32_t Lloc, int32_t local_pos0, msa_stream_t stream) {
-  Dims dm;
+// Everything that msa_norm_rotate and msa_norm_rotate_axes refuse alike, and their kernel's arguments.
+static int check_norm(const msa_config_t* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                      const void* v, int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                      int32_t rotate, const int32_t* pos, int32_t B, int32_t M, void* q_out, void* Kloc, void* Vloc,
+                      int32_t Lloc, int32_t local_pos0, Dims* out_dm, NormArgs* out_args) {
+  Dims& dm = *out_dm;
   const int rc = make_dims(cfg, &dm, kForAttend);
   if (rc != MSA_OK) return rc;
   if (pos == nullptr || (q == nullptr && k == nullptr && v == nullptr)) return MSA_ERR_INVALID_ARG;
@@ -397,7 +399,8 @@ int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, co
       misaligned(q_out) || misaligned(Kloc) || misaligned(Vloc) || misaligned4(pos) ||
       (q != nullptr && q_stride % 8 != 0) || (k != nullptr && k_stride % 8 != 0) || (v != nullptr && v_stride % 8 != 0))
     return MSA_ERR_MISALIGNED;
-  NormArgs a = {};
+  NormArgs& a = *out_args;
+  a = {};
   a.q = (const uint16_t*)q;
   a.k = (const uint16_t*)k;
   a.v = (const uint16_t*)v;
@@ -416,6 +419,40 @@ int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, co
   a.pos0 = local_pos0;
   a.rotate = rotate;
   a.eps = eps;
+  return MSA_OK;
+}
+
+int msa_norm_rotate(const msa_config_t* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const void* v, int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                    int32_t rotate, const int32_t* pos, int32_t B, int32_t M, void* q_out, void* Kloc, void* Vloc,
+                    int32_t Lloc, int32_t local_pos0, msa_stream_t stream) {
+  Dims dm;
+  NormArgs a;
+  const int rc = check_norm(cfg, q, q_stride, k, k_stride, v, v_stride, q_weight, k_weight, eps, rotate, pos, B, M, q_out,
+                            Kloc, Vloc, Lloc, local_pos0, &dm, &a);
+  if (rc != MSA_OK) return rc;
+  return launch_norm_rotate(dm, a, (hipStream_t)stream);
+}
+
+int msa_norm_rotate_axes(const msa_config_t* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, const void* q_weight, const void* k_weight, float eps,
+                         int32_t rotate, const int32_t* pos, int32_t n_axes, const int32_t* axes, const int32_t* rows,
+                         int32_t B, int32_t M, void* q_out, void* Kloc, void* Vloc, int32_t Lloc, int32_t local_pos0,
+                         msa_stream_t stream) {
+  Dims dm;
+  NormArgs a;
+  const int rc = check_norm(cfg, q, q_stride, k, k_stride, v, v_stride, q_weight, k_weight, eps, rotate, pos, B, M, q_out,
+                            Kloc, Vloc, Lloc, local_pos0, &dm, &a);
+  if (rc != MSA_OK) return rc;
+  if (n_axes < 1 || axes == nullptr) return MSA_ERR_INVALID_ARG;
+  if (n_axes > MSA_MAX_AXES) return MSA_ERR_UNSUPPORTED;
+  for (int u = 0; u < dm.d / 2; ++u) {
+    if (axes[u] < 0 || axes[u] >= n_axes) return MSA_ERR_INVALID_ARG;
+    a.axes[u / 32] |= (unsigned long long)axes[u] << (2 * (u % 32));
+  }
+  if (misaligned4(rows)) return MSA_ERR_MISALIGNED;
+  a.n_axes = n_axes;
+  a.rows = rows;
   return launch_norm_rotate(dm, a, (hipStream_t)stream);
 }
 
@@ -556,6 +593,127 @@ int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_
   a.window = INT32_MAX;
   a.sinks = 0;
   return launch_encoded(dm, pl, a, B, workspace, (hipStream_t)stream);
+}
+
+static int plan_prefix_of(const Dims& dm, int32_t B, int32_t M, int32_t Lpre, int32_t Lloc, PrefixPlan* pl) {
+  if (B < 1 || M < 1 || Lpre < 0 || Lloc < 0 || (Lpre == 0 && Lloc == 0)) return MSA_ERR_INVALID_ARG;
+  if (!encoded_sizes_ok(dm, B, M) || Lpre > (1 << 28) || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
+  *pl = plan_prefix(dm, B, M, Lpre, Lloc);
+  return pl->ws_bytes != 0 ? MSA_OK : MSA_ERR_UNSUPPORTED;
+}
+
+size_t msa_prefix_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lpre, int32_t Lloc) {
+  Dims dm;
+  PrefixPlan pl;
+  if (make_dims(cfg, &dm, kForAttend) != MSA_OK || plan_prefix_of(dm, B, M, Lpre, Lloc, &pl) != MSA_OK) return 0;
+  return pl.ws_bytes;
+}
+
+int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kpre, const void* Vpre,
+                      int32_t Lpre, const int32_t* prefix_lens, const void* Kloc, const void* Vloc, int32_t Lloc,
+                      int32_t local_pos0, const int32_t* q_pos, void* out, float* lse, void* workspace,
+                      size_t workspace_bytes, msa_stream_t stream) {
+  Dims dm;
+  PrefixPlan pl;
+  int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (q == nullptr || q_pos == nullptr || out == nullptr || workspace == nullptr || local_pos0 < 0) return MSA_ERR_INVALID_ARG;
+  if ((Lpre > 0 && (Kpre == nullptr || Vpre == nullptr)) || (Lloc > 0 && (Kloc == nullptr || Vloc == nullptr)))
+    return MSA_ERR_INVALID_ARG;
+  rc = plan_prefix_of(dm, B, M, Lpre, Lloc, &pl);
+  if (rc != MSA_OK) return rc;
+  if (misaligned(q) || misaligned(Kpre) || misaligned(Vpre) || misaligned4(prefix_lens) || misaligned(Kloc) ||
+      misaligned(Vloc) || misaligned4(q_pos) || misaligned(out) || misaligned4(lse) || misaligned(workspace))
+    return MSA_ERR_MISALIGNED;
+  if (workspace_bytes < pl.ws_bytes) return MSA_ERR_WORKSPACE;
+  PrefixArgs a = {};
+  a.q = (const uint16_t*)q;
+  a.Kpre = (const uint16_t*)Kpre;
+  a.Vpre = (const uint16_t*)Vpre;
+  a.pre_lens = prefix_lens;
+  a.Kloc = (const uint16_t*)Kloc;
+  a.Vloc = (const uint16_t*)Vloc;
+  a.q_pos = q_pos;
+  a.out = (uint16_t*)out;
+  a.lse = lse;
+  a.B = B;
+  a.M = M;
+  a.Lpre = Lpre;
+  a.Lloc = Lloc;
+  a.pos0 = local_pos0;
+  return launch_prefix(dm, pl, a, workspace, (hipStream_t)stream);
+}
+
+static int plan_mass_of(const Dims& dm, int32_t B, int32_t M, int32_t Lloc, int32_t window, int32_t sinks, MassPlan* pl) {
+  if (B < 1 || M < 1 || Lloc < 1 || window < 1 || sinks < 0) return MSA_ERR_INVALID_ARG;
+  if (!encoded_sizes_ok(dm, B, M) || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
+  *pl = plan_mass(dm, B, M, Lloc, window, sinks);
+  return pl->ws_bytes != 0 ? MSA_OK : MSA_ERR_UNSUPPORTED;
+}
+
+size_t msa_attend_mass_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
+                                       int32_t sinks) {
+  Dims dm;
+  MassPlan pl;
+  if (make_dims(cfg, &dm, kForAttend) != MSA_OK || plan_mass_of(dm, B, M, Lloc, window, sinks, &pl) != MSA_OK) return 0;
+  return pl.ws_bytes;
+}
+
+int msa_attend_mass(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kloc, int32_t Lloc,
+                    int32_t local_pos0, int32_t window, int32_t sinks, const int32_t* q_pos, const float* lse,
+                    const float* mass, float decay, float* mass_out, void* workspace, size_t workspace_bytes,
+                    msa_stream_t stream) {
+  Dims dm;
+  MassPlan pl;
+  int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (q == nullptr || Kloc == nullptr || q_pos == nullptr || lse == nullptr || mass_out == nullptr || workspace == nullptr ||
+      local_pos0 < 0 || !(decay >= 0.f && decay <= 1.f))
+    return MSA_ERR_INVALID_ARG;
+  rc = plan_mass_of(dm, B, M, Lloc, window, sinks, &pl);
+  if (rc != MSA_OK) return rc;
+  if (misaligned(q) || misaligned(Kloc) || misaligned4(q_pos) || misaligned4(lse) || misaligned4(mass) ||
+      misaligned4(mass_out) || misaligned(workspace))
+    return MSA_ERR_MISALIGNED;
+  if (workspace_bytes < pl.ws_bytes) return MSA_ERR_WORKSPACE;
+  MassArgs a = {};
+  a.q = (const uint16_t*)q;
+  a.Kloc = (const uint16_t*)Kloc;
+  a.lse = lse;
+  a.q_pos = q_pos;
+  a.mass = mass;
+  a.out = mass_out;
+  a.M = M;
+  a.Lloc = Lloc;
+  a.pos0 = local_pos0;
+  a.window = window;
+  a.sinks = sinks;
+  a.decay = decay;
+  return launch_mass(dm, pl, a, B, workspace, (hipStream_t)stream);
+}
+
+int msa_evict(const msa_config_t* cfg, const void* Kloc, const void* Vloc, const float* mass, const int32_t* lens, int32_t B,
+              int32_t Lloc, int32_t keep, int32_t sinks, int32_t recent, void* Kout, void* Vout, float* mass_out,
+              int32_t Lout, int32_t* rows, msa_stream_t stream) {
+  Dims dm;
+  const int rc = make_dims(cfg, &dm, kForAttend);
+  if (rc != MSA_OK) return rc;
+  if (Kloc == nullptr || Vloc == nullptr || mass == nullptr || lens == nullptr || Kout == nullptr || Vout == nullptr ||
+      mass_out == nullptr || rows == nullptr)
+    return MSA_ERR_INVALID_ARG;
+  if (B < 1 || Lloc < 1 || keep < 1 || keep > Lout || sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep)
+    return MSA_ERR_INVALID_ARG;
+  const bool in_place = Kout == Kloc;
+  if ((Vout == Vloc) != in_place || (mass_out == mass) != in_place || (in_place && Lout != Lloc)) return MSA_ERR_INVALID_ARG;
+  if ((int64_t)B * dm.Hkv > (1 << 16) || Lloc > (1 << 28) || Lout > (1 << 28) ||
+      (int64_t)B * dm.Hkv * keep > (1 << 29))
+    return MSA_ERR_UNSUPPORTED;
+  if (misaligned(Kloc) || misaligned(Vloc) || misaligned4(mass) || misaligned4(lens) || misaligned(Kout) ||
+      misaligned(Vout) || misaligned4(mass_out) || misaligned4(rows))
+    return MSA_ERR_MISALIGNED;
+  const EvictArgs a = {(const uint16_t*)Kloc, (const uint16_t*)Vloc, mass, lens, (uint16_t*)Kout, (uint16_t*)Vout, mass_out,
+                       rows, dm.Hkv, Lloc, Lout, keep, sinks, recent};
+  return launch_evict(dm, a, B, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -163,6 +163,13 @@ __device__ __forceinline__ float add_xor16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// x summed over the sixteen lanes that share lane / 16.
+__device__ __forceinline__ float add_over_16(float x) {
+  x += dpp_f<kDppXor1>(x);
+  x += dpp_f<kDppXor2>(x);
+  x += dpp_f<kDppHalfMirror>(x);
+  return x + dpp_f<kDppMirror>(x);
+}
 // x summed over the lanes that share lane % LPR (LPR in {4, 8, 16}).
 template <int LPR>
 __device__ __forceinline__ float add_row_groups(float x) {

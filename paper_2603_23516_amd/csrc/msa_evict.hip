@@ -1,0 +1,161 @@
+// msa_evict: of every (sequence, KV head) the rows of the cache that weigh most, the first ones and the last ones, moved together.
+//
+// Two launches.  evict_select_kernel, a workgroup to a (sequence, KV head), finds the weight of the lightest row that stays, bit by
+// bit from the top (the order-preserving image of a weight as an integer; how many rows reach a candidate is counted), then lists the
+// rows that stay in ascending order and moves their weights.  evict_move_kernel copies the rows of K and V.
+#include "msa_device.h"
+#include "msa_host.h"
+
+namespace msa {
+
+constexpr int kSelectThreads = 1024;
+
+// The order of weights as an integer: what is no number comes last, the zeros are equal.
+__device__ __forceinline__ uint32_t weight_key(float x) {
+  if (x != x) return 0u;
+  return orderable(x == 0.f ? 0.f : x);
+}
+
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
+  constexpr int WAVES = kSelectThreads / 64;
+  __shared__ int cnt_s[2][WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const long long pair = blockIdx.x;
+  int n = a.lens[pair / a.Hkv];
+  n = n < 0 ? 0 : (n > a.Lloc ? a.Lloc : n);
+  const float* const mass = a.mass + pair * a.Lloc;
+  float* const mass_out = a.mass_out + pair * a.Lout;
+  int32_t* const rows = a.rows + pair * a.keep;
+  if (n <= a.keep) {
+    for (int i = tid; i < a.keep; i += kSelectThreads) {
+      rows[i] = i < n ? i : -1;
+      if (i < n && mass_out != mass) mass_out[i] = mass[i];
+    }
+    for (int i = n + tid; i < a.Lout; i += kSelectThreads) mass_out[i] = 0.f;
+    return;
+  }
+  const int m0 = a.sinks, m1 = n - a.recent, need = a.keep - a.sinks - a.recent;  // of rows m0 .. m1 - 1, need < m1 - m0 stay
+  int turn = 0;
+  auto total = [&](int of_wave, int& before) {  // the same in a wave's lanes; the workgroup's sum, and that of the waves before
+    int* const c = cnt_s[turn ^= 1];            // (the other one may still be read)
+    if (lane == 0) c[wave] = of_wave;
+    __syncthreads();
+    int sum = 0;
+    before = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      if (w == wave) before = sum;
+      sum += c[w];
+    }
+    return sum;
+  };
+  uint32_t kth = 0u;
+  int before;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t cnd = kth | (1u << bit);
+    int c = 0;
+    for (int i0 = m0; i0 < m1; i0 += kSelectThreads)
+      c += __popcll(__ballot(i0 + tid < m1 && weight_key(mass[i0 + tid < m1 ? i0 + tid : m1 - 1]) >= cnd));
+    if (total(c, before) >= need) kth = cnd;
+  }
+  int c = 0;
+  for (int i0 = m0; i0 < m1; i0 += kSelectThreads)
+    c += __popcll(__ballot(i0 + tid < m1 && weight_key(mass[i0 + tid < m1 ? i0 + tid : m1 - 1]) > kth));
+  int ties = need - total(c, before);  // so many of the rows that weigh kth stay, the first ones
+  int at = 0;
+  for (int i0 = 0; i0 < n; i0 += kSelectThreads) {
+    const int i = i0 + tid;
+    const float x = mass[i < n ? i : n - 1];
+    const uint32_t key = weight_key(x);
+    const bool middle = i >= m0 && i < m1;
+    const unsigned long long tie = __ballot(middle && key == kth);
+    int t0;
+    const int tied = total(__popcll(tie), t0);  // (behind its barrier every weight of this turn is in a register)
+    const bool stays = i < n && (!middle || key > kth || (key == kth && t0 + __popcll(tie & ((1ull << lane) - 1ull)) < ties));
+    const unsigned long long kept = __ballot(stays);
+    int k0;
+    const int all = total(__popcll(kept), k0);
+    if (stays) {
+      const int to = at + k0 + __popcll(kept & ((1ull << lane) - 1ull));  // to <= i
+      rows[to] = i;
+      mass_out[to] = x;
+    }
+    at += all;
+    ties -= tied < ties ? tied : ties;
+  }
+  for (int i = a.keep + tid; i < a.Lout; i += kSelectThreads) mass_out[i] = 0.f;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int chunks) {
+  constexpr int LPR = D / 8, RPB = 256 / LPR, TURNS = 4;
+  const long long x = blockIdx.x;
+  const int chunk = (int)(x % chunks);
+  const long long pair = x / chunks;
+  const int lr = threadIdx.x % LPR, j0 = chunk * (RPB * TURNS) + threadIdx.x / LPR;
+  const int32_t* const rows = a.rows + pair * a.keep;
+  const uint16_t* const src = (blockIdx.y == 0 ? a.K : a.V) + pair * a.Lloc * D + 8 * lr;
+  uint16_t* const dst = (blockIdx.y == 0 ? a.Kout : a.Vout) + pair * a.Lout * D + 8 * lr;
+  int row[TURNS];
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t) row[t] = j0 + t * RPB < a.keep ? rows[j0 + t * RPB] : -1;
+  uint4 v[TURNS];
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t)
+    if (row[t] >= 0) v[t] = load_stream16(src + (long long)row[t] * D);
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t)
+    if (row[t] >= 0) store_stream16(dst + (long long)(j0 + t * RPB) * D, v[t]);
+}
+
+// In place: a workgroup has 64 bytes of every row of a (sequence, KV head), so that no other one's rows are in its way.  Row j comes
+// from row rows[j] >= j: a turn's rows are all in registers before the first of them is stored, and what later turns read lies
+// behind what this one stores.
+template <int D>
+__global__ __launch_bounds__(1024) void evict_move_in_place_kernel(EvictArgs a) {
+  constexpr int LPR = 4, RPB = 1024 / LPR, TURNS = 4, SLICES = D * 2 / 64;
+  const int slice = blockIdx.x % SLICES;
+  const long long pair = blockIdx.x / SLICES;
+  const int lr = threadIdx.x % LPR, jt = threadIdx.x / LPR;
+  const int32_t* const rows = a.rows + pair * a.keep;
+  uint16_t* const x = (blockIdx.y == 0 ? a.Kout : a.Vout) + pair * a.Lloc * D + slice * 32 + 8 * lr;
+  for (int j0 = 0; j0 < a.keep; j0 += RPB * TURNS) {
+    int row[TURNS];
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      const int j = j0 + t * RPB + jt;
+      row[t] = j < a.keep ? rows[j] : -1;
+      if (row[t] == j) row[t] = -1;  // stays where it is
+    }
+    uint4 v[TURNS];
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t)
+      if (row[t] >= 0) v[t] = *reinterpret_cast<const uint4*>(x + (long long)row[t] * D);
+    wait_stores_done();  // (the loads too)
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t)
+      if (row[t] >= 0) *reinterpret_cast<uint4*>(x + (long long)(j0 + t * RPB + jt) * D) = v[t];
+  }
+}
+
+int launch_evict(const Dims& dm, const EvictArgs& a, int B, hipStream_t st) {
+  const unsigned pairs = (unsigned)B * dm.Hkv;
+  hipLaunchKernelGGL(evict_select_kernel, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+  if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
+  if (a.Kout == a.K) {
+    if (dm.d == 128)
+      hipLaunchKernelGGL(evict_move_in_place_kernel<128>, dim3(pairs * 4, 2), dim3(1024), 0, st, a);
+    else
+      hipLaunchKernelGGL(evict_move_in_place_kernel<64>, dim3(pairs * 2, 2), dim3(1024), 0, st, a);
+  } else {
+    const int chunk = 4 * 256 / (dm.d / 8), chunks = (a.keep + chunk - 1) / chunk;
+    if (dm.d == 128)
+      hipLaunchKernelGGL(evict_move_kernel<128>, dim3(pairs * chunks, 2), dim3(256), 0, st, a, chunks);
+    else
+      hipLaunchKernelGGL(evict_move_kernel<64>, dim3(pairs * chunks, 2), dim3(256), 0, st, a, chunks);
+  }
+  return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
+}
+
+}  // namespace msa

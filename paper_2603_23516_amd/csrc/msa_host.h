@@ -196,7 +196,10 @@ struct NormArgs {
   const uint16_t *q, *k, *v;            // rows of a token, null = none of them
   long long q_stride, k_stride, v_stride;  // elements from one token to the next
   const uint16_t *qw, *kw;              // [D] or null: no norm
-  const int32_t* pos;                   // [BM]
+  const int32_t* pos;                   // [BM], with axes [BM][n_axes]
+  const int32_t* rows;                  // with axes: [BM] rows of the cache, or null: pos (of the first axis) - pos0
+  unsigned long long axes[2];           // the axis of every pair, two bits each
+  int n_axes;                           // 0: one position, pos
   uint16_t *q_out, *Kloc, *Vloc;
   long long BM;
   int M, Hq, Hkv, Lloc, pos0, rotate;
@@ -204,6 +207,35 @@ struct NormArgs {
   int turns_q, turns_k, turns, shares;  // groups of heads a wave takes at a time; waves that share a token
 };
 int launch_norm_rotate(const Dims& dm, NormArgs a, hipStream_t st);
+
+// Attention weights that the rows of the local cache receive (msa_mass.hip).
+struct MassArgs {
+  const uint16_t* q;      // [BM][Hq][D]
+  const uint16_t* Kloc;   // [B][Hkv][Lloc][D]
+  const float* lse;       // [BM][Hq]
+  const int32_t* q_pos;   // [BM]
+  const float* mass;      // [B][Hkv][Lloc] or null
+  float* out;             // may be mass
+  int M, Hq, Hkv, r, Lloc, pos0, window, sinks;
+  float decay, qscale;    // qscale: log2(e) / sqrt(d)
+};
+struct MassPlan {
+  size_t ws_bytes;
+};
+MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks);
+int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws, hipStream_t st);
+
+// The heaviest rows of a cache (msa_evict.hip).
+struct EvictArgs {
+  const uint16_t *K, *V;  // [B][Hkv][Lloc][D]
+  const float* mass;      // [B][Hkv][Lloc]
+  const int32_t* lens;    // [B]
+  uint16_t *Kout, *Vout;  // [B][Hkv][Lout][D]; K and V themselves: in place
+  float* mass_out;        // [B][Hkv][Lout]
+  int32_t* rows;          // [B][Hkv][keep]
+  int Hkv, Lloc, Lout, keep, sinks, recent;
+};
+int launch_evict(const Dims& dm, const EvictArgs& a, int B, hipStream_t st);
 
 // A bank in four bits (msa_kv4.hip).
 struct Pack4Args {  // [0] keys, [1] values; null = none of them

@@ -11,6 +11,9 @@
 // needs no other lane and both loads are 16 bytes; a wave takes 64 / (d/16) heads of one token at a time.  A lane's eight
 // angles are the same for all heads: the wave works out the d/2 angles of its token once, one per lane in double, and
 // passes them around through LDS.
+//
+// msa_norm_rotate_axes is the same pass with several positions per token: the lane that works out angle u takes the position of
+// axis axes[u], and the row of the cache comes with the token (AXES; a variant of its own, so that the other keeps its registers).
 #include "msa_attend.h"
 
 namespace msa {
@@ -28,7 +31,7 @@ __device__ __forceinline__ float head_sum_of_squares(const float (&f1)[8], const
 }
 
 // (Eight waves to a SIMD: the path of large squares would make it seven.)
-template <int D, bool STREAM>
+template <int D, bool STREAM, bool AXES>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(8))) void norm_rotate_kernel(NormArgs a, NormTheta th) {
   constexpr int HALF = D / 2;
   constexpr int LPH = D / 16;    // lanes per head
@@ -40,15 +43,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(8))) void n
   const long long bm = job / a.shares;
   const int share = (int)(job - bm * a.shares);
   if (bm >= a.BM) return;  // wave-uniform; no barrier below
-  const int p = a.pos[bm];
+  const int32_t* const at = a.pos + (AXES ? bm * a.n_axes : bm);
+  const int p = at[0];
   if (p < 0) return;  // padding
   const int l = lane % LPH, hl = lane / LPH;
-  const long long row = (long long)p - a.pos0;
+  const long long row = AXES && a.rows != nullptr ? a.rows[bm] : (long long)p - a.pos0;
   const bool stored = row >= 0 && row < a.Lloc;
   const long long b = bm / a.M;
 
   if (a.rotate) {
-    if (lane < HALF) angles[wave][lane] = cis_pos(p, th.th[lane]);
+    if (lane < HALF) angles[wave][lane] = cis_pos(AXES ? at[(a.axes[lane / 32] >> (2 * (lane % 32))) & 3] : p, th.th[lane]);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
@@ -136,12 +140,20 @@ int launch_norm_rotate(const Dims& dm, NormArgs a, hipStream_t st) {
   // [19.7 / 20.0].
   const int heads = (a.q != nullptr ? dm.Hq : 0) + (a.k != nullptr ? dm.Hkv : 0) + (a.v != nullptr ? dm.Hkv : 0);
   const bool stream = a.BM * heads * dm.d * 2 >= (128ll << 20);
-#define MSA_NORM(DD, SS) hipLaunchKernelGGL((norm_rotate_kernel<DD, SS>), dim3((unsigned)blocks), dim3(256), 0, st, a, th)
-  if (dm.d == 128) {
-    if (stream) MSA_NORM(128, true); else MSA_NORM(128, false);
-  } else {
-    if (stream) MSA_NORM(64, true); else MSA_NORM(64, false);
+#define MSA_NORM(DD, SS, AA) \
+  hipLaunchKernelGGL((norm_rotate_kernel<DD, SS, AA>), dim3((unsigned)blocks), dim3(256), 0, st, a, th)
+#define MSA_NORM_OF(AA)                                                     \
+  if (dm.d == 128) {                                                        \
+    if (stream) MSA_NORM(128, true, AA); else MSA_NORM(128, false, AA);     \
+  } else {                                                                  \
+    if (stream) MSA_NORM(64, true, AA); else MSA_NORM(64, false, AA);       \
   }
+  if (a.n_axes > 0) {
+    MSA_NORM_OF(true)
+  } else {
+    MSA_NORM_OF(false)
+  }
+#undef MSA_NORM_OF
 #undef MSA_NORM
   return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
 }
