@@ -30,6 +30,8 @@ struct TiledArgs {
   uint16_t *Kx, *Vx;  // [B][Hkv][mem_cap][D] rows of the selected documents in bf16, or null
   int* mem_rows;      // [B][Hkv] how many there are
   int mem_cap;        // k G
+  int shared;         // 1: the rows are a prefix of all sequences, [Hkv][mem_cap][D], only read ...
+  const int32_t* shared_lens;  // ... sequence b sees the first shared_lens[b] of; null: all of it
   int tpw, n_tiles;   // tokens per wave, tiles per sequence
 };
 
@@ -44,6 +46,8 @@ struct EncodedPlan {
 // cache that a token can see.  ws_bytes is 0 where the grid does not hold the call: one workgroup per token in its third
 // dimension, or tiles in its first, whose threads count to 2^32.
 EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc);
+// The same for rows in common that are in bf16 already (a prefix) and need no room to be expanded.
+EncodedPlan plan_encoded_prefix(const Dims& dm, int B, int M, long long mem_rows, int Lloc);
 int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, void* ws, hipStream_t st);
 int launch_encoded_tiled(const Dims& dm, const EncodedArgs& a, TiledArgs ta, int B, hipStream_t st);
 
@@ -72,6 +76,19 @@ __device__ __forceinline__ int number_rows(const EncodedArgs& a, int b, long lon
   if (lane == 0) pre[0] = 0;
   before = sum - len;
   return doc;
+}
+
+typedef float f32x16e_t __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16e_t mfma32e(bf16x8_t a, bf16x8_t b, f32x16e_t c) {
+  // D(32x32) += A(32x16) * B(16x32).  Lane l: A[l%32][8(l/32)..+8], B[8(l/32)..+8][l%32],
+  // D register i: row (i%4) + 8(i/4) + 4(l/32), column l%32.
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float max_xor32(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // Rows of the local cache that a token at position p (counted from the cache's first row) sees: [0, first) and [from, to).

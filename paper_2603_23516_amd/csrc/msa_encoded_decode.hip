@@ -366,7 +366,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 }
 
-EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc) {
+static EncodedPlan plan_of(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc,
+                           bool expand) {
   EncodedPlan p = {};
   const long long pairs = (long long)B * M * dm.Hkv;
   // Tokens that share their rows go through the tiled kernel where the single-token kernel would take long over them: its steps
@@ -468,7 +469,7 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   } else {
     take_parts(n_most, rows, dm.d, 1, (size_t)pairs);
   }
-  if (p.tiled && mem_rows > 0) {
+  if (p.tiled && mem_rows > 0 && expand) {
     const size_t x = (size_t)B * dm.Hkv * mem_rows * dm.d * 2;
     p.off_kx = take(x);
     p.off_vx = take(x);
@@ -477,6 +478,13 @@ EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool 
   if (at < single) at = single;
   p.ws_bytes = at > 256 ? at : 256;
   return p;
+}
+
+EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc) {
+  return plan_of(dm, B, M, mem_rows, shared, local_rows, Lloc, true);
+}
+EncodedPlan plan_encoded_prefix(const Dims& dm, int B, int M, long long mem_rows, int Lloc) {
+  return plan_of(dm, B, M, mem_rows, true, Lloc, Lloc, false);
 }
 
 int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, void* ws, hipStream_t st) {

@@ -1,5 +1,6 @@
 // Attention of many query tokens that share position-encoded keys: msa_window_attend over a prompt or a chunk of one,
-// msa_sparse_attend4 where the tokens of a sequence share their documents (token_pool = 1).  Bound by the matrix cores.
+// msa_sparse_attend4 where the tokens of a sequence share their documents (token_pool = 1), msa_prefix_attend where a sequence has
+// enough of them.  Bound by the matrix cores.
 //
 // A workgroup owns a tile of tokens of one (sequence, KV head); its columns are the (token, query head) pairs, 32 to a
 // wave.  The rows any token of the tile sees go by in steps of 32: rows of the documents (expanded to
@@ -30,19 +31,6 @@
 #include <type_traits>
 
 namespace msa {
-
-typedef float f32x16e_t __attribute__((ext_vector_type(16)));
-
-__device__ __forceinline__ f32x16e_t mfma32e(bf16x8_t a, bf16x8_t b, f32x16e_t c) {
-  // D(32x32) += A(32x16) * B(16x32).  Lane l: A[l%32][8(l/32)..+8], B[8(l/32)..+8][l%32],
-  // D register i: row (i%4) + 8(i/4) + 4(l/32), column l%32.
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ float max_xor32(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
 
 // ---- the selected documents of every (sequence, KV head), in bf16, one after another ---------------------------------------
 template <int D>
@@ -148,7 +136,17 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
     to = __builtin_amdgcn_readfirstlane(pmax_t + 1LL < a.Lloc ? pmax_t + 1 : a.Lloc);
   }
   const long long pair = (long long)b * a.Hkv + g;
-  const int rows_mem = ta.Kx != nullptr ? __builtin_amdgcn_readfirstlane(ta.mem_rows[pair]) : 0;
+  // rows that all tokens of the sequence see: its documents, or a prefix that the sequences share
+  const long long mem0 = (ta.shared ? g : pair) * ta.mem_cap;
+  int rows_mem = 0;
+  if (ta.Kx != nullptr) {
+    rows_mem = ta.mem_cap;
+    if (!ta.shared)
+      rows_mem = ta.mem_rows[pair];
+    else if (ta.shared_lens != nullptr)
+      rows_mem = ta.shared_lens[b] < 0 ? 0 : (ta.shared_lens[b] < rows_mem ? ta.shared_lens[b] : rows_mem);
+    rows_mem = __builtin_amdgcn_readfirstlane(rows_mem);
+  }
   const int steps_mem = (rows_mem + 31) / 32, steps_a = (first + 31) / 32, steps_b = (to - from + 31) / 32;
   const int steps = steps_mem + steps_a + steps_b;
   const int sb = (int)((long long)steps * sp / a.n_splits), se = (int)((long long)steps * (sp + 1) / a.n_splits);
@@ -196,8 +194,8 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
     n_run = 0;
     n_t0 = 32 * sb;
     n_end = rows_mem;
-    n_k = ta.Kx + (pair * ta.mem_cap + n_t0) * D;
-    n_v = ta.Vx + (pair * ta.mem_cap + n_t0) * D;
+    n_k = ta.Kx + (mem0 + n_t0) * D;
+    n_v = ta.Vx + (mem0 + n_t0) * D;
   } else if (sb < steps_mem + steps_a) {
     n_run = 1;
     n_t0 = 32 * (sb - steps_mem);

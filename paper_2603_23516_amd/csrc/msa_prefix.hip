@@ -1,9 +1,19 @@
 // msa_prefix_attend: one softmax over the rows of a prefix that all sequences share and over the rows of a sequence's own cache.
 //
-// A workgroup of four waves has sixteen columns, (token, query head) pairs of one (sequence, KV head), and deals the rows they see,
-// 32 at a time, to its waves: S^T[key][col] = K q^T by 16x16x32 bf16 MFMA with the keys straight from memory, an online softmax per
-// column, O^T[dd][col] += V^T P^T with the value rows through LDS and transposing reads.
+// Where a sequence has tokens enough to fill tiles of its own, encoded_tiled_kernel takes them over the prefix and the cache in one
+// go.  With fewer, one launch has workgroups of two kinds:
+//   over the prefix  tiles of 128 columns, (token, query head) pairs of one KV head and of all sequences together, 32 to a wave, so
+//                    that a row is read once for all of them (per tile); bound by the matrix cores once there are more than a few
+//                    tiles' worth, by memory below that.  As encoded_tiled_kernel, without windows and runs: 32 key and 32 value
+//                    rows a step, global -> LDS asynchronously, two steps ahead.
+//   over the caches  sixteen columns of one (sequence, KV head); the rows go straight from memory into registers, dealt to the
+//                    four waves 32 at a time; bound by memory.
+// Both leave (max, sum, output) parts by (token, head) row, which a launch joins.  Parts over the prefix may be many; the two kinds
+// fill each other's gaps, one at the matrix pipe and one at memory.
+// Softmax weights are rounded to bf16 for the second product (2^-8 of themselves at most), their sum is taken before the rounding.
 #include "msa_prefix.h"
+
+#include <type_traits>
 
 namespace msa {
 
@@ -23,6 +33,13 @@ struct Columns {
   f32x4_t o[D / 16];
 };
 
+// What sequence b sees of the prefix.
+__device__ __forceinline__ int prefix_of(const PrefixArgs& a, long long b) {
+  if (a.pre_lens == nullptr) return a.Lpre;
+  const int n = a.pre_lens[b];
+  return n < 0 ? 0 : (n < a.Lpre ? n : a.Lpre);
+}
+
 // Rows [0, end) of K, V, [end][D], in steps of 32: steps s, s + stride, ... below s_end.  Column n sees the rows below lim; least is
 // the smallest lim of the wave's columns.  vt: 32 rows of LDS of the wave's own.
 template <int D>
@@ -34,7 +51,7 @@ __device__ __forceinline__ void attend_rows(const uint16_t* K, const uint16_t* V
   // Value rows in LDS: 16-byte piece p of row i lies at place p ^ swz(i), so that neither the writes (16 rows, one piece) nor
   // the transposing reads (four rows, two pieces) meet in a bank.
   auto swz = [](int i) { return D == 128 ? 2 * (i & 7) : 2 * ((i >> 1) & 3); };
-  uint4 kx[2][NS], vx[2][NS];
+  u32x4_t kx[2][NS], vx[2][NS];
   auto load = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -43,8 +60,8 @@ __device__ __forceinline__ void attend_rows(const uint16_t* K, const uint16_t* V
       const long long at = (long long)row * D + 8 * qd;
 #pragma unroll
       for (int j = 0; j < NS; ++j) {
-        kx[t][j] = *reinterpret_cast<const uint4*>(K + at + 32 * j);
-        vx[t][j] = *reinterpret_cast<const uint4*>(V + at + 32 * j);
+        kx[t][j] = *reinterpret_cast<const u32x4_t*>(K + at + 32 * j);
+        vx[t][j] = *reinterpret_cast<const u32x4_t*>(V + at + 32 * j);
       }
     }
   };
@@ -56,8 +73,8 @@ __device__ __forceinline__ void attend_rows(const uint16_t* K, const uint16_t* V
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int j = 0; j < NS; ++j) {
-        sc[t] = mfma16(as_bf16x8(kx[t][j]), bq[j], sc[t]);
-        *reinterpret_cast<uint4*>(vt + (16 * t + n) * ROW + (((4 * j + qd) ^ swz(16 * t + n)) * 16)) = vx[t][j];
+        sc[t] = mfma16(__builtin_bit_cast(bf16x8_t, kx[t][j]), bq[j], sc[t]);
+        *reinterpret_cast<u32x4_t*>(vt + (16 * t + n) * ROW + (((4 * j + qd) ^ swz(16 * t + n)) * 16)) = vx[t][j];
       }
     if (s + stride < s_end) load(32 * (s + stride));  // under way while this step's weights are worked out
     const int t0 = 32 * s;
@@ -104,20 +121,203 @@ __device__ __forceinline__ void attend_rows(const uint16_t* K, const uint16_t* V
   }
 }
 
+constexpr int kPrefixStages = 3;
+
 template <int D>
-__global__ __launch_bounds__(256) void prefix_rows_kernel(PrefixArgs a, int groups) {
-  constexpr int NS = D / 32, NC = D / 16;
-  constexpr int ROW = D * 2, OROW = D + 4;  // bytes of a value row, floats of a row of a wave's output in the merge
-  constexpr int STAGE = 32 * ROW > 16 * OROW * 4 ? 32 * ROW : 16 * OROW * 4;
-  __shared__ __attribute__((aligned(16))) unsigned char stage[4][STAGE];
-  __shared__ float wm[4][16], wl[4][16];
+__device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned char* smem) {
+  constexpr int NW = 4;
+  constexpr int NP = D / 8;            // 16-byte pieces per row
+  constexpr int NS = D / 16;           // contraction slices of the score product
+  constexpr int NT = D / 32;           // 32-row tiles of the output product
+  constexpr int ROW = D * 2;
+  constexpr int TILE = 32 * ROW;       // bytes of 32 key or value rows
+  constexpr int NI = 32 * NP / 64;     // wave-wide copies for 32 rows
+  constexpr int NPW = 2 * NI / NW;     // copies of a wave per step, keys and values together
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int qd = lane >> 4, n = lane & 15, r = a.r, tpl = 16 / r;
-  const int g = (int)(blockIdx.x % a.Hkv), x = (int)(blockIdx.x / a.Hkv), m0 = x % groups * tpl;
-  const long long b = x / groups;
+  const int hf = lane >> 5, col = lane & 31, r = a.r;
+  // (tile, part, KV head): the KV head fastest, so that an XCD (every eighth workgroup) keeps to few heads' rows
+  const int g = x % a.Hkv;
+  x /= a.Hkv;
+  const int sp = x % a.n_pre, tile = x / a.n_pre;
+  const long long BM = (long long)a.B * a.M;
+
+  // this lane's column, and the rows [0, lim) that it sees
+  const int tl = col / r, head = col - tl * r;
+  const long long tok = ((long long)tile * NW + wave) * a.tpw + tl;
+  const bool ok = tl < a.tpw && tok < BM;
+  const int lim = ok ? prefix_of(a, tok / a.M) : 0;
+  int least = ok ? lim : INT32_MAX, most = lim;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    const int u = __shfl_xor(least, off, 64), v = __shfl_xor(most, off, 64);
+    least = u < least ? u : least;
+    most = v > most ? v : most;
+  }
+  least = __builtin_amdgcn_readfirstlane(least);
+  most = __builtin_amdgcn_readfirstlane(most);
+  int* const most_s = reinterpret_cast<int*>(smem);
+  if (lane == 0) most_s[wave] = most;
+  __syncthreads();
+  int end = most_s[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) end = most_s[w] > end ? most_s[w] : end;
+  end = __builtin_amdgcn_readfirstlane(end);
+  __syncthreads();  // (the copies come to the same place)
+  const int steps = (end + 31) / 32;
+  const int sb = (int)((long long)steps * sp / a.n_pre), se = (int)((long long)steps * (sp + 1) / a.n_pre);
+
+  bf16x8_t bq[NS];
+  const long long qh = (ok ? tok : 0) * a.Hq + g * r + (ok ? head : 0);
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    uint4 v = *reinterpret_cast<const uint4*>(a.q + qh * D + 8 * hf + 16 * s);
+    if (!ok) v = make_uint4(0, 0, 0, 0);
+    bq[s] = as_bf16x8(v);
+  }
+
+  // Places of the 16-byte pieces of a row in LDS: piece p of row i lies at p ^ swz(i), so that the reads meet no bank twice.
+  auto swz_k = [](int i) { return D == 128 ? (i & 15) : ((i >> 1) & 7); };
+  auto swz_v = [](int i) { return D == 128 ? 4 * (i & 3) : 4 * ((i >> 1) & 1); };
+  const int j16 = lane & 15, vrow = 4 * hf + (j16 >> 2);
+  int kat[NS], vat[NT];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) kat[s] = (col * ROW + ((hf ^ swz_k(col)) * 16)) ^ (32 * s);
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    vat[t] = TILE + ((vrow * ROW + (((2 * ((lane >> 4) & 1) + ((j16 & 3) >> 1)) ^ swz_v(vrow)) * 16) + 8 * (j16 & 1)) ^ (64 * t));
+  int coff[NPW];
+#pragma unroll
+  for (int i = 0; i < NPW; ++i) {
+    const int j = i * NW + wave, y = (j < NI ? j : j - NI) * 64 + lane, row = y / NP;
+    coff[i] = row * ROW + ((y % NP) ^ (j < NI ? swz_k(row) : swz_v(row))) * 16;
+  }
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + wave * 1024);
+  const long long at0 = ((long long)g * a.Lpre + 32LL * sb) * D;
+  const uint16_t *n_k = a.Kpre + at0, *n_v = a.Vpre + at0;
+  int n_cnt = end - 32 * sb;  // rows from the next copy's first one on
+  auto issue = [&](auto stage) __attribute__((always_inline)) {
+    constexpr int INTO = decltype(stage)::value;
+#pragma unroll
+    for (int i = 0; i < NPW; ++i) {
+      const uint16_t* src = n_v;
+      if (i * NW + wave < NI) src = n_k;
+      int off = coff[i];
+      if (n_cnt < 32) {  // rows that nobody sees: the last one that somebody does
+        const int last = (n_cnt - 1) * ROW + (off & (ROW - 1));
+        off = off < last ? off : last;
+      }
+      copy16_to_lds_async_at(src, off, lds0 + INTO * 2 * TILE + i * NW * 1024);
+    }
+    n_cnt -= 32;
+    n_k += 32 * D;
+    n_v += 32 * D;
+  };
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16e_t o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+
+  auto step = [&](int s, auto stage) __attribute__((always_inline)) {
+    constexpr int BUF = decltype(stage)::value;
+    unsigned char* const st = smem + BUF * 2 * TILE;
+    if (s + 1 < se)
+      wait_copies_but<NPW>();
+    else
+      wait_copies_but<0>();
+    // step s is staged for everyone; everyone is done with step s - 1's stage (its LDS reads have come back)
+    lds_barrier();
+    if (s + 2 < se) issue(std::integral_constant<int, (BUF + 2) % kPrefixStages>());
+    const int t0 = 32 * s;
+    if (t0 >= most) return;  // this wave sees nothing of the step (uniform)
+    f32x16e_t sc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) sc = mfma32e(as_bf16x8(*reinterpret_cast<const uint4*>(st + kat[k])), bq[k], sc);
+    if (t0 + 32 > least) {
+      const int left = lim - t0 - 4 * hf;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = (i & 3) + 8 * (i >> 2) < left ? sc[i] : -INFINITY;
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+    mx = max_xor32(mx) * a.qscale;
+    if (__ballot(mx > m_run + 8.f) != 0) {  // m_run follows the maximum once that is 2^8 ahead
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t] *= alpha;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    // contraction slot j of slice sg and half hf is key 16 sg + (j % 4) + 8 (j / 4) + 4 hf: the lane's own registers
+#pragma unroll
+    for (int sg = 0; sg < 2; ++sg) {
+      uint32_t pw[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * sg + 2 * i], a.qscale, -m_use));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * sg + 2 * i + 1], a.qscale, -m_use));
+        l_run += p0 + p1;
+        pw[i] = pack_bf16(p0, p1);
+      }
+      const bf16x8_t pb = as_bf16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+      __builtin_amdgcn_sched_barrier(0);  // (the products of one half beside the exponentials of the other)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const s16x4_t v0 = lds_read_tr16(st + vat[t] + 16 * sg * ROW), v1 = lds_read_tr16(st + vat[t] + (16 * sg + 8) * ROW);
+        const bf16x8_t av = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[t] = mfma32e(av, pb, o[t]);
+      }
+    }
+  };
+  if (sb < se) issue(std::integral_constant<int, 0>());
+  if (sb + 1 < se) issue(std::integral_constant<int, 1>());
+  for (int s = sb; s < se; s += kPrefixStages) {  // stages by number, so that LDS addresses are constants
+    step(s, std::integral_constant<int, 0>());
+    if (s + 1 < se) step(s + 1, std::integral_constant<int, 1>());
+    if (s + 2 < se) step(s + 2, std::integral_constant<int, 2>());
+  }
+  const uint32_t u = __float_as_uint(l_run);
+  const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  if (!ok) return;
+  const long long ph = qh * a.n_pre + sp;
+  if (hf == 0) a.pre_ml[ph] = make_float2(m_run, l);
+  if (m_run == -INFINITY) return;  // (an empty part's outputs are not read)
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4_t*>(a.pre_o + ph * D + 32 * t + 8 * i + 4 * hf) =
+          (f32x4_t){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+}
+
+template <int D>
+__device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned char* smem) {
+  constexpr int NS = D / 32, NC = D / 16;
+  constexpr int OROW = D + 4;  // floats of a row of a wave's output in the merge
+  constexpr int STAGE = 16 * OROW * 4;
+  static_assert(STAGE >= 32 * D * 2, "32 value rows");
+  float* const wm = reinterpret_cast<float*>(smem + 4 * STAGE);  // [4][16] maxima, [4][16] sums
+  float* const wl = wm + 64;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qd = lane >> 4, n = lane & 15, r = a.r;
+  const int g = x % a.Hkv;
+  x /= a.Hkv;
+  const int sp = x % a.n_loc;
+  x /= a.n_loc;
+  const int m0 = x % a.groups * a.tpl;
+  const long long b = x / a.groups;
   const int tl = n / r, tok = m0 + tl;
-  const bool ok = tl < tpl && tok < a.M;
+  const bool ok = tl < a.tpl && tok < a.M;
   const long long qh = (b * a.M + (ok ? tok : m0)) * a.Hq + g * r + (ok ? n - tl * r : 0);
   bf16x8_t bq[NS];
 #pragma unroll
@@ -126,12 +326,6 @@ __global__ __launch_bounds__(256) void prefix_rows_kernel(PrefixArgs a, int grou
     if (!ok) v = make_uint4(0, 0, 0, 0);
     bq[s] = as_bf16x8(v);
   }
-  int pre = a.Lpre;
-  if (a.pre_lens != nullptr) {
-    pre = a.pre_lens[b];
-    pre = pre < 0 ? 0 : (pre > a.Lpre ? a.Lpre : pre);
-  }
-  pre = __builtin_amdgcn_readfirstlane(pre);
   const long long p1 = (long long)a.q_pos[b * a.M + (ok ? tok : m0)] - a.pos0 + 1;
   const int lim = ok ? (p1 < 0 ? 0 : (p1 < a.Lloc ? (int)p1 : a.Lloc)) : 0;
   int least = ok ? lim : INT32_MAX, most = lim;
@@ -143,65 +337,144 @@ __global__ __launch_bounds__(256) void prefix_rows_kernel(PrefixArgs a, int grou
   }
   least = __builtin_amdgcn_readfirstlane(least);
   most = __builtin_amdgcn_readfirstlane(most);
+  const int steps = (most + 31) / 32;
+  const int sb = (int)((long long)steps * sp / a.n_loc), se = (int)((long long)steps * (sp + 1) / a.n_loc);
   Columns<D> y;
   y.m_run = -INFINITY;
   y.l_run = 0.f;
 #pragma unroll
   for (int c = 0; c < NC; ++c) y.o[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-  attend_rows<D>(a.Kpre + (long long)g * a.Lpre * D, a.Vpre + (long long)g * a.Lpre * D, pre, wave, (pre + 31) / 32, 4, bq,
-                 ok ? pre : 0, pre, a.qscale, stage[wave], y);
   const long long loc = (b * a.Hkv + g) * a.Lloc * D;
-  attend_rows<D>(a.Kloc + loc, a.Vloc + loc, most, wave, (most + 31) / 32, 4, bq, lim, least, a.qscale, stage[wave], y);
+  attend_rows<D>(a.Kloc + loc, a.Vloc + loc, most, sb + wave, se, 4, bq, lim, least, a.qscale, smem + wave * STAGE, y);
 
   // the four waves' results
   y.l_run = add_xor32(add_xor16(y.l_run));
-  float* const mine = reinterpret_cast<float*>(stage[wave]);
+  float* const mine = reinterpret_cast<float*>(smem + wave * STAGE);
 #pragma unroll
   for (int c = 0; c < NC; ++c) *reinterpret_cast<f32x4_t*>(mine + n * OROW + 16 * c + 4 * qd) = y.o[c];
   if (qd == 0) {
-    wm[wave][n] = y.m_run;
-    wl[wave][n] = y.l_run;
+    wm[16 * wave + n] = y.m_run;
+    wl[16 * wave + n] = y.l_run;
   }
   __syncthreads();
-  for (int e = tid; e < 16 * D; e += 256) {
-    const int c = e / D, dd = e % D, t = c / r;
-    if (t >= tpl || m0 + t >= a.M) continue;
-    const long long at = (b * a.M + m0 + t) * a.Hq + g * r + (c - t * r);
-    float m = wm[0][c];
+  for (int e = tid; e < 16 * D / 4; e += 256) {
+    const int c = e / (D / 4), dd = e % (D / 4) * 4, t = c / r;
+    if (t >= a.tpl || m0 + t >= a.M) continue;
+    const long long ph = ((b * a.M + m0 + t) * a.Hq + g * r + (c - t * r)) * a.n_loc + sp;
+    float m = wm[c];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) m = fmaxf(m, wm[w][c]);
-    float l = 0.f, v = 0.f;
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, wm[16 * w + c]);
+    float l = 0.f;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = wm[w][c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[w][c] - m);
-      l += f * wl[w][c];
-      v += f * reinterpret_cast<const float*>(stage[w])[c * OROW + dd];
+      const float f = wm[16 * w + c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[16 * w + c] - m);
+      l += f * wl[16 * w + c];
+      v += f * *reinterpret_cast<const f32x4_t*>(smem + w * STAGE + (c * OROW + dd) * 4);
     }
-    a.out[at * D + dd] = (uint16_t)pack_bf16(l > 0.f ? v / l : 0.f, 0.f);
-    if (dd == 0 && a.lse != nullptr) a.lse[at] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (dd == 0) a.loc_ml[ph] = make_float2(m, l);
+    *reinterpret_cast<f32x4_t*>(a.loc_o + ph * D + dd) = v;
   }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void prefix_kernel(PrefixArgs a) {
+  constexpr int BYTES = kPrefixStages * 2 * 32 * D * 2;
+  constexpr int CACHE = 4 * 16 * (D + 4) * 4 + 512;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[BYTES > CACHE ? BYTES : CACHE];
+  if ((int)blockIdx.x < a.pre_groups)
+    over_prefix<D>(a, blockIdx.x, smem);
+  else
+    over_cache<D>(a, blockIdx.x - a.pre_groups, smem);
 }
 
 PrefixPlan plan_prefix(const Dims& dm, int B, int M, int Lpre, int Lloc) {
   PrefixPlan p = {};
-  const int tpl = 16 / dm.r;
-  if ((long long)B * ((M + tpl - 1) / tpl) * dm.Hkv >= 1 << 24) return p;
-  p.ws_bytes = 256;
+  if (M >= 32 && M * dm.r >= 128) {
+    p.tiled = 1;
+    p.tiles = plan_encoded_prefix(dm, B, M, Lpre, Lloc);
+    p.ws_bytes = p.tiles.ws_bytes;
+    return p;
+  }
+  const long long BM = (long long)B * M, rows = BM * dm.Hq;
+  const int tpw = 32 / dm.r, tpl = 16 / dm.r;
+  const long long tiles = (BM + 4 * tpw - 1) / (4 * tpw) * dm.Hkv, groups = (long long)B * ((M + tpl - 1) / tpl) * dm.Hkv;
+  if (tiles + groups >= 1 << 22) return p;
+  auto parts = [](long long steps, long long units, long long wanted, long long least, int most) {
+    long long n = (wanted + units - 1) / units;
+    if (n > steps / least) n = steps / least;
+    return (int)(n < 1 ? 1 : (n > most ? most : n));
+  };
+  p.n_pre = Lpre > 0 ? parts((Lpre + 31) / 32, tiles, 512, 4, 64) : 0;
+  p.n_loc = Lloc > 0 ? parts((Lloc + 31) / 32, groups, 512, 8, 32) : 0;
+  size_t at = round_up256((size_t)rows * p.n_pre * dm.d * sizeof(float));
+  p.off_pre_ml = at;
+  at += round_up256((size_t)rows * p.n_pre * sizeof(float2));
+  p.off_loc_o = at;
+  at += round_up256((size_t)rows * p.n_loc * dm.d * sizeof(float));
+  p.off_loc_ml = at;
+  at += round_up256((size_t)rows * p.n_loc * sizeof(float2));
+  p.ws_bytes = at;
   return p;
 }
 
 int launch_prefix(const Dims& dm, const PrefixPlan& pl, PrefixArgs a, void* ws, hipStream_t st) {
+  unsigned char* const w = (unsigned char*)ws;
   a.Hq = dm.Hq;
   a.Hkv = dm.Hkv;
   a.r = dm.r;
   a.qscale = (float)(1.4426950408889634 / sqrt((double)dm.d));
-  const int tpl = 16 / dm.r, groups = (a.M + tpl - 1) / tpl;
-  const dim3 grid((unsigned)((long long)a.B * groups * dm.Hkv));
+  if (pl.tiled) {
+    EncodedArgs e = {};
+    e.q = a.q;
+    e.Kloc = a.Kloc;
+    e.Vloc = a.Vloc;
+    e.q_pos = a.q_pos;
+    e.out = a.out;
+    e.lse = a.lse;
+    e.part_o = (float*)w;
+    e.part_ml = (float2*)(w + pl.tiles.off_ml);
+    e.M = a.M;
+    e.Hq = a.Hq;
+    e.Hkv = a.Hkv;
+    e.r = a.r;
+    e.Lloc = a.Lloc;
+    e.pos0 = a.pos0;
+    e.window = INT32_MAX;
+    e.n_splits = pl.tiles.n_splits;
+    e.qscale = a.qscale;
+    if (e.n_splits == 2) e.tickets = (unsigned long long*)(w + pl.tiles.off_tickets);
+    e.nonce = launch_nonce48();
+    TiledArgs ta = {};
+    ta.tpw = pl.tiles.tpw;
+    ta.n_tiles = pl.tiles.n_tiles;
+    if (a.Lpre > 0) {
+      ta.Kx = const_cast<uint16_t*>(a.Kpre);
+      ta.Vx = const_cast<uint16_t*>(a.Vpre);
+      ta.mem_cap = a.Lpre;
+      ta.shared = 1;
+      ta.shared_lens = a.pre_lens;
+    }
+    return launch_encoded_tiled(dm, e, ta, a.B, st);
+  }
+  const long long BM = (long long)a.B * a.M;
+  a.tpw = 32 / dm.r;
+  a.tpl = 16 / dm.r;
+  a.groups = (a.M + a.tpl - 1) / a.tpl;
+  a.n_pre = pl.n_pre;
+  a.n_loc = pl.n_loc;
+  a.pre_o = (float*)w;
+  a.pre_ml = (float2*)(w + pl.off_pre_ml);
+  a.loc_o = (float*)(w + pl.off_loc_o);
+  a.loc_ml = (float2*)(w + pl.off_loc_ml);
+  a.pre_groups = (int)((BM + 4 * a.tpw - 1) / (4 * a.tpw) * dm.Hkv * a.n_pre);
+  const dim3 grid((unsigned)(a.pre_groups + (long long)a.B * a.groups * dm.Hkv * a.n_loc));
   if (dm.d == 128)
-    hipLaunchKernelGGL(prefix_rows_kernel<128>, grid, dim3(256), 0, st, a, groups);
+    hipLaunchKernelGGL(prefix_kernel<128>, grid, dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL(prefix_rows_kernel<64>, grid, dim3(256), 0, st, a, groups);
-  return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
+    hipLaunchKernelGGL(prefix_kernel<64>, grid, dim3(256), 0, st, a);
+  if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
+  return launch_merge2(dm.d, a.pre_o, a.pre_ml, a.n_pre, a.loc_o, a.loc_ml, a.n_loc, a.out, a.lse, 0, BM * dm.Hq, st);
 }
 
 }  // namespace msa
