@@ -51,6 +51,11 @@ __device__ __forceinline__ void copy16_to_lds_async_stream64(const void* gaddr, 
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
                :: "v"(gaddr), "s"(lds_addr) : "memory", "m0");
 }
+// ... with 4 bytes per lane, lane l's word at lds_addr + 4 l.
+__device__ __forceinline__ void copy4_to_lds_async64(const void* gaddr, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+               :: "v"(gaddr), "s"(lds_addr) : "memory", "m0");
+}
 // LDS byte address of a __shared__ object
 __device__ __forceinline__ uint32_t lds_addr_of(const void* p) {
   return (uint32_t)(size_t)(const __attribute__((address_space(3))) void*)p;

@@ -220,6 +220,9 @@ struct MassArgs {
   float decay, qscale;    // qscale: log2(e) / sqrt(d)
 };
 struct MassPlan {
+  int tiled;               // 1: mass_tiled_kernel, 0: mass_rows_kernel
+  int n_blocks, per_wave;  // rows: workgroups of a (sequence, KV head), blocks of 32 rows of a wave
+  int n_tiles, n_parts, tpw;
   size_t ws_bytes;
 };
 MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks);

@@ -1,86 +1,356 @@
 // msa_attend_mass: the attention weight that every row of the local cache receives from the tokens of a call,
 //     out[b][g][t] = decay mass[b][g][t] + sum over tokens m and heads h of group g that see row t of
 //                    exp(q[b][m][h] . Kloc[b][g][t] / sqrt(d) - lse[b][m][h])
-// with the log-sums that the attention left.  A wave owns 32 rows, which stay in registers; the (token, head) pairs go by sixteen at
-// a time, scores by 16x16x32 bf16 MFMA (rows of K against columns of pairs), and every lane adds up its rows' weights, joined over
-// the sixteen columns at the end.  Nothing depends on an order of arrival.
+// with the log-sums that the attention left.  The product has rows of K against columns, (token, head) pairs of one (sequence, KV
+// head); a weight is one fma and one exponential, and every lane adds up its rows' weights over the columns it meets, the lanes of a
+// row at the end.  Nothing depends on an order of arrival.  Queries and keys are bf16 as given, products and sums fp32: nothing is
+// rounded to fewer bits.
+//
+// mass_rows_kernel, up to 64 columns: the queries stay in registers, a wave streams blocks of 32 rows, the next one under way while
+// one is worked out.  Bound by memory: K is read once.
+//
+// mass_tiled_kernel, more columns: a wave keeps 64 rows in registers, the queries come by in steps of 32 columns through LDS.  Per 64 x
+// 32 weights 16 products of 32x32x16 (d = 128) stand against 96 vector instructions of which 32 are exponentials at a quarter of the
+// rate: bound by those and the matrix pipe together.  The columns that a tile of 256 rows needs are shared out to several workgroups,
+// whose sums mass_join_kernel adds in order.
 #include "msa_encoded.h"
+
+#include <type_traits>
 
 namespace msa {
 
-template <int D>
-__global__ __launch_bounds__(256) void mass_rows_kernel(MassArgs a, int n_blocks) {
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Which rows a token sees: t <= p with t >= lo or t < sinks; none: p = -1.
+struct SeenBy {
+  int p, lo;
+};
+__device__ __forceinline__ SeenBy seen_by(const MassArgs& a, int32_t q_pos) {
+  const long long pl = (long long)q_pos - a.pos0;
+  SeenBy s;
+  s.p = pl < -1 ? -1 : (pl < a.Lloc ? (int)pl : a.Lloc - 1);
+  const long long lo = pl - a.window + 1;
+  s.lo = lo < 0 ? 0 : (lo < a.Lloc ? (int)lo : a.Lloc);
+  return s;
+}
+__device__ __forceinline__ float old_weight(const MassArgs& a, long long at) {
+  return a.mass != nullptr && a.decay != 0.f ? a.mass[at] * a.decay : 0.f;
+}
+
+// ---- few columns ---------------------------------------------------------------------------------------------------------
+template <int D, int CG>  // CG: groups of 16 columns
+__global__ __launch_bounds__(256) void mass_rows_kernel(MassArgs a, int n_blocks, int per_wave) {
   constexpr int NS = D / 32;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qd = lane >> 4, n = lane & 15, r = a.r;
   const long long pair = blockIdx.x / n_blocks;
-  const int t0 = ((int)(blockIdx.x % n_blocks) * 4 + wave) * 32;
-  if (t0 >= a.Lloc) return;  // no barrier below
+  const int first = (int)(blockIdx.x % n_blocks) * 4 * per_wave + wave;  // the wave's blocks: first, first + 4, ...
   const int g = (int)(pair % a.Hkv);
   const long long b = pair / a.Hkv;
-  float sum[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-  bool loaded = false;
-  bf16x8_t k[2][NS];
   const int cols = a.M * r;
-  for (int c0 = 0; c0 < cols; c0 += 16) {
-    const int c = c0 + n < cols ? c0 + n : cols - 1;
-    const long long tok = b * a.M + c / r;
-    const long long qh = tok * a.Hq + g * r + c % r;
-    const long long pl = (long long)a.q_pos[tok] - a.pos0;
-    // rows t <= p with t >= lo or t < sinks
-    int p = c0 + n < cols ? (pl < -1 ? -1 : (pl < a.Lloc ? (int)pl : a.Lloc - 1)) : -1;
-    const float ls = a.lse[qh] * 1.4426950408889634f;
-    if (ls == -INFINITY) p = -1;  // a token that saw nothing
-    const long long lol = pl - a.window + 1;
-    const int lo = lol < 0 ? 0 : (lol < a.Lloc ? (int)lol : a.Lloc);
-    if (__ballot(t0 <= p && (t0 + 31 >= lo || t0 < a.sinks)) == 0) continue;
-    if (!loaded) {
-      loaded = true;
+  bf16x8_t q[CG][NS];
+  float ls[CG];
+  SeenBy see[CG];
+  int most = -1;  // the last row that any column sees
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int row = t0 + 16 * t + n < a.Lloc ? t0 + 16 * t + n : a.Lloc - 1;
+  for (int c = 0; c < CG; ++c) {
+    const int at = 16 * c + n, col = at < cols ? at : cols - 1;
+    const long long tok = b * a.M + col / r, qh = tok * a.Hq + g * r + col % r;
+    see[c] = seen_by(a, a.q_pos[tok]);
+    ls[c] = a.lse[qh] * kLog2e;
+    if (at >= cols || ls[c] == -INFINITY) see[c].p = -1;  // (a token that saw nothing)
+    most = see[c].p > most ? see[c].p : most;
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
-          k[t][s] = as_bf16x8(*reinterpret_cast<const uint4*>(a.Kloc + (pair * a.Lloc + row) * D + 32 * s + 8 * qd));
-      }
-    }
-    f32x4_t sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const bf16x8_t q = as_bf16x8(*reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd));
-      sc[0] = mfma16(k[0][s], q, sc[0]);
-      sc[1] = mfma16(k[1][s], q, sc[1]);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int t = t0 + 16 * (i >> 2) + 4 * qd + (i & 3);
-      const float w = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][i & 3], a.qscale, -ls));
-      sum[i] += t <= p && (t >= lo || t < a.sinks) ? w : 0.f;
-    }
+    for (int s = 0; s < NS; ++s) q[c][s] = as_bf16x8(*reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd));
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum[i] = add_over_16(sum[i]);
-  if (n < 8) {
-    float v = sum[0];
+  for (int off = 8; off > 0; off >>= 1) {
+    const int v = __shfl_xor(most, off, 64);
+    most = v > most ? v : most;
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  const uint16_t* const keys = a.Kloc + pair * a.Lloc * D + 8 * qd;
+  u32x4_t k[2][NS];
+  auto load = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v = n == i ? sum[i] : v;
-    const int t = t0 + 16 * (n >> 2) + 4 * qd + (n & 3);
-    if (t < a.Lloc) {
-      const long long at = pair * a.Lloc + t;
-      if (a.mass != nullptr && a.decay != 0.f) v = fmaf(a.mass[at], a.decay, v);
-      a.out[at] = v;
+    for (int t = 0; t < 2; ++t) {
+      int row = t0 + 16 * t + n;
+      row = row <= most ? row : most;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[t][s] = *reinterpret_cast<const u32x4_t*>(keys + (long long)row * D + 32 * s);
+    }
+  };
+  if (32 * first <= most) load(32 * first);
+  for (int i = 0; i < per_wave; ++i) {
+    const int t0 = 32 * (first + 4 * i);
+    if (t0 >= a.Lloc) break;
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+    if (t0 <= most) {  // wave-uniform
+      f32x4_t sc[CG][2];
+#pragma unroll
+      for (int c = 0; c < CG; ++c) {
+        sc[c][0] = sc[c][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          sc[c][0] = mfma16(__builtin_bit_cast(bf16x8_t, k[0][s]), q[c][s], sc[c][0]);
+          sc[c][1] = mfma16(__builtin_bit_cast(bf16x8_t, k[1][s]), q[c][s], sc[c][1]);
+        }
+      }
+      if (i + 1 < per_wave && t0 + 128 <= most) load(t0 + 128);
+#pragma unroll
+      for (int c = 0; c < CG; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = t0 + 16 * (j >> 2) + 4 * qd + (j & 3);
+          const float w = __builtin_amdgcn_exp2f(fmaf(sc[c][j >> 2][j & 3], a.qscale, -ls[c]));
+          sum[j] += (t <= see[c].p) & ((t >= see[c].lo) | (t < a.sinks)) ? w : 0.f;
+        }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] = add_over_16(sum[j]);
+    }
+    if (n < 8) {
+      float v = sum[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) v = n == j ? sum[j] : v;
+      const int t = t0 + 16 * (n >> 2) + 4 * qd + (n & 3);
+      if (t < a.Lloc && (t0 <= most || a.mass != a.out || a.decay != 1.f)) {  // (rows that nobody sees, in place: as they are)
+        const long long at = pair * a.Lloc + t;
+        a.out[at] = old_weight(a, at) + v;
+      }
     }
   }
 }
 
+// ---- many columns --------------------------------------------------------------------------------------------------------
+constexpr int kMassRows = 64;    // rows of a wave
+constexpr int kMassStages = 3;
+constexpr long long kMassItems = 2048;  // fewer tiles than this: their columns in parts
+
+struct MassParts {
+  float* part;      // [B * Hkv][n_parts][Lloc] sums of the parts, n_parts > 1
+  int n_parts, n_tiles, tpw;  // tpw: tokens per step
+};
+
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void mass_tiled_kernel(MassArgs a, MassParts pp) {
+  constexpr int NP = D / 8, NS = D / 16, ROW = D * 2;
+  constexpr int KT = kMassRows / 32;
+  constexpr int TILE = 32 * ROW;          // bytes of a step's queries
+  constexpr int NPW = 32 * NP / 64 / 4;   // copies of a wave per step
+  constexpr int SIDE = 4 * 256;           // behind them, for every wave: 32 log-sums and 32 positions
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kMassStages * (TILE + SIDE)];
+  __shared__ int lo_s[4], hi_s[4];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hf = lane >> 5, col = lane & 31, r = a.r;
+  int x = blockIdx.x;
+  const int g = x % a.Hkv;  // the KV head fastest: an XCD keeps to few heads' queries
+  x /= a.Hkv;
+  const int part = x % pp.n_parts;
+  x /= pp.n_parts;
+  const int tile = x % pp.n_tiles;
+  const long long b = x / pp.n_tiles, pair = b * a.Hkv + g;
+  const int tile0 = tile * 4 * kMassRows, t0 = tile0 + wave * kMassRows;
+
+  // steps with a token that sees a row of the tile: from the first to the last of them
+  const int tile1 = (tile0 + 4 * kMassRows < a.Lloc ? tile0 + 4 * kMassRows : a.Lloc) - 1;
+  int s_lo = INT32_MAX, s_hi = -1;
+  for (int m = tid; m < a.M; m += 256) {
+    const SeenBy s = seen_by(a, a.q_pos[b * a.M + m]);
+    if (s.p >= tile0 && (s.lo <= tile1 || tile0 < a.sinks)) {
+      s_lo = s_lo < m ? s_lo : m;
+      s_hi = m;
+    }
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const int u = __shfl_xor(s_lo, off, 64), v = __shfl_xor(s_hi, off, 64);
+    s_lo = u < s_lo ? u : s_lo;
+    s_hi = v > s_hi ? v : s_hi;
+  }
+  if (lane == 0) {
+    lo_s[wave] = s_lo;
+    hi_s[wave] = s_hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    s_lo = lo_s[w] < s_lo ? lo_s[w] : s_lo;
+    s_hi = hi_s[w] > s_hi ? hi_s[w] : s_hi;
+  }
+  s_lo = __builtin_amdgcn_readfirstlane(s_lo) / pp.tpw;
+  s_hi = __builtin_amdgcn_readfirstlane(s_hi);
+  const int n_steps = s_hi < 0 ? 0 : s_hi / pp.tpw + 1 - s_lo;
+  if (n_steps == 0) s_lo = 0;
+  const int sb = s_lo + (int)((long long)n_steps * part / pp.n_parts);
+  const int se = s_lo + (int)((long long)n_steps * (part + 1) / pp.n_parts);
+
+  float sum[KT][16];
+#pragma unroll
+  for (int k = 0; k < KT; ++k)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[k][i] = 0.f;
+  if (sb < se) {
+    // rows: A operand of slice s: dims 16 s + 8 hf .. + 8 of row lane % 32
+    bf16x8_t key[KT][NS];
+#pragma unroll
+    for (int k = 0; k < KT; ++k) {
+      int row = t0 + 32 * k + col;
+      row = row < a.Lloc ? row : a.Lloc - 1;
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        key[k][s] = as_bf16x8(*reinterpret_cast<const uint4*>(a.Kloc + (pair * a.Lloc + row) * D + 16 * s + 8 * hf));
+    }
+    // Queries in LDS: piece p of column i lies at p ^ swz(i), so that the reads meet no bank twice.
+    auto swz = [](int i) { return D == 128 ? (i & 15) : ((i >> 1) & 7); };
+    int qat[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qat[s] = (col * ROW + ((hf ^ swz(col)) * 16)) ^ (32 * s);
+    // A wave's copies of a step: copy j brings 1 KiB, 16 bytes to a lane; column c of a step is head c % r of its token c / r
+    // (columns past the last whole token: the first one again)
+    int ctok[NPW], coff[NPW];
+#pragma unroll
+    for (int i = 0; i < NPW; ++i) {
+      const int y = (i * 4 + wave) * 64 + lane, row = y / NP;
+      int c = row;
+      if (c >= pp.tpw * r) c = 0;
+      ctok[i] = c / r;
+      coff[i] = (c % r) * ROW + ((y % NP) ^ swz(row)) * 16;
+    }
+    const int my_tok = col / r, my_head = col - my_tok * r;
+    const bool col_ok = my_tok < pp.tpw;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem));
+    const uint16_t* const q0 = a.q + (b * a.M * a.Hq + g * r) * D;
+    auto issue = [&](int s, auto stage) __attribute__((always_inline)) {
+      constexpr int INTO = decltype(stage)::value;
+      const int m0 = s * pp.tpw, left = a.M - 1 - m0;  // left >= 0
+#pragma unroll
+      for (int i = 0; i < NPW; ++i) {
+        const int t = ctok[i] < left ? ctok[i] : left;
+        copy16_to_lds_async_at(q0 + (long long)m0 * a.Hq * D, t * a.Hq * ROW + coff[i],
+                               lds0 + INTO * (TILE + SIDE) + (i * 4 + wave) * 1024);
+      }
+      int t = col_ok ? my_tok : 0;
+      t = t < left ? t : left;
+      const long long tok = b * a.M + m0 + t;
+      const void* const src = hf == 0 ? (const void*)(a.lse + tok * a.Hq + g * r + (col_ok ? my_head : 0))
+                                      : (const void*)(a.q_pos + tok);
+      copy4_to_lds_async64(src, lds0 + INTO * (TILE + SIDE) + TILE + wave * 256);
+    };
+    auto step = [&](int s, auto stage) __attribute__((always_inline)) {
+      constexpr int BUF = decltype(stage)::value;
+      const unsigned char* const st = smem + BUF * (TILE + SIDE);
+      if (s + 1 < se)
+        wait_copies_but<NPW + 1>();
+      else
+        wait_copies_but<0>();
+      lds_barrier();
+      if (s + 2 < se) issue(s + 2, std::integral_constant<int, (BUF + 2) % kMassStages>());
+      const float* const side = reinterpret_cast<const float*>(st + TILE + wave * 256);
+      float nls = -side[col] * kLog2e;
+      SeenBy see = seen_by(a, __float_as_int(side[32 + col]));
+      const bool there = col_ok && my_tok < a.M - s * pp.tpw;
+      if (!there || nls == INFINITY) see.p = -1;  // (a token that saw nothing)
+      const bool any = see.p >= t0 && (see.lo < t0 + kMassRows || t0 < a.sinks);
+      if (__ballot(any) == 0) return;
+      // seen whole by all columns that are there; the others weigh exp2(-inf)
+      const bool whole = __ballot(there && !(see.p >= t0 + kMassRows - 1 && (see.lo <= t0 || t0 + kMassRows <= a.sinks))) == 0;
+      if (!there) nls = -INFINITY;
+      f32x16e_t sc[KT];
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[k][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        const bf16x8_t q = as_bf16x8(*reinterpret_cast<const uint4*>(st + qat[i]));
+#pragma unroll
+        for (int k = 0; k < KT; ++k) sc[k] = mfma32e(key[k][i], q, sc[k]);
+      }
+      if (whole) {
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[k][i] += __builtin_amdgcn_exp2f(fmaf(sc[k][i], a.qscale, nls));
+      } else {
+        const int most = see.p - t0 - 4 * hf, least = see.lo - t0 - 4 * hf, few = a.sinks - t0 - 4 * hf;
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int t = 32 * k + (i & 3) + 8 * (i >> 2);
+            const float w = __builtin_amdgcn_exp2f(fmaf(sc[k][i], a.qscale, nls));
+            sum[k][i] += (t <= most) & ((t >= least) | (t < few)) ? w : 0.f;
+          }
+      }
+    };
+    issue(sb, std::integral_constant<int, 0>());
+    if (sb + 1 < se) issue(sb + 1, std::integral_constant<int, 1>());
+    for (int s = sb; s < se; s += kMassStages) {  // stages by number, so that LDS addresses are constants
+      step(s, std::integral_constant<int, 0>());
+      if (s + 1 < se) step(s + 1, std::integral_constant<int, 1>());
+      if (s + 2 < se) step(s + 2, std::integral_constant<int, 2>());
+    }
+  }
+  // over the 32 columns: lane c of a half keeps the sum of register c
+#pragma unroll
+  for (int k = 0; k < KT; ++k) {
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float s = add_xor16(add_over_16(sum[k][i]));
+      v = (lane & 15) == i ? s : v;
+    }
+    const int i = lane & 15, t = t0 + 32 * k + (i & 3) + 8 * (i >> 2) + 4 * hf;
+    if ((lane & 16) == 0 && t < a.Lloc) {
+      const long long at = pair * a.Lloc + t;
+      if (pp.n_parts > 1)
+        pp.part[(pair * pp.n_parts + part) * a.Lloc + t] = v;
+      else
+        a.out[at] = old_weight(a, at) + v;
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void mass_join_kernel(MassArgs a, const float* part, int n_parts, long long n) {
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (at >= n) return;
+  const long long pair = at / a.Lloc;
+  const float* const p = part + pair * n_parts * a.Lloc + (at - pair * a.Lloc);
+  float v = old_weight(a, at);
+  for (int i = 0; i < n_parts; ++i) v += p[(long long)i * a.Lloc];
+  a.out[at] = v;
+}
+
 MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks) {
   MassPlan p = {};
-  const long long blocks = (long long)B * dm.Hkv * ((Lloc + 127) / 128);
-  if (blocks >= 1 << 24) return p;
+  const long long pairs = (long long)B * dm.Hkv;
   p.ws_bytes = 256;
+  if (M * dm.r <= 64) {
+    const long long blocks = (Lloc + 31) / 32;
+    p.per_wave = 1;
+    while (p.per_wave < 8 && pairs * blocks / (p.per_wave * 2) >= 4096) p.per_wave *= 2;
+    p.n_blocks = (int)((blocks + 4 * p.per_wave - 1) / (4 * p.per_wave));
+    if (pairs * p.n_blocks >= 1 << 24) p.ws_bytes = 0;
+    return p;
+  }
+  p.tiled = 1;
+  p.tpw = 32 / dm.r;
+  p.n_tiles = (Lloc + 4 * kMassRows - 1) / (4 * kMassRows);
+  const long long tiles = pairs * p.n_tiles, steps = (M + p.tpw - 1) / p.tpw;
+  long long n = (kMassItems + tiles - 1) / tiles, most = steps / 16 < 32 ? steps / 16 : 32;
+  if (n > most) n = most;
+  p.n_parts = (int)(n < 1 ? 1 : n);
+  if (tiles * p.n_parts >= 1 << 24) {
+    p.ws_bytes = 0;
+    return p;
+  }
+  // (tiles in parts are fewer than kMassItems, so less than twice as many workgroups in all; no less for a longer cache)
+  const long long sums = most * pairs * Lloc, bound = 2 * kMassItems * 4 * kMassRows;
+  if (most > 1) p.ws_bytes = round_up256((size_t)(sums < bound ? sums : bound) * sizeof(float));
   return p;
 }
 
@@ -89,12 +359,35 @@ int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws,
   a.Hkv = dm.Hkv;
   a.r = dm.r;
   a.qscale = (float)(1.4426950408889634 / sqrt((double)dm.d));
-  const int n_blocks = (a.Lloc + 127) / 128;
-  const dim3 grid((unsigned)((long long)B * dm.Hkv * n_blocks));
+  const long long pairs = (long long)B * dm.Hkv;
+  if (!pl.tiled) {
+    const dim3 grid((unsigned)(pairs * pl.n_blocks)), block(256);
+    const int groups = (a.M * dm.r + 15) / 16;
+#define MSA_MASS(DD, CC) hipLaunchKernelGGL((mass_rows_kernel<DD, CC>), grid, block, 0, st, a, pl.n_blocks, pl.per_wave)
+#define MSA_MASS_OF(DD)            \
+  if (groups == 1) MSA_MASS(DD, 1); \
+  else if (groups == 2) MSA_MASS(DD, 2); \
+  else MSA_MASS(DD, 4)
+    if (dm.d == 128) {
+      MSA_MASS_OF(128);
+    } else {
+      MSA_MASS_OF(64);
+    }
+#undef MSA_MASS_OF
+#undef MSA_MASS
+    return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
+  }
+  const MassParts pp = {(float*)ws, pl.n_parts, pl.n_tiles, pl.tpw};
+  const dim3 grid((unsigned)(pairs * pl.n_tiles * pl.n_parts));
   if (dm.d == 128)
-    hipLaunchKernelGGL(mass_rows_kernel<128>, grid, dim3(256), 0, st, a, n_blocks);
+    hipLaunchKernelGGL(mass_tiled_kernel<128>, grid, dim3(256), 0, st, a, pp);
   else
-    hipLaunchKernelGGL(mass_rows_kernel<64>, grid, dim3(256), 0, st, a, n_blocks);
+    hipLaunchKernelGGL(mass_tiled_kernel<64>, grid, dim3(256), 0, st, a, pp);
+  if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
+  if (pl.n_parts > 1) {
+    const long long n = pairs * a.Lloc;
+    hipLaunchKernelGGL(mass_join_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, (const float*)ws, pl.n_parts, n);
+  }
   return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
 }
 

@@ -44,6 +44,9 @@ def test_workspace_sizes(lib):
         n = msa.attend_mass_workspace_bytes(cfg, B, M, L, L, 0)
         assert n >= 256 and n % 256 == 0
         assert _call(lib, cfg, B=B, M=M, L=L, W=L, bytes=n - 1) == msa.MSA_ERR_WORKSPACE
+    for cfg, B, M in itertools.product((_cfg(32, 8, 128), _cfg(8, 1, 64)), (1, 3, 40), (1, 40, 700, 9000)):   # a longer cache: no less
+        sizes = [msa.attend_mass_workspace_bytes(cfg, B, M, L, L) for L in (1, 255, 256, 257, 1000, 9000, 70000, 700000)]
+        assert sizes == sorted(sizes)
     with pytest.raises(ValueError):
         msa.attend_mass_workspace_bytes(_cfg(), 1, 2 ** 32 + 1, 8, 8)
     assert msa.attend_mass_workspace_bytes(_cfg(), 1, 1, 0, 8) == 0
