@@ -16,10 +16,13 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
   return orderable(x == 0.f ? 0.f : x);
 }
 
+// REGS: rows of a thread, held in registers, of at most 1024 REGS in all; 0: any number, read again for every bit.
+template <int REGS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int WAVES = kSelectThreads / 64;
   __shared__ int cnt_s[2][WAVES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long pair = blockIdx.x;
   int n = a.lens[pair / a.Hkv];
   n = n < 0 ? 0 : (n > a.Lloc ? a.Lloc : n);
@@ -49,39 +52,108 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     }
     return sum;
   };
+  static_assert(REGS <= 32, "a bit per row");
+  // a wave's rows are `blocks` times 64 in a row, from w0 on; without registers the workgroup's are taken 1024 at a time
+  const int blocks = (n + kSelectThreads - 1) / kSelectThreads, w0 = wave * blocks * 64 + lane;
+  float x[REGS > 0 ? REGS : 1];
+  uint32_t key[REGS > 0 ? REGS : 1];  // of rows in the middle, else 0: they never count below
+  if constexpr (REGS > 0) {
+#pragma unroll
+    for (int u = 0; u < REGS; ++u) x[u] = u < blocks && w0 + 64 * u < n ? mass[w0 + 64 * u] : 0.f;
+#pragma unroll
+    for (int u = 0; u < REGS; ++u) {
+      const int i = w0 + 64 * u;
+      key[u] = u < blocks && i >= m0 && i < m1 ? weight_key(x[u]) : 0u;
+    }
+  }
+  auto reach = [&](uint32_t least) {  // how many rows in the middle weigh `least` > 0 or more
+    int c = 0, before;
+    if constexpr (REGS > 0) {
+#pragma unroll
+      for (int u = 0; u < REGS; ++u)
+        if (u < blocks) c += __popcll(__ballot(key[u] >= least));
+    } else {
+      for (int i0 = m0; i0 < m1; i0 += kSelectThreads)
+        c += __popcll(__ballot(i0 + tid < m1 && weight_key(mass[i0 + tid < m1 ? i0 + tid : m1 - 1]) >= least));
+    }
+    return total(c, before);
+  };
+  // rows heavier than kth stay, and of those that weigh kth the first `ties`
   uint32_t kth = 0u;
-  int before;
+  int ties = -1;
   for (int bit = 31; bit >= 0; --bit) {
     const uint32_t cnd = kth | (1u << bit);
-    int c = 0;
-    for (int i0 = m0; i0 < m1; i0 += kSelectThreads)
-      c += __popcll(__ballot(i0 + tid < m1 && weight_key(mass[i0 + tid < m1 ? i0 + tid : m1 - 1]) >= cnd));
-    if (total(c, before) >= need) kth = cnd;
-  }
-  int c = 0;
-  for (int i0 = m0; i0 < m1; i0 += kSelectThreads)
-    c += __popcll(__ballot(i0 + tid < m1 && weight_key(mass[i0 + tid < m1 ? i0 + tid : m1 - 1]) > kth));
-  int ties = need - total(c, before);  // so many of the rows that weigh kth stay, the first ones
-  int at = 0;
-  for (int i0 = 0; i0 < n; i0 += kSelectThreads) {
-    const int i = i0 + tid;
-    const float x = mass[i < n ? i : n - 1];
-    const uint32_t key = weight_key(x);
-    const bool middle = i >= m0 && i < m1;
-    const unsigned long long tie = __ballot(middle && key == kth);
-    int t0;
-    const int tied = total(__popcll(tie), t0);  // (behind its barrier every weight of this turn is in a register)
-    const bool stays = i < n && (!middle || key > kth || (key == kth && t0 + __popcll(tie & ((1ull << lane) - 1ull)) < ties));
-    const unsigned long long kept = __ballot(stays);
-    int k0;
-    const int all = total(__popcll(kept), k0);
-    if (stays) {
-      const int to = at + k0 + __popcll(kept & ((1ull << lane) - 1ull));  // to <= i
-      rows[to] = i;
-      mass_out[to] = x;
+    const int c = reach(cnd);
+    if (c < need) continue;
+    kth = cnd;
+    if (c == need) {  // exactly those
+      --kth;
+      ties = 0;
+      break;
     }
-    at += all;
-    ties -= tied < ties ? tied : ties;
+  }
+  if (ties < 0) ties = need - (kth == UINT32_MAX ? 0 : reach(kth + 1));
+  int tied_before = 0;
+  if constexpr (REGS > 0) {
+    if (ties > 0) {
+      int c = 0;
+#pragma unroll
+      for (int u = 0; u < REGS; ++u) {
+        const int i = w0 + 64 * u;
+        if (u < blocks) c += __popcll(__ballot(i >= m0 && i < m1 && key[u] == kth));
+      }
+      total(c, tied_before);
+    }
+    uint32_t kept = 0u;  // bit u: row w0 + 64 u stays
+    int c = 0, at;
+#pragma unroll
+    for (int u = 0; u < REGS; ++u) {
+      if (u >= blocks) continue;
+      const int i = w0 + 64 * u;
+      const bool middle = i >= m0 && i < m1;
+      bool stays = i < n && (!middle || key[u] > kth);
+      if (ties > 0) {
+        const unsigned long long tie = __ballot(middle && key[u] == kth);
+        stays |= middle && key[u] == kth && tied_before + __popcll(tie & ((1ull << lane) - 1ull)) < ties;
+        tied_before += __popcll(tie);
+      }
+      kept |= stays ? 1u << u : 0u;
+      c += __popcll(__ballot(stays));
+    }
+    total(c, at);  // (behind its barrier every weight is in a register)
+#pragma unroll
+    for (int u = 0; u < REGS; ++u) {
+      if (u >= blocks) continue;
+      const bool stays = (kept >> u) & 1u;
+      const unsigned long long all = __ballot(stays);
+      if (stays) {
+        const int to = at + __popcll(all & ((1ull << lane) - 1ull));
+        rows[to] = w0 + 64 * u;
+        mass_out[to] = x[u];
+      }
+      at += __popcll(all);
+    }
+  } else {
+    int at = 0;
+    for (int i0 = 0; i0 < n; i0 += kSelectThreads) {
+      const int i = i0 + tid;
+      const float w = mass[i < n ? i : n - 1];
+      const uint32_t k = weight_key(w);
+      const bool middle = i >= m0 && i < m1;
+      const unsigned long long tie = __ballot(middle && k == kth);
+      int t0, k0;
+      const int tied = total(__popcll(tie), t0);  // (behind its barrier every weight of this turn is in a register)
+      const bool stays = i < n && (!middle || k > kth || (k == kth && tied_before + t0 + __popcll(tie & ((1ull << lane) - 1ull)) < ties));
+      const unsigned long long kept = __ballot(stays);
+      const int all = total(__popcll(kept), k0);
+      if (stays) {
+        const int to = at + k0 + __popcll(kept & ((1ull << lane) - 1ull));  // to <= i
+        rows[to] = i;
+        mass_out[to] = w;
+      }
+      at += all;
+      tied_before += tied;
+    }
   }
   for (int i = a.keep + tid; i < a.Lout; i += kSelectThreads) mass_out[i] = 0.f;
 }
@@ -141,7 +213,12 @@ __global__ __launch_bounds__(1024) void evict_move_in_place_kernel(EvictArgs a) 
 
 int launch_evict(const Dims& dm, const EvictArgs& a, int B, hipStream_t st) {
   const unsigned pairs = (unsigned)B * dm.Hkv;
-  hipLaunchKernelGGL(evict_select_kernel, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+  if (a.Lloc <= 8 * kSelectThreads)
+    hipLaunchKernelGGL(evict_select_kernel<8>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+  else if (a.Lloc <= 32 * kSelectThreads)
+    hipLaunchKernelGGL(evict_select_kernel<32>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL(evict_select_kernel<0>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
   if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
   if (a.Kout == a.K) {
     if (dm.d == 128)
