@@ -1,14 +1,17 @@
 // msa_evict: of every (sequence, KV head) the rows of the cache that weigh most, the first ones and the last ones, moved together.
 //
-// Two launches.  evict_select_kernel, a workgroup to a (sequence, KV head), finds the weight of the lightest row that stays, bit by
-// bit from the top (the order-preserving image of a weight as an integer; how many rows reach a candidate is counted), then lists the
-// rows that stay in ascending order and moves their weights.  evict_move_kernel copies the rows of K and V.
+// Two launches.  evict_select_kernel, a workgroup to a (sequence, KV head), finds the weight of the lightest row that stays (as an
+// integer of the same order, in digits of 11, 11 and 10 bits from the top, each by counting), then lists the rows that stay in
+// ascending order and moves their weights.  Counted in LDS, where the order of additions changes nothing.  evict_move_kernel copies
+// the rows of K and V.
 #include "msa_device.h"
 #include "msa_host.h"
 
 namespace msa {
 
 constexpr int kSelectThreads = 1024;
+constexpr int kBins = 2048;  // values of a digit, two to a thread
+static_assert(kBins == 2 * kSelectThreads, "two bins to a thread");
 
 // The order of weights as an integer: what is no number comes last, the zeros are equal.
 __device__ __forceinline__ uint32_t weight_key(float x) {
@@ -16,11 +19,12 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
   return orderable(x == 0.f ? 0.f : x);
 }
 
-// REGS: rows of a thread, held in registers, of at most 1024 REGS in all; 0: any number, read again for every bit.
+// REGS: rows of a thread, held in registers, of at most 1024 REGS in all; 0: any number, read again for every digit.
 template <int REGS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int WAVES = kSelectThreads / 64;
-  __shared__ int cnt_s[2][WAVES];
+  __shared__ int cnt_s[2][WAVES], found[3];
+  __shared__ __attribute__((aligned(8))) int bins[kBins];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long pair = blockIdx.x;
@@ -56,43 +60,63 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   // a wave's rows are `blocks` times 64 in a row, from w0 on; without registers the workgroup's are taken 1024 at a time
   const int blocks = (n + kSelectThreads - 1) / kSelectThreads, w0 = wave * blocks * 64 + lane;
   float x[REGS > 0 ? REGS : 1];
-  uint32_t key[REGS > 0 ? REGS : 1];  // of rows in the middle, else 0: they never count below
+  uint32_t key[REGS > 0 ? REGS : 1];
   if constexpr (REGS > 0) {
 #pragma unroll
     for (int u = 0; u < REGS; ++u) x[u] = u < blocks && w0 + 64 * u < n ? mass[w0 + 64 * u] : 0.f;
 #pragma unroll
-    for (int u = 0; u < REGS; ++u) {
-      const int i = w0 + 64 * u;
-      key[u] = u < blocks && i >= m0 && i < m1 ? weight_key(x[u]) : 0u;
-    }
+    for (int u = 0; u < REGS; ++u) key[u] = weight_key(x[u]);
   }
-  auto reach = [&](uint32_t least) {  // how many rows in the middle weigh `least` > 0 or more
-    int c = 0, before;
+  // Digit by digit from the top: the rows in the middle that agree with kth so far, counted by their next digit; the lightest row
+  // that stays has the largest digit from which on there are as many as are wanted.
+  uint32_t kth = 0u;  // rows heavier than kth stay, and of those that weigh kth the first `ties`
+  int ties = need;
+  for (int shift = 21, bits = 11; need > 0; shift = shift == 21 ? 10 : 0, bits = shift == 0 ? 10 : 11) {
+    const uint32_t mask = (1u << bits) - 1u, above = shift == 21 ? 0u : ~0u << (shift + bits);
+    *reinterpret_cast<int2*>(&bins[2 * tid]) = make_int2(0, 0);
+    __syncthreads();
+    auto count = [&](uint32_t k) {
+      if (((k ^ kth) & above) == 0u) atomicAdd(&bins[(k >> shift) & mask], 1);
+    };
     if constexpr (REGS > 0) {
 #pragma unroll
-      for (int u = 0; u < REGS; ++u)
-        if (u < blocks) c += __popcll(__ballot(key[u] >= least));
+      for (int u = 0; u < REGS; ++u) {
+        const int i = w0 + 64 * u;
+        if (u < blocks && i >= m0 && i < m1) count(key[u]);
+      }
     } else {
-      for (int i0 = m0; i0 < m1; i0 += kSelectThreads)
-        c += __popcll(__ballot(i0 + tid < m1 && weight_key(mass[i0 + tid < m1 ? i0 + tid : m1 - 1]) >= least));
+      for (int i = m0 + tid; i < m1; i += kSelectThreads) count(weight_key(mass[i]));
     }
-    return total(c, before);
-  };
-  // rows heavier than kth stay, and of those that weigh kth the first `ties`
-  uint32_t kth = 0u;
-  int ties = -1;
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t cnd = kth | (1u << bit);
-    const int c = reach(cnd);
-    if (c < need) continue;
-    kth = cnd;
-    if (c == need) {  // exactly those
-      --kth;
-      ties = 0;
+    __syncthreads();
+    const int top = kBins - 1 - 2 * tid;  // this thread's two digits: top and the one below
+    const int2 two = *reinterpret_cast<const int2*>(&bins[top - 1]);
+    int upto = two.x + two.y;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int v = __shfl_up(upto, off, 64);
+      if (lane >= off) upto += v;
+    }
+    int before;
+    total(__builtin_amdgcn_readlane(upto, 63), before);
+    upto += before;  // rows of these two digits and all larger ones
+    const int over = upto - two.x - two.y;
+    if (over < ties && upto >= ties) {  // one thread's, since 0 < ties <= all that were counted
+      const bool lower = over + two.y < ties;
+      found[0] = lower ? top - 1 : top;
+      found[1] = ties - over - (lower ? two.y : 0);
+      found[2] = lower ? two.x : two.y;
+    }
+    __syncthreads();
+    kth |= (uint32_t)found[0] << shift;
+    ties = found[1];
+    if (ties == found[2]) {  // all that agree so far stay: those from kth on
+      ties = kth == 0u ? INT32_MAX : 0;
+      kth = kth == 0u ? 0u : kth - 1u;
       break;
     }
+    if (shift == 0) break;
   }
-  if (ties < 0) ties = need - (kth == UINT32_MAX ? 0 : reach(kth + 1));
+  if (need == 0) kth = UINT32_MAX;
   int tied_before = 0;
   if constexpr (REGS > 0) {
     if (ties > 0) {

@@ -221,7 +221,7 @@ struct MassArgs {
 };
 struct MassPlan {
   int tiled;               // 1: mass_tiled_kernel, 0: mass_rows_kernel
-  int n_blocks, per_wave;  // rows: workgroups of a (sequence, KV head), blocks of 32 rows of a wave
+  int n_blocks;            // rows: workgroups of a (sequence, KV head)
   int n_tiles, n_parts, tpw;
   size_t ws_bytes;
 };

@@ -6,8 +6,7 @@
 // row at the end.  Nothing depends on an order of arrival.  Queries and keys are bf16 as given, products and sums fp32: nothing is
 // rounded to fewer bits.
 //
-// mass_rows_kernel, up to 64 columns: the queries stay in registers, a wave streams blocks of 32 rows, the next one under way while
-// one is worked out.  Bound by memory: K is read once.
+// mass_rows_kernel, up to 64 columns: a wave to 32 rows, all of them and all columns in registers.  Bound by memory: K is read once.
 //
 // mass_tiled_kernel, more columns: a wave keeps 64 rows in registers, the queries come by in steps of 32 columns through LDS.  Per 64 x
 // 32 weights 16 products of 32x32x16 (d = 128) stand against 96 vector instructions of which 32 are exponentials at a quarter of the
@@ -38,17 +37,28 @@ __device__ __forceinline__ float old_weight(const MassArgs& a, long long at) {
 }
 
 // ---- few columns ---------------------------------------------------------------------------------------------------------
+// (A wave to 32 rows and eight of them to a SIMD: 40 sequences of 8192 rows, 8 heads of 128, 115 us, 6.0 TB/s, of 0 to 8192 rows,
+// 4000 on average, 83.  Waves that go on through 64 to 512 rows with one or two blocks ahead 120 to 139 and 88 to 93; 64 rows at once
+// 119 and 96; workgroups by rows first and sequences second 127 and 79.)
 template <int D, int CG>  // CG: groups of 16 columns
-__global__ __launch_bounds__(256) void mass_rows_kernel(MassArgs a, int n_blocks, int per_wave) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 : 1))) void mass_rows_kernel(MassArgs a, int n_blocks) {
   constexpr int NS = D / 32;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qd = lane >> 4, n = lane & 15, r = a.r;
   const long long pair = blockIdx.x / n_blocks;
-  const int first = (int)(blockIdx.x % n_blocks) * 4 * per_wave + wave;  // the wave's blocks: first, first + 4, ...
+  const int t0 = ((int)(blockIdx.x % n_blocks) * 4 + wave) * 32;
+  if (t0 >= a.Lloc) return;  // no barrier below
   const int g = (int)(pair % a.Hkv);
   const long long b = pair / a.Hkv;
   const int cols = a.M * r;
+  const bool weighed = a.mass != nullptr && a.decay != 0.f;
+  float old[2];  // of row 4 qd + n % 4 of either half of the 32
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int t = t0 + 16 * k + 4 * qd + (n & 3);
+    old[k] = weighed ? a.mass[pair * a.Lloc + (t < a.Lloc ? t : a.Lloc - 1)] : 0.f;
+  }
   bf16x8_t q[CG][NS];
   float ls[CG];
   SeenBy see[CG];
@@ -70,62 +80,53 @@ __global__ __launch_bounds__(256) void mass_rows_kernel(MassArgs a, int n_blocks
     most = v > most ? v : most;
   }
   most = __builtin_amdgcn_readfirstlane(most);
-  const uint16_t* const keys = a.Kloc + pair * a.Lloc * D + 8 * qd;
-  u32x4_t k[2][NS];
-  auto load = [&](int t0) __attribute__((always_inline)) {
+  if (t0 > most && a.mass == a.out && a.decay == 1.f) return;  // rows that nobody sees, in place: as they are
+  float sum[2][4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      int row = t0 + 16 * t + n;
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[k][i] = 0.f;
+  if (t0 <= most) {  // wave-uniform
+    const uint16_t* const keys = a.Kloc + pair * a.Lloc * D + 8 * qd;
+    u32x4_t key[2][NS];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      int row = t0 + 16 * k + n;
       row = row <= most ? row : most;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) k[t][s] = *reinterpret_cast<const u32x4_t*>(keys + (long long)row * D + 32 * s);
+      for (int s = 0; s < NS; ++s) key[k][s] = *reinterpret_cast<const u32x4_t*>(keys + (long long)row * D + 32 * s);
     }
-  };
-  if (32 * first <= most) load(32 * first);
-  for (int i = 0; i < per_wave; ++i) {
-    const int t0 = 32 * (first + 4 * i);
-    if (t0 >= a.Lloc) break;
-    float sum[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-    if (t0 <= most) {  // wave-uniform
-      f32x4_t sc[CG][2];
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int c = 0; c < CG; ++c) {
-        sc[c][0] = sc[c][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          sc[c][0] = mfma16(__builtin_bit_cast(bf16x8_t, k[0][s]), q[c][s], sc[c][0]);
-          sc[c][1] = mfma16(__builtin_bit_cast(bf16x8_t, k[1][s]), q[c][s], sc[c][1]);
+        for (int s = 0; s < NS; ++s) sc = mfma16(__builtin_bit_cast(bf16x8_t, key[k][s]), q[c][s], sc);
+        const int t = t0 + 16 * k + 4 * qd;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(sc[i], a.qscale, -ls[c]));
+          sum[k][i] += (t + i <= see[c].p) & ((t + i >= see[c].lo) | (t + i < a.sinks)) ? w : 0.f;
         }
       }
-      if (i + 1 < per_wave && t0 + 128 <= most) load(t0 + 128);
+  }
 #pragma unroll
-      for (int c = 0; c < CG; ++c)
+  for (int k = 0; k < 2; ++k) {
+    float v = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = t0 + 16 * (j >> 2) + 4 * qd + (j & 3);
-          const float w = __builtin_amdgcn_exp2f(fmaf(sc[c][j >> 2][j & 3], a.qscale, -ls[c]));
-          sum[j] += (t <= see[c].p) & ((t >= see[c].lo) | (t < a.sinks)) ? w : 0.f;
-        }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] = add_over_16(sum[j]);
+    for (int i = 0; i < 4; ++i) {
+      const float s = add_over_16(sum[k][i]);
+      v = (n & 3) == i ? s : v;
     }
-    if (n < 8) {
-      float v = sum[0];
-#pragma unroll
-      for (int j = 1; j < 8; ++j) v = n == j ? sum[j] : v;
-      const int t = t0 + 16 * (n >> 2) + 4 * qd + (n & 3);
-      if (t < a.Lloc && (t0 <= most || a.mass != a.out || a.decay != 1.f)) {  // (rows that nobody sees, in place: as they are)
-        const long long at = pair * a.Lloc + t;
-        a.out[at] = old_weight(a, at) + v;
-      }
-    }
+    const int t = t0 + 16 * k + 4 * qd + (n & 3);
+    if (n < 4 && t < a.Lloc) a.out[pair * a.Lloc + t] = weighed ? old[k] * a.decay + v : v;
   }
 }
 
 // ---- many columns --------------------------------------------------------------------------------------------------------
-constexpr int kMassRows = 64;    // rows of a wave
+constexpr int kMassRows = 32;    // rows of a wave
+constexpr int kMassWaves = 4;
 constexpr int kMassStages = 3;
 constexpr long long kMassItems = 2048;  // fewer tiles than this: their columns in parts
 
@@ -135,14 +136,15 @@ struct MassParts {
 };
 
 template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void mass_tiled_kernel(MassArgs a, MassParts pp) {
-  constexpr int NP = D / 8, NS = D / 16, ROW = D * 2;
+__global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu(3))) void mass_tiled_kernel(MassArgs a, MassParts pp) {
+  constexpr int NW = kMassWaves, NP = D / 8, NS = D / 16, ROW = D * 2;
   constexpr int KT = kMassRows / 32;
   constexpr int TILE = 32 * ROW;          // bytes of a step's queries
-  constexpr int NPW = 32 * NP / 64 / 4;   // copies of a wave per step
-  constexpr int SIDE = 4 * 256;           // behind them, for every wave: 32 log-sums and 32 positions
+  constexpr int NPW = 32 * NP / 64 / NW;  // copies of a wave per step
+  static_assert(NPW >= 1, "a step is a whole number of copies per wave");
+  constexpr int SIDE = NW * 256;           // behind them, for every wave: 32 log-sums and 32 positions
   __shared__ __attribute__((aligned(16))) unsigned char smem[kMassStages * (TILE + SIDE)];
-  __shared__ int lo_s[4], hi_s[4];
+  __shared__ int lo_s[NW], hi_s[NW];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hf = lane >> 5, col = lane & 31, r = a.r;
@@ -153,12 +155,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void m
   x /= pp.n_parts;
   const int tile = x % pp.n_tiles;
   const long long b = x / pp.n_tiles, pair = b * a.Hkv + g;
-  const int tile0 = tile * 4 * kMassRows, t0 = tile0 + wave * kMassRows;
+  const int tile0 = tile * NW * kMassRows, t0 = tile0 + wave * kMassRows;
 
   // steps with a token that sees a row of the tile: from the first to the last of them
-  const int tile1 = (tile0 + 4 * kMassRows < a.Lloc ? tile0 + 4 * kMassRows : a.Lloc) - 1;
+  const int tile1 = (tile0 + NW * kMassRows < a.Lloc ? tile0 + NW * kMassRows : a.Lloc) - 1;
   int s_lo = INT32_MAX, s_hi = -1;
-  for (int m = tid; m < a.M; m += 256) {
+  for (int m = tid; m < a.M; m += NW * 64) {
     const SeenBy s = seen_by(a, a.q_pos[b * a.M + m]);
     if (s.p >= tile0 && (s.lo <= tile1 || tile0 < a.sinks)) {
       s_lo = s_lo < m ? s_lo : m;
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void m
   }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     s_lo = lo_s[w] < s_lo ? lo_s[w] : s_lo;
     s_hi = hi_s[w] > s_hi ? hi_s[w] : s_hi;
   }
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void m
     int ctok[NPW], coff[NPW];
 #pragma unroll
     for (int i = 0; i < NPW; ++i) {
-      const int y = (i * 4 + wave) * 64 + lane, row = y / NP;
+      const int y = (i * NW + wave) * 64 + lane, row = y / NP;
       int c = row;
       if (c >= pp.tpw * r) c = 0;
       ctok[i] = c / r;
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void m
       for (int i = 0; i < NPW; ++i) {
         const int t = ctok[i] < left ? ctok[i] : left;
         copy16_to_lds_async_at(q0 + (long long)m0 * a.Hq * D, t * a.Hq * ROW + coff[i],
-                               lds0 + INTO * (TILE + SIDE) + (i * 4 + wave) * 1024);
+                               lds0 + INTO * (TILE + SIDE) + (i * NW + wave) * 1024);
       }
       int t = col_ok ? my_tok : 0;
       t = t < left ? t : left;
@@ -330,16 +332,13 @@ MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks
   const long long pairs = (long long)B * dm.Hkv;
   p.ws_bytes = 256;
   if (M * dm.r <= 64) {
-    const long long blocks = (Lloc + 31) / 32;
-    p.per_wave = 1;
-    while (p.per_wave < 8 && pairs * blocks / (p.per_wave * 2) >= 4096) p.per_wave *= 2;
-    p.n_blocks = (int)((blocks + 4 * p.per_wave - 1) / (4 * p.per_wave));
+    p.n_blocks = (Lloc + 127) / 128;
     if (pairs * p.n_blocks >= 1 << 24) p.ws_bytes = 0;
     return p;
   }
   p.tiled = 1;
   p.tpw = 32 / dm.r;
-  p.n_tiles = (Lloc + 4 * kMassRows - 1) / (4 * kMassRows);
+  p.n_tiles = (Lloc + kMassWaves * kMassRows - 1) / (kMassWaves * kMassRows);
   const long long tiles = pairs * p.n_tiles, steps = (M + p.tpw - 1) / p.tpw;
   long long n = (kMassItems + tiles - 1) / tiles, most = steps / 16 < 32 ? steps / 16 : 32;
   if (n > most) n = most;
@@ -349,7 +348,7 @@ MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks
     return p;
   }
   // (tiles in parts are fewer than kMassItems, so less than twice as many workgroups in all; no less for a longer cache)
-  const long long sums = most * pairs * Lloc, bound = 2 * kMassItems * 4 * kMassRows;
+  const long long sums = most * pairs * Lloc, bound = 2 * kMassItems * kMassWaves * kMassRows;
   if (most > 1) p.ws_bytes = round_up256((size_t)(sums < bound ? sums : bound) * sizeof(float));
   return p;
 }
@@ -363,7 +362,7 @@ int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws,
   if (!pl.tiled) {
     const dim3 grid((unsigned)(pairs * pl.n_blocks)), block(256);
     const int groups = (a.M * dm.r + 15) / 16;
-#define MSA_MASS(DD, CC) hipLaunchKernelGGL((mass_rows_kernel<DD, CC>), grid, block, 0, st, a, pl.n_blocks, pl.per_wave)
+#define MSA_MASS(DD, CC) hipLaunchKernelGGL((mass_rows_kernel<DD, CC>), grid, block, 0, st, a, pl.n_blocks)
 #define MSA_MASS_OF(DD)            \
   if (groups == 1) MSA_MASS(DD, 1); \
   else if (groups == 2) MSA_MASS(DD, 2); \
@@ -380,9 +379,9 @@ int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws,
   const MassParts pp = {(float*)ws, pl.n_parts, pl.n_tiles, pl.tpw};
   const dim3 grid((unsigned)(pairs * pl.n_tiles * pl.n_parts));
   if (dm.d == 128)
-    hipLaunchKernelGGL(mass_tiled_kernel<128>, grid, dim3(256), 0, st, a, pp);
+    hipLaunchKernelGGL(mass_tiled_kernel<128>, grid, dim3(kMassWaves * 64), 0, st, a, pp);
   else
-    hipLaunchKernelGGL(mass_tiled_kernel<64>, grid, dim3(256), 0, st, a, pp);
+    hipLaunchKernelGGL(mass_tiled_kernel<64>, grid, dim3(kMassWaves * 64), 0, st, a, pp);
   if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
   if (pl.n_parts > 1) {
     const long long n = pairs * a.Lloc;
