@@ -161,6 +161,8 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
     uint4 v = *reinterpret_cast<const uint4*>(qp + 16 * s);
     if (!ok) v = make_uint4(0, 0, 0, 0);
     bq[s] = as_bf16x8(v);
+    // (waited for here: at their first use, in the loop, the wait would be one for all copies in flight as well)
+    asm volatile("" : "+v"(bq[s]));
   }
 
   // Places of the 16-byte pieces of a row in LDS: piece p of row i lies at p ^ swz(i).  What a lane reads of slice s (keys) or
