@@ -46,7 +46,7 @@ struct EncodedPlan {
 // cache that a token can see.  ws_bytes is 0 where the grid does not hold the call: one workgroup per token in its third
 // dimension, or tiles in its first, whose threads count to 2^32.
 EncodedPlan plan_encoded(const Dims& dm, int B, int M, long long mem_rows, bool shared, long long local_rows, int Lloc);
-// The same for rows in common that are in bf16 already (a prefix) and need no room to be expanded.
+// The tiled kernel for rows in common that are in bf16 already (a prefix) and need no room to be expanded.
 EncodedPlan plan_encoded_prefix(const Dims& dm, int B, int M, long long mem_rows, int Lloc);
 int launch_encoded(const Dims& dm, const EncodedPlan& pl, EncodedArgs a, int B, void* ws, hipStream_t st);
 int launch_encoded_tiled(const Dims& dm, const EncodedArgs& a, TiledArgs ta, int B, hipStream_t st);

@@ -389,7 +389,7 @@ static EncodedPlan plan_of(const Dims& dm, int B, int M, long long mem_rows, boo
   // the right, which applies from M = 8 on.)
   const long long steps_mem = (mem_rows + 31) / 32, cost = steps_mem + kLocalCost * ((local_rows + 31) / 32);
   const long long work = pairs * cost, least = 20000 + 8 * pairs / M * steps_mem;
-  p.tiled = (mem_rows == 0 || shared) && (M >= 32 || (M >= (mem_rows > 0 ? 8 : 4) && work >= least)) ? 1 : 0;
+  p.tiled = !expand || ((mem_rows == 0 || shared) && (M >= 32 || (M >= (mem_rows > 0 ? 8 : 4) && work >= least))) ? 1 : 0;
   int n_most;  // splits that the workspace holds: grows with the rows, so that one sized for the longest call serves all
   long long most1 = (cost + 15) / 16;
   if (most1 > 2048 / pairs) most1 = 2048 / pairs;
@@ -458,7 +458,7 @@ static EncodedPlan plan_of(const Dims& dm, int B, int M, long long mem_rows, boo
     p.off_tickets = take(counters * sizeof(unsigned long long));
   };
   size_t single = 0;
-  if (p.tiled && M < 32) {  // what a shorter call, which takes its tokens one by one, asks for
+  if (p.tiled && expand && M < 32) {  // what a shorter call, which takes its tokens one by one, asks for
     take_parts(single_most, rows, dm.d, 1, (size_t)pairs);
     single = at;
     at = 0;

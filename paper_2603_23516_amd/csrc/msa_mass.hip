@@ -25,11 +25,11 @@ struct SeenBy {
   int p, lo;
 };
 __device__ __forceinline__ SeenBy seen_by(const MassArgs& a, int32_t q_pos) {
-  const long long pl = (long long)q_pos - a.pos0;
+  const int pl = __builtin_elementwise_sub_sat(q_pos, a.pos0);  // (saturated: in front of the cache all the same)
   SeenBy s;
-  s.p = pl < -1 ? -1 : (pl < a.Lloc ? (int)pl : a.Lloc - 1);
-  const long long lo = pl - a.window + 1;
-  s.lo = lo < 0 ? 0 : (lo < a.Lloc ? (int)lo : a.Lloc);
+  s.p = pl < -1 ? -1 : (pl < a.Lloc ? pl : a.Lloc - 1);
+  const int lo = __builtin_elementwise_sub_sat(pl, a.window - 1);
+  s.lo = lo < 0 ? 0 : lo;
   return s;
 }
 __device__ __forceinline__ float old_weight(const MassArgs& a, long long at) {
@@ -222,26 +222,31 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
       ctok[i] = c / r;
       coff[i] = (c % r) * ROW + ((y % NP) ^ swz(row)) * 16;
     }
-    const int my_tok = col / r, my_head = col - my_tok * r;
+    int my_tok = col / r, my_head = col - my_tok * r;
     const bool col_ok = my_tok < pp.tpw;
+    if (!col_ok) my_tok = my_head = 0;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem));
-    const uint16_t* const q0 = a.q + (b * a.M * a.Hq + g * r) * D;
-    auto issue = [&](int s, auto stage) __attribute__((always_inline)) {
+    // where the next step's queries, and this lane's log-sum (lanes below 32) or position, come from
+    const long long m1 = b * a.M + (long long)sb * pp.tpw;
+    const int tok_bytes = a.Hq * ROW, side_bytes = hf == 0 ? a.Hq * 4 : 4;
+    const unsigned char* n_q = reinterpret_cast<const unsigned char*>(a.q + (m1 * a.Hq + g * r) * D);
+    const unsigned char* n_side = hf == 0 ? reinterpret_cast<const unsigned char*>(a.lse + m1 * a.Hq + g * r + my_head)
+                                          : reinterpret_cast<const unsigned char*>(a.q_pos + m1);
+    int n_left = a.M - 1 - sb * pp.tpw;  // tokens behind the step's first one
+    auto issue = [&](auto stage) __attribute__((always_inline)) {
       constexpr int INTO = decltype(stage)::value;
-      const int m0 = s * pp.tpw, left = a.M - 1 - m0;  // left >= 0
 #pragma unroll
       for (int i = 0; i < NPW; ++i) {
-        const int t = ctok[i] < left ? ctok[i] : left;
-        copy16_to_lds_async_at(q0 + (long long)m0 * a.Hq * D, t * a.Hq * ROW + coff[i],
-                               lds0 + INTO * (TILE + SIDE) + (i * NW + wave) * 1024);
+        const int t = ctok[i] < n_left ? ctok[i] : n_left;
+        copy16_to_lds_async_at(n_q, t * tok_bytes + coff[i], lds0 + INTO * (TILE + SIDE) + (i * NW + wave) * 1024);
       }
-      int t = col_ok ? my_tok : 0;
-      t = t < left ? t : left;
-      const long long tok = b * a.M + m0 + t;
-      const void* const src = hf == 0 ? (const void*)(a.lse + tok * a.Hq + g * r + (col_ok ? my_head : 0))
-                                      : (const void*)(a.q_pos + tok);
-      copy4_to_lds_async64(src, lds0 + INTO * (TILE + SIDE) + TILE + wave * 256);
+      const int t = my_tok < n_left ? my_tok : n_left;
+      copy4_to_lds_async64(n_side + t * side_bytes, lds0 + INTO * (TILE + SIDE) + TILE + wave * 256);
+      n_q += (long long)pp.tpw * tok_bytes;
+      n_side += (long long)pp.tpw * side_bytes;
+      n_left -= pp.tpw;
     };
+    int left = a.M - sb * pp.tpw;  // tokens from the step's first one on
     auto step = [&](int s, auto stage) __attribute__((always_inline)) {
       constexpr int BUF = decltype(stage)::value;
       const unsigned char* const st = smem + BUF * (TILE + SIDE);
@@ -250,16 +255,17 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
       else
         wait_copies_but<0>();
       lds_barrier();
-      if (s + 2 < se) issue(s + 2, std::integral_constant<int, (BUF + 2) % kMassStages>());
+      if (s + 2 < se) issue(std::integral_constant<int, (BUF + 2) % kMassStages>());
       const float* const side = reinterpret_cast<const float*>(st + TILE + wave * 256);
       float nls = -side[col] * kLog2e;
       SeenBy see = seen_by(a, __float_as_int(side[32 + col]));
-      const bool there = col_ok && my_tok < a.M - s * pp.tpw;
-      if (!there || nls == INFINITY) see.p = -1;  // (a token that saw nothing)
-      const bool any = see.p >= t0 && (see.lo < t0 + kMassRows || t0 < a.sinks);
-      if (__ballot(any) == 0) return;
+      const bool there = col_ok & (my_tok < left);
+      left -= pp.tpw;
+      if (!there | (nls == INFINITY)) see.p = -1;  // (a token that saw nothing)
       // seen whole by all columns that are there; the others weigh exp2(-inf)
-      const bool whole = __ballot(there && !(see.p >= t0 + kMassRows - 1 && (see.lo <= t0 || t0 + kMassRows <= a.sinks))) == 0;
+      const bool whole =
+          __builtin_amdgcn_ballot_w64(there & !((see.p >= t0 + kMassRows - 1) & ((see.lo <= t0) | (t0 + kMassRows <= a.sinks)))) == 0;
+      if (!whole && __builtin_amdgcn_ballot_w64((see.p >= t0) & ((see.lo < t0 + kMassRows) | (t0 < a.sinks))) == 0) return;
       if (!there) nls = -INFINITY;
       f32x16e_t sc[KT];
 #pragma unroll
@@ -289,8 +295,13 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
           }
       }
     };
-    issue(sb, std::integral_constant<int, 0>());
-    if (sb + 1 < se) issue(sb + 1, std::integral_constant<int, 1>());
+    // (the rows are waited for here: at their first use, in the loop, the wait would be one for all copies in flight as well)
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int i = 0; i < NS; ++i) asm volatile("" : "+v"(key[k][i]));
+    issue(std::integral_constant<int, 0>());
+    if (sb + 1 < se) issue(std::integral_constant<int, 1>());
     for (int s = sb; s < se; s += kMassStages) {  // stages by number, so that LDS addresses are constants
       step(s, std::integral_constant<int, 0>());
       if (s + 1 < se) step(s + 1, std::integral_constant<int, 1>());
@@ -340,7 +351,7 @@ MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks
   p.tpw = 32 / dm.r;
   p.n_tiles = (Lloc + kMassWaves * kMassRows - 1) / (kMassWaves * kMassRows);
   const long long tiles = pairs * p.n_tiles, steps = (M + p.tpw - 1) / p.tpw;
-  long long n = (kMassItems + tiles - 1) / tiles, most = steps / 16 < 32 ? steps / 16 : 32;
+  long long n = (kMassItems + tiles - 1) / tiles, most = steps / 8 < 32 ? steps / 8 : 32;
   if (n > most) n = most;
   p.n_parts = (int)(n < 1 ? 1 : n);
   if (tiles * p.n_parts >= 1 << 24) {

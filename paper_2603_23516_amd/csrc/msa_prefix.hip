@@ -14,6 +14,7 @@
 #include "msa_prefix.h"
 
 #include <type_traits>
+#include <utility>
 
 namespace msa {
 
@@ -121,11 +122,18 @@ __device__ __forceinline__ void attend_rows(const uint16_t* K, const uint16_t* V
   }
 }
 
+constexpr int kPrefixParts = 192;  // of a row at most, 32 of them over the cache
 constexpr int kPrefixStages = 3;
+constexpr int kPrefixWaves = 4;
+
+template <int... I, class F>
+__device__ __forceinline__ void each_stage(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
 
 template <int D>
 __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned char* smem) {
-  constexpr int NW = 4;
+  constexpr int NW = kPrefixWaves, AHEAD = kPrefixStages - 1;  // steps whose copies are under way
   constexpr int NP = D / 8;            // 16-byte pieces per row
   constexpr int NS = D / 16;           // contraction slices of the score product
   constexpr int NT = D / 32;           // 32-row tiles of the output product
@@ -165,7 +173,7 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
   end = __builtin_amdgcn_readfirstlane(end);
   __syncthreads();  // (the copies come to the same place)
   const int steps = (end + 31) / 32;
-  const int sb = (int)((long long)steps * sp / a.n_pre), se = (int)((long long)steps * (sp + 1) / a.n_pre);
+  const int se = (steps - sp + a.n_pre - 1) / a.n_pre;  // this part's steps: sp, sp + n_pre, ...
 
   bf16x8_t bq[NS];
   const long long qh = (ok ? tok : 0) * a.Hq + g * r + (ok ? head : 0);
@@ -174,6 +182,8 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
     uint4 v = *reinterpret_cast<const uint4*>(a.q + qh * D + 8 * hf + 16 * s);
     if (!ok) v = make_uint4(0, 0, 0, 0);
     bq[s] = as_bf16x8(v);
+    // (waited for here: at their first use, in the loop, the wait would be one for all copies in flight as well)
+    asm volatile("" : "+v"(bq[s]));
   }
 
   // Places of the 16-byte pieces of a row in LDS: piece p of row i lies at p ^ swz(i), so that the reads meet no bank twice.
@@ -193,9 +203,9 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
     coff[i] = row * ROW + ((y % NP) ^ (j < NI ? swz_k(row) : swz_v(row))) * 16;
   }
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + wave * 1024);
-  const long long at0 = ((long long)g * a.Lpre + 32LL * sb) * D;
+  const long long at0 = ((long long)g * a.Lpre + 32LL * sp) * D;
   const uint16_t *n_k = a.Kpre + at0, *n_v = a.Vpre + at0;
-  int n_cnt = end - 32 * sb;  // rows from the next copy's first one on
+  int n_cnt = end - 32 * sp;  // rows from the next copy's first one on
   auto issue = [&](auto stage) __attribute__((always_inline)) {
     constexpr int INTO = decltype(stage)::value;
 #pragma unroll
@@ -209,9 +219,9 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
       }
       copy16_to_lds_async_at(src, off, lds0 + INTO * 2 * TILE + i * NW * 1024);
     }
-    n_cnt -= 32;
-    n_k += 32 * D;
-    n_v += 32 * D;
+    n_cnt -= 32 * a.n_pre;
+    n_k += (long long)a.n_pre * 32 * D;
+    n_v += (long long)a.n_pre * 32 * D;
   };
 
   float m_run = -INFINITY, l_run = 0.f;
@@ -224,14 +234,14 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
   auto step = [&](int s, auto stage) __attribute__((always_inline)) {
     constexpr int BUF = decltype(stage)::value;
     unsigned char* const st = smem + BUF * 2 * TILE;
-    if (s + 1 < se)
-      wait_copies_but<NPW>();
+    if (s + AHEAD - 1 < se)
+      wait_copies_but<(AHEAD - 1) * NPW>();
     else
       wait_copies_but<0>();
     // step s is staged for everyone; everyone is done with step s - 1's stage (its LDS reads have come back)
     lds_barrier();
-    if (s + 2 < se) issue(std::integral_constant<int, (BUF + 2) % kPrefixStages>());
-    const int t0 = 32 * s;
+    if (s + AHEAD < se) issue(std::integral_constant<int, (BUF + AHEAD) % kPrefixStages>());
+    const int t0 = 32 * (sp + s * a.n_pre);
     if (t0 >= most) return;  // this wave sees nothing of the step (uniform)
     f32x16e_t sc;
 #pragma unroll
@@ -277,13 +287,14 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
       }
     }
   };
-  if (sb < se) issue(std::integral_constant<int, 0>());
-  if (sb + 1 < se) issue(std::integral_constant<int, 1>());
-  for (int s = sb; s < se; s += kPrefixStages) {  // stages by number, so that LDS addresses are constants
-    step(s, std::integral_constant<int, 0>());
-    if (s + 1 < se) step(s + 1, std::integral_constant<int, 1>());
-    if (s + 2 < se) step(s + 2, std::integral_constant<int, 2>());
-  }
+  // stages by number, so that LDS addresses are constants
+  each_stage(std::make_integer_sequence<int, AHEAD>(), [&](auto stage) {
+    if (decltype(stage)::value < se) issue(stage);
+  });
+  for (int s = 0; s < se; s += kPrefixStages)
+    each_stage(std::make_integer_sequence<int, kPrefixStages>(), [&](auto stage) __attribute__((always_inline)) {
+      if (s + decltype(stage)::value < se) step(s + decltype(stage)::value, stage);
+    });
   const uint32_t u = __float_as_uint(l_run);
   const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
@@ -301,12 +312,12 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
 
 template <int D>
 __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned char* smem) {
-  constexpr int NS = D / 32, NC = D / 16;
+  constexpr int NW = kPrefixWaves, NS = D / 32, NC = D / 16;
   constexpr int OROW = D + 4;  // floats of a row of a wave's output in the merge
   constexpr int STAGE = 16 * OROW * 4;
   static_assert(STAGE >= 32 * D * 2, "32 value rows");
-  float* const wm = reinterpret_cast<float*>(smem + 4 * STAGE);  // [4][16] maxima, [4][16] sums
-  float* const wl = wm + 64;
+  float* const wm = reinterpret_cast<float*>(smem + NW * STAGE);  // [NW][16] maxima, sums
+  float* const wl = wm + 16 * NW;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qd = lane >> 4, n = lane & 15, r = a.r;
@@ -345,9 +356,9 @@ __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned 
 #pragma unroll
   for (int c = 0; c < NC; ++c) y.o[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   const long long loc = (b * a.Hkv + g) * a.Lloc * D;
-  attend_rows<D>(a.Kloc + loc, a.Vloc + loc, most, sb + wave, se, 4, bq, lim, least, a.qscale, smem + wave * STAGE, y);
+  attend_rows<D>(a.Kloc + loc, a.Vloc + loc, most, sb + wave, se, NW, bq, lim, least, a.qscale, smem + wave * STAGE, y);
 
-  // the four waves' results
+  // the waves' results
   y.l_run = add_xor32(add_xor16(y.l_run));
   float* const mine = reinterpret_cast<float*>(smem + wave * STAGE);
 #pragma unroll
@@ -357,17 +368,17 @@ __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned 
     wl[16 * wave + n] = y.l_run;
   }
   __syncthreads();
-  for (int e = tid; e < 16 * D / 4; e += 256) {
+  for (int e = tid; e < 16 * D / 4; e += 64 * NW) {
     const int c = e / (D / 4), dd = e % (D / 4) * 4, t = c / r;
     if (t >= a.tpl || m0 + t >= a.M) continue;
     const long long ph = ((b * a.M + m0 + t) * a.Hq + g * r + (c - t * r)) * a.n_loc + sp;
     float m = wm[c];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) m = fmaxf(m, wm[16 * w + c]);
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, wm[16 * w + c]);
     float l = 0.f;
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float f = wm[16 * w + c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[16 * w + c] - m);
       l += f * wl[16 * w + c];
       v += f * *reinterpret_cast<const f32x4_t*>(smem + w * STAGE + (c * OROW + dd) * 4);
@@ -378,9 +389,9 @@ __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned 
 }
 
 template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void prefix_kernel(PrefixArgs a) {
+__global__ __launch_bounds__(64 * kPrefixWaves) __attribute__((amdgpu_waves_per_eu(3))) void prefix_kernel(PrefixArgs a) {
   constexpr int BYTES = kPrefixStages * 2 * 32 * D * 2;
-  constexpr int CACHE = 4 * 16 * (D + 4) * 4 + 512;
+  constexpr int CACHE = kPrefixWaves * (16 * (D + 4) * 4 + 128);
   __shared__ __attribute__((aligned(16))) unsigned char smem[BYTES > CACHE ? BYTES : CACHE];
   if ((int)blockIdx.x < a.pre_groups)
     over_prefix<D>(a, blockIdx.x, smem);
@@ -388,9 +399,91 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
     over_cache<D>(a, blockIdx.x - a.pre_groups, smem);
 }
 
+// The parts of every (token, head): a workgroup to a row, its waves the parts i, i + 4, ..., eight of them at a time under way
+// together with all (max, sum) pairs.  (A wave to a row, as the other paths join theirs, is one part after another where rows are few
+// and parts many: 256 rows of 68 parts 22 us, 2048 of 33 13.)
+template <int D>
+__global__ __launch_bounds__(256) void prefix_join_kernel(PrefixArgs a) {
+  constexpr int V = D / 64, U = 8;
+  typedef float vec_t __attribute__((ext_vector_type(V)));
+  __shared__ float o_s[4][D];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long row = blockIdx.x;
+  const int n1 = a.n_pre, ns = n1 + a.n_loc;
+  const float2 *const m1 = a.pre_ml + row * n1, *const m2 = a.loc_ml + row * a.n_loc;
+  const float *const p1 = a.pre_o + row * n1 * D + lane * V, *const p2 = a.loc_o + row * a.n_loc * D + lane * V;
+  vec_t v[U];
+  auto fetch = [&](int s0) {  // (past the end: the last one again)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + 4 * u < ns ? s0 + 4 * u : ns - 1;
+      v[u] = *reinterpret_cast<const vec_t*>(s < n1 ? p1 + (long long)s * D : p2 + (long long)(s - n1) * D);
+    }
+  };
+  float2 ml[kPrefixParts / 64];
+#pragma unroll
+  for (int i = 0; i < kPrefixParts / 64; ++i) {
+    const int s = lane + 64 * i;
+    ml[i] = make_float2(-INFINITY, 0.f);
+    if (64 * i < ns && s < ns) ml[i] = s < n1 ? m1[s] : m2[s - n1];
+  }
+  fetch(wave);
+  float mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kPrefixParts / 64; ++i) mx = fmaxf(mx, ml[i].x);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
+  float lsum = 0.f, w[kPrefixParts / 64];
+#pragma unroll
+  for (int i = 0; i < kPrefixParts / 64; ++i) {
+    const bool empty = ml[i].x == -INFINITY;  // (its outputs may be anything)
+    w[i] = empty ? -1.f : __builtin_amdgcn_exp2f(ml[i].x - mx);
+    lsum += empty ? 0.f : w[i] * ml[i].y;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) lsum += __shfl_xor(lsum, off, 64);
+  vec_t acc = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPrefixParts / 64; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {  // parts 64 i + 32 j + wave, + 4, ... of this wave
+      const int s0 = 64 * i + 32 * j;
+      if (s0 + wave >= ns) continue;
+      if (s0 > 0) fetch(s0 + wave);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w[i]), 32 * j + wave + 4 * u));
+        if (s0 + wave + 4 * u < ns && f >= 0.f) acc += f * v[u];  // wave-uniform
+      }
+    }
+#pragma unroll
+  for (int c = 0; c < V; ++c) o_s[wave][lane * V + c] = acc[c];
+  __syncthreads();
+  if (threadIdx.x < D / 2) {
+    const int d = 2 * threadIdx.x;
+    float x0 = 0.f, x1 = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      x0 += o_s[u][d];
+      x1 += o_s[u][d + 1];
+    }
+    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+    reinterpret_cast<uint32_t*>(a.out + row * D)[threadIdx.x] = pack_bf16(x0 * inv, x1 * inv);
+    if (threadIdx.x == 0 && a.lse != nullptr) a.lse[row] = lsum > 0.f ? (mx + log2f(lsum)) * 0.6931471805599453f : -INFINITY;
+  }
+}
+
 PrefixPlan plan_prefix(const Dims& dm, int B, int M, int Lpre, int Lloc) {
   PrefixPlan p = {};
-  if (M >= 32 && M * dm.r >= 128) {
+  // A sequence's tokens in tiles of their own, where they fill three quarters of one and the batch fills three.  us, so / with tiles of
+  // all sequences' tokens, 32 / 8 heads of 128, 600 rows of a cache, a prefix of 2000 (16384):
+  //   1 sequence    M = 32 21 / 16 (37 / 30), 48 22 / 21 (43 / 41)
+  //   2 sequences   M = 24 21 / 21 (44 / 41), 48 27 / 29 (58 / 66)
+  //   8 sequences   M = 16 27 / 32 (99 / 75), 24 30 / 42 (91 / 115), 48 43 / 71 (155 / 202)
+  //   32 sequences  M = 12 58 / 72 (268 / 205), 24 63 / 115 (288 / 323), 48 98 / 204 (540 / 566)
+  //   4 sequences, 8 / 8 heads of 64, 4000   M = 64 22 / 16, 128 25 / 23
+  if (M * dm.r >= 96 && (long long)B * M * dm.r >= 384) {
     p.tiled = 1;
     p.tiles = plan_encoded_prefix(dm, B, M, Lpre, Lloc);
     p.ws_bytes = p.tiles.ws_bytes;
@@ -398,14 +491,14 @@ PrefixPlan plan_prefix(const Dims& dm, int B, int M, int Lpre, int Lloc) {
   }
   const long long BM = (long long)B * M, rows = BM * dm.Hq;
   const int tpw = 32 / dm.r, tpl = 16 / dm.r;
-  const long long tiles = (BM + 4 * tpw - 1) / (4 * tpw) * dm.Hkv, groups = (long long)B * ((M + tpl - 1) / tpl) * dm.Hkv;
+  const long long tiles = (BM + kPrefixWaves * tpw - 1) / (kPrefixWaves * tpw) * dm.Hkv, groups = (long long)B * ((M + tpl - 1) / tpl) * dm.Hkv;
   if (tiles + groups >= 1 << 22) return p;
   auto parts = [](long long steps, long long units, long long wanted, long long least, int most) {
     long long n = (wanted + units - 1) / units;
     if (n > steps / least) n = steps / least;
     return (int)(n < 1 ? 1 : (n > most ? most : n));
   };
-  p.n_pre = Lpre > 0 ? parts((Lpre + 31) / 32, tiles, 512, 4, 64) : 0;
+  p.n_pre = Lpre > 0 ? parts((Lpre + 31) / 32, tiles, 256, 4, kPrefixParts - 32) : 0;
   p.n_loc = Lloc > 0 ? parts((Lloc + 31) / 32, groups, 512, 8, 32) : 0;
   size_t at = round_up256((size_t)rows * p.n_pre * dm.d * sizeof(float));
   p.off_pre_ml = at;
@@ -467,14 +560,19 @@ int launch_prefix(const Dims& dm, const PrefixPlan& pl, PrefixArgs a, void* ws, 
   a.pre_ml = (float2*)(w + pl.off_pre_ml);
   a.loc_o = (float*)(w + pl.off_loc_o);
   a.loc_ml = (float2*)(w + pl.off_loc_ml);
-  a.pre_groups = (int)((BM + 4 * a.tpw - 1) / (4 * a.tpw) * dm.Hkv * a.n_pre);
+  a.pre_groups = (int)((BM + kPrefixWaves * a.tpw - 1) / (kPrefixWaves * a.tpw) * dm.Hkv * a.n_pre);
   const dim3 grid((unsigned)(a.pre_groups + (long long)a.B * a.groups * dm.Hkv * a.n_loc));
   if (dm.d == 128)
-    hipLaunchKernelGGL(prefix_kernel<128>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(prefix_kernel<128>, grid, dim3(64 * kPrefixWaves), 0, st, a);
   else
-    hipLaunchKernelGGL(prefix_kernel<64>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(prefix_kernel<64>, grid, dim3(64 * kPrefixWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
-  return launch_merge2(dm.d, a.pre_o, a.pre_ml, a.n_pre, a.loc_o, a.loc_ml, a.n_loc, a.out, a.lse, 0, BM * dm.Hq, st);
+  const dim3 rows((unsigned)(BM * dm.Hq));
+  if (dm.d == 128)
+    hipLaunchKernelGGL(prefix_join_kernel<128>, rows, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(prefix_join_kernel<64>, rows, dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
 }
 
 }  // namespace msa
