@@ -1,7 +1,7 @@
 // msa_evict: of every (sequence, KV head) the rows of the cache that weigh most, the first ones and the last ones, moved together.
 //
 // Two launches.  evict_select_kernel, a workgroup to a (sequence, KV head), finds the weight of the lightest row that stays (as an
-// integer of the same order, in digits of 11, 11 and 10 bits from the top, each by counting), then lists the rows that stay in
+// integer of the same order, in digits of up to 11 bits from the top, each by counting), then lists the rows that stay in
 // ascending order and moves their weights.  Counted in LDS, where the order of additions changes nothing.  evict_move_kernel copies
 // the rows of K and V.
 #include "msa_device.h"
@@ -11,6 +11,8 @@ namespace msa {
 
 constexpr int kSelectThreads = 1024;
 constexpr int kBins = 2048;  // values of a digit, two to a thread
+constexpr int kListed = 64;  // a lane to each
+static_assert(kListed * 2 <= kBins, "a list in the counters' memory");
 static_assert(kBins == 2 * kSelectThreads, "two bins to a thread");
 
 // The order of weights as an integer: what is no number comes last, the zeros are equal.
@@ -24,7 +26,9 @@ template <int REGS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int WAVES = kSelectThreads / 64;
   __shared__ int cnt_s[2][WAVES], found[3];
+  __shared__ uint32_t ends_s[2][WAVES];
   __shared__ __attribute__((aligned(8))) int bins[kBins];
+  uint2* const list = reinterpret_cast<uint2*>(bins);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long pair = blockIdx.x;
@@ -67,26 +71,52 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 #pragma unroll
     for (int u = 0; u < REGS; ++u) key[u] = weight_key(x[u]);
   }
-  // Digit by digit from the top: the rows in the middle that agree with kth so far, counted by their next digit; the lightest row
-  // that stays has the largest digit from which on there are as many as are wanted.
-  uint32_t kth = 0u;  // rows heavier than kth stay, and of those that weigh kth the first `ties`
-  int ties = need;
-  for (int shift = 21, bits = 11; need > 0; shift = shift == 21 ? 10 : 0, bits = shift == 0 ? 10 : 11) {
-    const uint32_t mask = (1u << bits) - 1u, above = shift == 21 ? 0u : ~0u << (shift + bits);
-    *reinterpret_cast<int2*>(&bins[2 * tid]) = make_int2(0, 0);
-    __syncthreads();
-    auto count = [&](uint32_t k) {
-      if (((k ^ kth) & above) == 0u) atomicAdd(&bins[(k >> shift) & mask], 1);
-    };
+  auto each = [&](auto f) {  // the weights of this thread's rows in the middle
     if constexpr (REGS > 0) {
 #pragma unroll
       for (int u = 0; u < REGS; ++u) {
         const int i = w0 + 64 * u;
-        if (u < blocks && i >= m0 && i < m1) count(key[u]);
+        if (u < blocks && i >= m0 && i < m1) f(key[u], i);
       }
     } else {
-      for (int i = m0 + tid; i < m1; i += kSelectThreads) count(weight_key(mass[i]));
+      for (int i = m0 + tid; i < m1; i += kSelectThreads) f(weight_key(mass[i]), i);
     }
+  };
+  uint32_t lo = UINT32_MAX, hi = 0u;
+  each([&](uint32_t k, int) {
+    lo = k < lo ? k : lo;
+    hi = k > hi ? k : hi;
+  });
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const uint32_t u = __shfl_xor(lo, off, 64), v = __shfl_xor(hi, off, 64);
+    lo = u < lo ? u : lo;
+    hi = v > hi ? v : hi;
+  }
+  if (lane == 0) {
+    ends_s[0][wave] = lo;
+    ends_s[1][wave] = hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    lo = ends_s[0][w] < lo ? ends_s[0][w] : lo;
+    hi = ends_s[1][w] > hi ? ends_s[1][w] : hi;
+  }
+  // Digit by digit from the top of what the weights (less the least of them) span: the rows that agree with kth so far, counted by
+  // their next digit; the lightest row that stays has the largest digit from which on there are as many as are wanted.  (Digits of
+  // the span and not of 32 bits: weights within a few octaves are in many counters then, and lanes of a wave seldom in the same.)
+  const int span = hi > lo ? 32 - __clz(hi - lo) : 1;
+  uint32_t kth = 0u;  // less lo.  Rows heavier than kth stay, and of those that weigh kth the first `ties`
+  int ties = need, tie_row = -1;  // ... or those up to tie_row
+  for (int bits = span < 11 ? span : 11, shift = span - bits; need > 0;) {
+    const uint32_t mask = (1u << bits) - 1u, above = shift + bits >= span ? 0u : ~0u << (shift + bits);
+    *reinterpret_cast<int2*>(&bins[2 * tid]) = make_int2(0, 0);
+    __syncthreads();
+    each([&](uint32_t k, int) {
+      k -= lo;
+      if (((k ^ kth) & above) == 0u) atomicAdd(&bins[(k >> shift) & mask], 1);
+    });
     __syncthreads();
     const int top = kBins - 1 - 2 * tid;  // this thread's two digits: top and the one below
     const int2 two = *reinterpret_cast<const int2*>(&bins[top - 1]);
@@ -109,14 +139,41 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     __syncthreads();
     kth |= (uint32_t)found[0] << shift;
     ties = found[1];
-    if (ties == found[2]) {  // all that agree so far stay: those from kth on
-      ties = kth == 0u ? INT32_MAX : 0;
-      kth = kth == 0u ? 0u : kth - 1u;
+    const int agree = found[2];
+    if (ties == agree) {  // all that agree so far stay: those from kth on, which is not 0, since some row goes
+      --kth;
+      ties = 0;
       break;
     }
     if (shift == 0) break;
+    if (agree <= kListed) {  // few: each is compared with all of them (the counters' memory is free for the list)
+      const uint32_t agreed = ~0u << shift;
+      if (tid == 0) found[0] = 0;
+      __syncthreads();
+      each([&](uint32_t k, int i) {
+        k -= lo;
+        if (((k ^ kth) & agreed) == 0u) list[atomicAdd(&found[0], 1)] = make_uint2(k, (uint32_t)i);
+      });
+      __syncthreads();
+      const uint2 other = list[lane < agree ? lane : 0];
+      for (int c = wave; c < agree; c += WAVES) {  // a wave to each of them
+        const uint2 mine = list[c];
+        const bool better = lane < agree && (other.x > mine.x || (other.x == mine.x && other.y < mine.y));
+        if (__popcll(__ballot(better)) == ties - 1 && lane == 0) {
+          found[1] = (int)mine.x;
+          found[2] = (int)mine.y;
+        }
+      }
+      __syncthreads();
+      kth = (uint32_t)found[1];
+      tie_row = found[2];
+      ties = 0;
+      break;
+    }
+    bits = shift < 11 ? shift : 11;
+    shift -= bits;
   }
-  if (need == 0) kth = UINT32_MAX;
+  kth = need > 0 ? kth + lo : UINT32_MAX;
   int tied_before = 0;
   if constexpr (REGS > 0) {
     if (ties > 0) {
@@ -135,7 +192,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
       if (u >= blocks) continue;
       const int i = w0 + 64 * u;
       const bool middle = i >= m0 && i < m1;
-      bool stays = i < n && (!middle || key[u] > kth);
+      bool stays = i < n && (!middle || key[u] > kth || (key[u] == kth && i <= tie_row));
       if (ties > 0) {
         const unsigned long long tie = __ballot(middle && key[u] == kth);
         stays |= middle && key[u] == kth && tied_before + __popcll(tie & ((1ull << lane) - 1ull)) < ties;
@@ -167,7 +224,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
       const unsigned long long tie = __ballot(middle && k == kth);
       int t0, k0;
       const int tied = total(__popcll(tie), t0);  // (behind its barrier every weight of this turn is in a register)
-      const bool stays = i < n && (!middle || k > kth || (k == kth && tied_before + t0 + __popcll(tie & ((1ull << lane) - 1ull)) < ties));
+      const bool stays = i < n && (!middle || k > kth || (k == kth && i <= tie_row) || (k == kth && tied_before + t0 + __popcll(tie & ((1ull << lane) - 1ull)) < ties));
       const unsigned long long kept = __ballot(stays);
       const int all = total(__popcll(kept), k0);
       if (stays) {
@@ -239,6 +296,8 @@ int launch_evict(const Dims& dm, const EvictArgs& a, int B, hipStream_t st) {
   const unsigned pairs = (unsigned)B * dm.Hkv;
   if (a.Lloc <= 8 * kSelectThreads)
     hipLaunchKernelGGL(evict_select_kernel<8>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
+  else if (a.Lloc <= 16 * kSelectThreads)
+    hipLaunchKernelGGL(evict_select_kernel<16>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
   else if (a.Lloc <= 32 * kSelectThreads)
     hipLaunchKernelGGL(evict_select_kernel<32>, dim3(pairs), dim3(kSelectThreads), 0, st, a);
   else

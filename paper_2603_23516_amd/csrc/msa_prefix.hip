@@ -310,6 +310,33 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
           (f32x4_t){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
 }
 
+// A column of a workgroup over a cache: column n is head n % r of token m0 + n / r of sequence b, and sees the rows below lim.
+struct CacheColumn {
+  bool ok;          // there is such a token ...
+  int tok, head;    // ... else another that there is
+  int lim;
+  int least, most;  // of the sixteen columns' lim, those that are
+};
+__device__ __forceinline__ CacheColumn cache_column(const PrefixArgs& a, long long b, int m0, int n) {
+  CacheColumn c;
+  const int tl = n / a.r;
+  c.ok = tl < a.tpl && m0 + tl < a.M;
+  c.tok = c.ok ? m0 + tl : m0;
+  c.head = c.ok ? n - tl * a.r : 0;
+  const long long p1 = (long long)a.q_pos[b * a.M + c.tok] - a.pos0 + 1;
+  c.lim = c.ok ? (p1 < 0 ? 0 : (p1 < a.Lloc ? (int)p1 : a.Lloc)) : 0;
+  int least = c.ok ? c.lim : INT32_MAX, most = c.lim;
+#pragma unroll
+  for (int off = 8; off > 0; off >>= 1) {
+    const int u = __shfl_xor(least, off, 64), v = __shfl_xor(most, off, 64);
+    least = u < least ? u : least;
+    most = v > most ? v : most;
+  }
+  c.least = __builtin_amdgcn_readfirstlane(least);
+  c.most = __builtin_amdgcn_readfirstlane(most);
+  return c;
+}
+
 template <int D>
 __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned char* smem) {
   constexpr int NW = kPrefixWaves, NS = D / 32, NC = D / 16;
@@ -327,28 +354,16 @@ __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned 
   x /= a.n_loc;
   const int m0 = x % a.groups * a.tpl;
   const long long b = x / a.groups;
-  const int tl = n / r, tok = m0 + tl;
-  const bool ok = tl < a.tpl && tok < a.M;
-  const long long qh = (b * a.M + (ok ? tok : m0)) * a.Hq + g * r + (ok ? n - tl * r : 0);
+  const CacheColumn col = cache_column(a, b, m0, n);
+  const long long qh = (b * a.M + col.tok) * a.Hq + g * r + col.head;
   bf16x8_t bq[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     uint4 v = *reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd);
-    if (!ok) v = make_uint4(0, 0, 0, 0);
+    if (!col.ok) v = make_uint4(0, 0, 0, 0);
     bq[s] = as_bf16x8(v);
   }
-  const long long p1 = (long long)a.q_pos[b * a.M + (ok ? tok : m0)] - a.pos0 + 1;
-  const int lim = ok ? (p1 < 0 ? 0 : (p1 < a.Lloc ? (int)p1 : a.Lloc)) : 0;
-  int least = ok ? lim : INT32_MAX, most = lim;
-#pragma unroll
-  for (int off = 8; off > 0; off >>= 1) {
-    const int u = __shfl_xor(least, off, 64), v = __shfl_xor(most, off, 64);
-    least = u < least ? u : least;
-    most = v > most ? v : most;
-  }
-  least = __builtin_amdgcn_readfirstlane(least);
-  most = __builtin_amdgcn_readfirstlane(most);
-  const int steps = (most + 31) / 32;
+  const int steps = (col.most + 31) / 32;
   const int sb = (int)((long long)steps * sp / a.n_loc), se = (int)((long long)steps * (sp + 1) / a.n_loc);
   Columns<D> y;
   y.m_run = -INFINITY;
@@ -356,7 +371,7 @@ __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned 
 #pragma unroll
   for (int c = 0; c < NC; ++c) y.o[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   const long long loc = (b * a.Hkv + g) * a.Lloc * D;
-  attend_rows<D>(a.Kloc + loc, a.Vloc + loc, most, sb + wave, se, NW, bq, lim, least, a.qscale, smem + wave * STAGE, y);
+  attend_rows<D>(a.Kloc + loc, a.Vloc + loc, col.most, sb + wave, se, NW, bq, col.lim, col.least, a.qscale, smem + wave * STAGE, y);
 
   // the waves' results
   y.l_run = add_xor32(add_xor16(y.l_run));
