@@ -4,6 +4,9 @@
 #pragma once
 #include "msa_attend.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace msa {
 
 struct EncodedArgs {
@@ -89,6 +92,12 @@ __device__ __forceinline__ float max_xor32(float x) {
   const uint32_t u = __float_as_uint(x);
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// f(0), f(1), ... with the numbers as types.
+template <int... I, class F>
+__device__ __forceinline__ void each_stage(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>()), ...);
 }
 
 // Rows of the local cache that a token at position p (counted from the cache's first row) sees: [0, first) and [from, to).

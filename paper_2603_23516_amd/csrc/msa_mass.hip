@@ -15,6 +15,7 @@
 #include "msa_encoded.h"
 
 #include <type_traits>
+#include <utility>
 
 namespace msa {
 
@@ -138,12 +139,12 @@ struct MassParts {
 template <int D>
 __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu(3))) void mass_tiled_kernel(MassArgs a, MassParts pp) {
   constexpr int NW = kMassWaves, NP = D / 8, NS = D / 16, ROW = D * 2;
-  constexpr int KT = kMassRows / 32;
+  constexpr int KT = kMassRows / 32, STAGES = kMassStages, AHEAD = STAGES - 1;  // steps whose copies are under way
   constexpr int TILE = 32 * ROW;          // bytes of a step's queries
   constexpr int NPW = 32 * NP / 64 / NW;  // copies of a wave per step
   static_assert(NPW >= 1, "a step is a whole number of copies per wave");
   constexpr int SIDE = NW * 256;           // behind them, for every wave: 32 log-sums and 32 positions
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kMassStages * (TILE + SIDE)];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[STAGES * (TILE + SIDE)];
   __shared__ int lo_s[NW], hi_s[NW];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -250,12 +251,12 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
     auto step = [&](int s, auto stage) __attribute__((always_inline)) {
       constexpr int BUF = decltype(stage)::value;
       const unsigned char* const st = smem + BUF * (TILE + SIDE);
-      if (s + 1 < se)
-        wait_copies_but<NPW + 1>();
+      if (s + AHEAD - 1 < se)
+        wait_copies_but<(AHEAD - 1) * (NPW + 1)>();
       else
         wait_copies_but<0>();
       lds_barrier();
-      if (s + 2 < se) issue(std::integral_constant<int, (BUF + 2) % kMassStages>());
+      if (s + AHEAD < se) issue(std::integral_constant<int, (BUF + AHEAD) % STAGES>());
       const float* const side = reinterpret_cast<const float*>(st + TILE + wave * 256);
       float nls = -side[col] * kLog2e;
       SeenBy see = seen_by(a, __float_as_int(side[32 + col]));
@@ -300,13 +301,14 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
     for (int k = 0; k < KT; ++k)
 #pragma unroll
       for (int i = 0; i < NS; ++i) asm volatile("" : "+v"(key[k][i]));
-    issue(std::integral_constant<int, 0>());
-    if (sb + 1 < se) issue(std::integral_constant<int, 1>());
-    for (int s = sb; s < se; s += kMassStages) {  // stages by number, so that LDS addresses are constants
-      step(s, std::integral_constant<int, 0>());
-      if (s + 1 < se) step(s + 1, std::integral_constant<int, 1>());
-      if (s + 2 < se) step(s + 2, std::integral_constant<int, 2>());
-    }
+    // stages by number, so that LDS addresses are constants
+    each_stage(std::make_integer_sequence<int, AHEAD>(), [&](auto stage) {
+      if (sb + decltype(stage)::value < se) issue(stage);
+    });
+    for (int s = sb; s < se; s += STAGES)
+      each_stage(std::make_integer_sequence<int, STAGES>(), [&](auto stage) __attribute__((always_inline)) {
+        if (s + decltype(stage)::value < se) step(s + decltype(stage)::value, stage);
+      });
   }
   // over the 32 columns: lane c of a half keeps the sum of register c
 #pragma unroll

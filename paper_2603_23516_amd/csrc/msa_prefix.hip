@@ -126,14 +126,9 @@ constexpr int kPrefixParts = 192;  // of a row at most, 32 of them over the cach
 constexpr int kPrefixStages = 3;
 constexpr int kPrefixWaves = 4;
 
-template <int... I, class F>
-__device__ __forceinline__ void each_stage(std::integer_sequence<int, I...>, F f) {
-  (f(std::integral_constant<int, I>()), ...);
-}
-
 template <int D>
 __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned char* smem) {
-  constexpr int NW = kPrefixWaves, AHEAD = kPrefixStages - 1;  // steps whose copies are under way
+  constexpr int NW = kPrefixWaves, STAGES = kPrefixStages, AHEAD = STAGES - 1;  // steps whose copies are under way
   constexpr int NP = D / 8;            // 16-byte pieces per row
   constexpr int NS = D / 16;           // contraction slices of the score product
   constexpr int NT = D / 32;           // 32-row tiles of the output product
@@ -240,7 +235,7 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
       wait_copies_but<0>();
     // step s is staged for everyone; everyone is done with step s - 1's stage (its LDS reads have come back)
     lds_barrier();
-    if (s + AHEAD < se) issue(std::integral_constant<int, (BUF + AHEAD) % kPrefixStages>());
+    if (s + AHEAD < se) issue(std::integral_constant<int, (BUF + AHEAD) % STAGES>());
     const int t0 = 32 * (sp + s * a.n_pre);
     if (t0 >= most) return;  // this wave sees nothing of the step (uniform)
     f32x16e_t sc;
@@ -291,8 +286,8 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
   each_stage(std::make_integer_sequence<int, AHEAD>(), [&](auto stage) {
     if (decltype(stage)::value < se) issue(stage);
   });
-  for (int s = 0; s < se; s += kPrefixStages)
-    each_stage(std::make_integer_sequence<int, kPrefixStages>(), [&](auto stage) __attribute__((always_inline)) {
+  for (int s = 0; s < se; s += STAGES)
+    each_stage(std::make_integer_sequence<int, STAGES>(), [&](auto stage) __attribute__((always_inline)) {
       if (s + decltype(stage)::value < se) step(s + decltype(stage)::value, stage);
     });
   const uint32_t u = __float_as_uint(l_run);
