@@ -25,7 +25,7 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
 template <int REGS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int WAVES = kSelectThreads / 64;
-  __shared__ int cnt_s[2][WAVES], found[3];
+  __shared__ int cnt_s[2][WAVES], found[3], listed;
   __shared__ uint32_t ends_s[2][WAVES];
   __shared__ __attribute__((aligned(8))) int bins[kBins];
   uint2* const list = reinterpret_cast<uint2*>(bins);
@@ -112,6 +112,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   for (int bits = span < 11 ? span : 11, shift = span - bits; need > 0;) {
     const uint32_t mask = (1u << bits) - 1u, above = shift + bits >= span ? 0u : ~0u << (shift + bits);
     *reinterpret_cast<int2*>(&bins[2 * tid]) = make_int2(0, 0);
+    if (tid == 0) listed = 0;
     __syncthreads();
     each([&](uint32_t k, int) {
       k -= lo;
@@ -148,11 +149,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     if (shift == 0) break;
     if (agree <= kListed) {  // few: each is compared with all of them (the counters' memory is free for the list)
       const uint32_t agreed = ~0u << shift;
-      if (tid == 0) found[0] = 0;
-      __syncthreads();
       each([&](uint32_t k, int i) {
         k -= lo;
-        if (((k ^ kth) & agreed) == 0u) list[atomicAdd(&found[0], 1)] = make_uint2(k, (uint32_t)i);
+        if (((k ^ kth) & agreed) == 0u) list[atomicAdd(&listed, 1)] = make_uint2(k, (uint32_t)i);
       });
       __syncthreads();
       const uint2 other = list[lane < agree ? lane : 0];

@@ -413,74 +413,76 @@ __global__ __launch_bounds__(64 * kPrefixWaves) __attribute__((amdgpu_waves_per_
 // together with all (max, sum) pairs.  (A wave to a row, as the other paths join theirs, is one part after another where rows are few
 // and parts many: 256 rows of 68 parts 22 us, 2048 of 33 13.)
 template <int D>
-__global__ __launch_bounds__(256) void prefix_join_kernel(PrefixArgs a) {
+__global__ __launch_bounds__(256) void prefix_join_kernel(PrefixArgs a, long long rows) {
   constexpr int V = D / 64, U = 8;
   typedef float vec_t __attribute__((ext_vector_type(V)));
   __shared__ float o_s[4][D];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long row = blockIdx.x;
   const int n1 = a.n_pre, ns = n1 + a.n_loc;
-  const float2 *const m1 = a.pre_ml + row * n1, *const m2 = a.loc_ml + row * a.n_loc;
-  const float *const p1 = a.pre_o + row * n1 * D + lane * V, *const p2 = a.loc_o + row * a.n_loc * D + lane * V;
-  vec_t v[U];
-  auto fetch = [&](int s0) {  // (past the end: the last one again)
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = s0 + 4 * u < ns ? s0 + 4 * u : ns - 1;
-      v[u] = *reinterpret_cast<const vec_t*>(s < n1 ? p1 + (long long)s * D : p2 + (long long)(s - n1) * D);
-    }
-  };
-  float2 ml[kPrefixParts / 64];
-#pragma unroll
-  for (int i = 0; i < kPrefixParts / 64; ++i) {
-    const int s = lane + 64 * i;
-    ml[i] = make_float2(-INFINITY, 0.f);
-    if (64 * i < ns && s < ns) ml[i] = s < n1 ? m1[s] : m2[s - n1];
-  }
-  fetch(wave);
-  float mx = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kPrefixParts / 64; ++i) mx = fmaxf(mx, ml[i].x);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
-  float lsum = 0.f, w[kPrefixParts / 64];
-#pragma unroll
-  for (int i = 0; i < kPrefixParts / 64; ++i) {
-    const bool empty = ml[i].x == -INFINITY;  // (its outputs may be anything)
-    w[i] = empty ? -1.f : __builtin_amdgcn_exp2f(ml[i].x - mx);
-    lsum += empty ? 0.f : w[i] * ml[i].y;
-  }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) lsum += __shfl_xor(lsum, off, 64);
-  vec_t acc = 0.f;
-#pragma unroll
-  for (int i = 0; i < kPrefixParts / 64; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {  // parts 64 i + 32 j + wave, + 4, ... of this wave
-      const int s0 = 64 * i + 32 * j;
-      if (s0 + wave >= ns) continue;
-      if (s0 > 0) fetch(s0 + wave);
+  for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+    const float2 *const m1 = a.pre_ml + row * n1, *const m2 = a.loc_ml + row * a.n_loc;
+    const float *const p1 = a.pre_o + row * n1 * D + lane * V, *const p2 = a.loc_o + row * a.n_loc * D + lane * V;
+    vec_t v[U];
+    auto fetch = [&](int s0) {  // (past the end: the last one again)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w[i]), 32 * j + wave + 4 * u));
-        if (s0 + wave + 4 * u < ns && f >= 0.f) acc += f * v[u];  // wave-uniform
+        const int s = s0 + 4 * u < ns ? s0 + 4 * u : ns - 1;
+        v[u] = *reinterpret_cast<const vec_t*>(s < n1 ? p1 + (long long)s * D : p2 + (long long)(s - n1) * D);
       }
+    };
+    float2 ml[kPrefixParts / 64];
+#pragma unroll
+    for (int i = 0; i < kPrefixParts / 64; ++i) {
+      const int s = lane + 64 * i;
+      ml[i] = make_float2(-INFINITY, 0.f);
+      if (64 * i < ns && s < ns) ml[i] = s < n1 ? m1[s] : m2[s - n1];
+    }
+    fetch(wave);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPrefixParts / 64; ++i) mx = fmaxf(mx, ml[i].x);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
+    float lsum = 0.f, w[kPrefixParts / 64];
+#pragma unroll
+    for (int i = 0; i < kPrefixParts / 64; ++i) {
+      const bool empty = ml[i].x == -INFINITY;  // (its outputs may be anything)
+      w[i] = empty ? -1.f : __builtin_amdgcn_exp2f(ml[i].x - mx);
+      lsum += empty ? 0.f : w[i] * ml[i].y;
     }
 #pragma unroll
-  for (int c = 0; c < V; ++c) o_s[wave][lane * V + c] = acc[c];
-  __syncthreads();
-  if (threadIdx.x < D / 2) {
-    const int d = 2 * threadIdx.x;
-    float x0 = 0.f, x1 = 0.f;
+    for (int off = 32; off > 0; off >>= 1) lsum += __shfl_xor(lsum, off, 64);
+    vec_t acc = 0.f;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      x0 += o_s[u][d];
-      x1 += o_s[u][d + 1];
+    for (int i = 0; i < kPrefixParts / 64; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {  // parts 64 i + 32 j + wave, + 4, ... of this wave
+        const int s0 = 64 * i + 32 * j;
+        if (s0 + wave >= ns) continue;
+        if (s0 > 0) fetch(s0 + wave);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w[i]), 32 * j + wave + 4 * u));
+          if (s0 + wave + 4 * u < ns && !(f < 0.f)) acc += f * v[u];  // wave-uniform
+        }
+      }
+#pragma unroll
+    for (int c = 0; c < V; ++c) o_s[wave][lane * V + c] = acc[c];
+    __syncthreads();
+    if (threadIdx.x < D / 2) {
+      const int d = 2 * threadIdx.x;
+      float x0 = 0.f, x1 = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        x0 += o_s[u][d];
+        x1 += o_s[u][d + 1];
+      }
+      const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+      reinterpret_cast<uint32_t*>(a.out + row * D)[threadIdx.x] = pack_bf16(x0 * inv, x1 * inv);
+      if (threadIdx.x == 0 && a.lse != nullptr) a.lse[row] = lsum > 0.f ? (mx + log2f(lsum)) * 0.6931471805599453f : -INFINITY;
     }
-    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-    reinterpret_cast<uint32_t*>(a.out + row * D)[threadIdx.x] = pack_bf16(x0 * inv, x1 * inv);
-    if (threadIdx.x == 0 && a.lse != nullptr) a.lse[row] = lsum > 0.f ? (mx + log2f(lsum)) * 0.6931471805599453f : -INFINITY;
+    __syncthreads();  // (the next row's outputs come to the same place)
   }
 }
 
@@ -577,11 +579,12 @@ int launch_prefix(const Dims& dm, const PrefixPlan& pl, PrefixArgs a, void* ws, 
   else
     hipLaunchKernelGGL(prefix_kernel<64>, grid, dim3(64 * kPrefixWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
-  const dim3 rows((unsigned)(BM * dm.Hq));
+  const long long rows = BM * dm.Hq;
+  const dim3 joins((unsigned)(rows < 1 << 20 ? rows : 1 << 20));
   if (dm.d == 128)
-    hipLaunchKernelGGL(prefix_join_kernel<128>, rows, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(prefix_join_kernel<128>, joins, dim3(256), 0, st, a, rows);
   else
-    hipLaunchKernelGGL(prefix_join_kernel<64>, rows, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(prefix_join_kernel<64>, joins, dim3(256), 0, st, a, rows);
   return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
 }
 
