@@ -388,7 +388,7 @@ static EncodedPlan plan_of(const Dims& dm, int B, int M, long long mem_rows, boo
   // (More rows never lead back to the single-token kernel: both sides count them in whole steps, M of them on the left and 8 on
   // the right, which applies from M = 8 on.)
   const long long steps_mem = (mem_rows + 31) / 32, cost = steps_mem + kLocalCost * ((local_rows + 31) / 32);
-  const long long work = pairs * cost, least = 20000 + 8 * pairs / M * steps_mem;
+  const double work = (double)pairs * cost, least = 20000 + (double)(8 * pairs / M) * steps_mem;  // (past 64 bits at the largest sizes)
   p.tiled = !expand || ((mem_rows == 0 || shared) && (M >= 32 || (M >= (mem_rows > 0 ? 8 : 4) && work >= least))) ? 1 : 0;
   int n_most;  // splits that the workspace holds: grows with the rows, so that one sized for the longest call serves all
   long long most1 = (cost + 15) / 16;

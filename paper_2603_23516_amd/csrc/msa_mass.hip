@@ -39,8 +39,8 @@ __device__ __forceinline__ float old_weight(const MassArgs& a, long long at) {
 
 // ---- few columns ---------------------------------------------------------------------------------------------------------
 // (A wave to 32 rows and eight of them to a SIMD: 40 sequences of 8192 rows, 8 heads of 128, 115 us, 6.0 TB/s, of 0 to 8192 rows,
-// 4000 on average, 83.  Waves that go on through 64 to 512 rows with one or two blocks ahead 120 to 139 and 88 to 93; 64 rows at once
-// 119 and 96; workgroups by rows first and sequences second 127 and 79.)
+// 4000 on average, 72.  Waves that go on through 64 to 512 rows with one or two blocks ahead 120 to 139 and 88 to 93; 64 rows at once
+// 119 and 73; workgroups by rows first and sequences second 127 and 79.)
 template <int D, int CG>  // CG: groups of 16 columns
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 : 1))) void mass_rows_kernel(MassArgs a, int n_blocks) {
   constexpr int NS = D / 32;
@@ -346,6 +346,9 @@ MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks
   p.ws_bytes = 256;
   if (M * dm.r <= 64) {
     p.n_blocks = (Lloc + 127) / 128;
+    // An odd number to a (sequence, KV head): an even one puts the same blocks of all of them, and with them the ones behind the
+    // sequences' ends, on the same XCDs and shader engines.  (40 sequences of 0 to 8192 rows 83 us, so 72; one of 8192 6.5, so 7.2.)
+    if (B > 1 && pairs * p.n_blocks >= 4096) p.n_blocks |= 1;
     if (pairs * p.n_blocks >= 1 << 24) p.ws_bytes = 0;
     return p;
   }
