@@ -94,6 +94,12 @@ __device__ __forceinline__ float max_xor32(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// x or zeros, by arithmetic: as a choice it becomes a branch around each load, which then come one after another.
+__device__ __forceinline__ uint4 keep_if(uint4 x, bool keep) {
+  const uint32_t m = keep ? ~0u : 0u;
+  return make_uint4(x.x & m, x.y & m, x.z & m, x.w & m);
+}
+
 // f(0), f(1), ... with the numbers as types.
 template <int... I, class F>
 __device__ __forceinline__ void each_stage(std::integer_sequence<int, I...>, F f) {

@@ -157,13 +157,10 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
   bf16x8_t bq[NS];
   const uint16_t* qp = a.q + (((long long)b * a.M + (ok ? tok : 0)) * a.Hq + g * r + (ok ? head : 0)) * D + 8 * hf;
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    uint4 v = *reinterpret_cast<const uint4*>(qp + 16 * s);
-    if (!ok) v = make_uint4(0, 0, 0, 0);
-    bq[s] = as_bf16x8(v);
-    // (waited for here: at their first use, in the loop, the wait would be one for all copies in flight as well)
-    asm volatile("" : "+v"(bq[s]));
-  }
+  for (int s = 0; s < NS; ++s) bq[s] = as_bf16x8(keep_if(*reinterpret_cast<const uint4*>(qp + 16 * s), ok));
+  // (waited for here: at their first use, in the loop, the wait would be one for all copies in flight as well)
+#pragma unroll
+  for (int s = 0; s < NS; ++s) asm volatile("" : "+v"(bq[s]));
 
   // Places of the 16-byte pieces of a row in LDS: piece p of row i lies at p ^ swz(i).  What a lane reads of slice s (keys) or
   // tile t (values) is then its first address with 32 s or 64 t xored in; rows further on and stages are constants.

@@ -143,12 +143,17 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
   const int g = x % a.Hkv;
   x /= a.Hkv;
   const int sp = x % a.n_pre, tile = x / a.n_pre;
-  const long long BM = (long long)a.B * a.M;
+  const int BM = a.B * a.M;  // (2^25 at most)
 
   // this lane's column, and the rows [0, lim) that it sees
   const int tl = col / r, head = col - tl * r;
-  const long long tok = ((long long)tile * NW + wave) * a.tpw + tl;
+  const int tok = (tile * NW + wave) * a.tpw + tl;
   const bool ok = tl < a.tpw && tok < BM;
+  bf16x8_t bq[NS];
+  const long long qh = (long long)(ok ? tok : 0) * a.Hq + g * r + (ok ? head : 0);
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+    bq[s] = as_bf16x8(keep_if(*reinterpret_cast<const uint4*>(a.q + qh * D + 8 * hf + 16 * s), ok));
   const int lim = ok ? prefix_of(a, tok / a.M) : 0;
   int least = ok ? lim : INT32_MAX, most = lim;
 #pragma unroll
@@ -170,16 +175,9 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
   const int steps = (end + 31) / 32;
   const int se = (steps - sp + a.n_pre - 1) / a.n_pre;  // this part's steps: sp, sp + n_pre, ...
 
-  bf16x8_t bq[NS];
-  const long long qh = (ok ? tok : 0) * a.Hq + g * r + (ok ? head : 0);
+  // (waited for here: at their first use, in the loop, the wait would be one for all copies in flight as well)
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    uint4 v = *reinterpret_cast<const uint4*>(a.q + qh * D + 8 * hf + 16 * s);
-    if (!ok) v = make_uint4(0, 0, 0, 0);
-    bq[s] = as_bf16x8(v);
-    // (waited for here: at their first use, in the loop, the wait would be one for all copies in flight as well)
-    asm volatile("" : "+v"(bq[s]));
-  }
+  for (int s = 0; s < NS; ++s) asm volatile("" : "+v"(bq[s]));
 
   // Places of the 16-byte pieces of a row in LDS: piece p of row i lies at p ^ swz(i), so that the reads meet no bank twice.
   auto swz_k = [](int i) { return D == 128 ? (i & 15) : ((i >> 1) & 7); };
@@ -353,11 +351,8 @@ __device__ __forceinline__ void over_cache(const PrefixArgs& a, int x, unsigned 
   const long long qh = (b * a.M + col.tok) * a.Hq + g * r + col.head;
   bf16x8_t bq[NS];
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    uint4 v = *reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd);
-    if (!col.ok) v = make_uint4(0, 0, 0, 0);
-    bq[s] = as_bf16x8(v);
-  }
+  for (int s = 0; s < NS; ++s)
+    bq[s] = as_bf16x8(keep_if(*reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd), col.ok));
   const int steps = (col.most + 31) / 32;
   const int sb = (int)((long long)steps * sp / a.n_loc), se = (int)((long long)steps * (sp + 1) / a.n_loc);
   Columns<D> y;
@@ -419,70 +414,75 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(PrefixArgs a, long lon
   __shared__ float o_s[4][D];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long row = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  if (row >= rows) return;
   const int n1 = a.n_pre, ns = n1 + a.n_loc;
-  for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
-    const float2 *const m1 = a.pre_ml + row * n1, *const m2 = a.loc_ml + row * a.n_loc;
-    const float *const p1 = a.pre_o + row * n1 * D + lane * V, *const p2 = a.loc_o + row * a.n_loc * D + lane * V;
-    vec_t v[U];
-    auto fetch = [&](int s0) {  // (past the end: the last one again)
+  const float2 *const m1 = a.pre_ml + row * n1, *const m2 = a.loc_ml + row * a.n_loc;
+  const float *const p1 = a.pre_o + row * n1 * D + lane * V, *const p2 = a.loc_o + row * a.n_loc * D + lane * V;
+  vec_t v[U];
+  auto fetch = [&](int s0) {  // (past the end: the last one again)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + 4 * u < ns ? s0 + 4 * u : ns - 1;
+      v[u] = *reinterpret_cast<const vec_t*>(s < n1 ? p1 + (long long)s * D : p2 + (long long)(s - n1) * D);
+    }
+  };
+  auto pair_at = [&](int s) {  // (no load under a condition of its own: they are under way together)
+    const int at = s < ns ? s : ns - 1;
+    float2 ml = *(at < n1 ? m1 + at : m2 + (at - n1));
+    if (s >= ns) ml.x = -INFINITY;
+    return ml;
+  };
+  fetch(wave);
+  float2 ml[kPrefixParts / 64];
+  ml[0] = pair_at(lane);
+#pragma unroll
+  for (int i = 1; i < kPrefixParts / 64; ++i) {
+    ml[i] = make_float2(-INFINITY, 0.f);
+    if (64 * i < ns) ml[i] = pair_at(lane + 64 * i);
+  }
+  float mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kPrefixParts / 64; ++i) mx = fmaxf(mx, ml[i].x);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
+  float lsum = 0.f, w[kPrefixParts / 64];
+#pragma unroll
+  for (int i = 0; i < kPrefixParts / 64; ++i) {
+    const bool empty = ml[i].x == -INFINITY;  // (its outputs may be anything)
+    w[i] = empty ? -1.f : __builtin_amdgcn_exp2f(ml[i].x - mx);
+    lsum += empty ? 0.f : w[i] * ml[i].y;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) lsum += __shfl_xor(lsum, off, 64);
+  vec_t acc = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPrefixParts / 64; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {  // parts 64 i + 32 j + wave, + 4, ... of this wave
+      const int s0 = 64 * i + 32 * j;
+      if (s0 + wave >= ns) continue;
+      if (s0 > 0) fetch(s0 + wave);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int s = s0 + 4 * u < ns ? s0 + 4 * u : ns - 1;
-        v[u] = *reinterpret_cast<const vec_t*>(s < n1 ? p1 + (long long)s * D : p2 + (long long)(s - n1) * D);
+        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w[i]), 32 * j + wave + 4 * u));
+        if (s0 + wave + 4 * u < ns && !(f < 0.f)) acc += f * v[u];  // wave-uniform
       }
-    };
-    float2 ml[kPrefixParts / 64];
-#pragma unroll
-    for (int i = 0; i < kPrefixParts / 64; ++i) {
-      const int s = lane + 64 * i;
-      ml[i] = make_float2(-INFINITY, 0.f);
-      if (64 * i < ns && s < ns) ml[i] = s < n1 ? m1[s] : m2[s - n1];
-    }
-    fetch(wave);
-    float mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kPrefixParts / 64; ++i) mx = fmaxf(mx, ml[i].x);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
-    float lsum = 0.f, w[kPrefixParts / 64];
-#pragma unroll
-    for (int i = 0; i < kPrefixParts / 64; ++i) {
-      const bool empty = ml[i].x == -INFINITY;  // (its outputs may be anything)
-      w[i] = empty ? -1.f : __builtin_amdgcn_exp2f(ml[i].x - mx);
-      lsum += empty ? 0.f : w[i] * ml[i].y;
     }
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) lsum += __shfl_xor(lsum, off, 64);
-    vec_t acc = 0.f;
+  for (int c = 0; c < V; ++c) o_s[wave][lane * V + c] = acc[c];
+  __syncthreads();
+  if (threadIdx.x < D / 2) {
+    const int d = 2 * threadIdx.x;
+    float x0 = 0.f, x1 = 0.f;
 #pragma unroll
-    for (int i = 0; i < kPrefixParts / 64; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {  // parts 64 i + 32 j + wave, + 4, ... of this wave
-        const int s0 = 64 * i + 32 * j;
-        if (s0 + wave >= ns) continue;
-        if (s0 > 0) fetch(s0 + wave);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w[i]), 32 * j + wave + 4 * u));
-          if (s0 + wave + 4 * u < ns && !(f < 0.f)) acc += f * v[u];  // wave-uniform
-        }
-      }
-#pragma unroll
-    for (int c = 0; c < V; ++c) o_s[wave][lane * V + c] = acc[c];
-    __syncthreads();
-    if (threadIdx.x < D / 2) {
-      const int d = 2 * threadIdx.x;
-      float x0 = 0.f, x1 = 0.f;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        x0 += o_s[u][d];
-        x1 += o_s[u][d + 1];
-      }
-      const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-      reinterpret_cast<uint32_t*>(a.out + row * D)[threadIdx.x] = pack_bf16(x0 * inv, x1 * inv);
-      if (threadIdx.x == 0 && a.lse != nullptr) a.lse[row] = lsum > 0.f ? (mx + log2f(lsum)) * 0.6931471805599453f : -INFINITY;
+    for (int u = 0; u < 4; ++u) {
+      x0 += o_s[u][d];
+      x1 += o_s[u][d + 1];
     }
-    __syncthreads();  // (the next row's outputs come to the same place)
+    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+    reinterpret_cast<uint32_t*>(a.out + row * D)[threadIdx.x] = pack_bf16(x0 * inv, x1 * inv);
+    if (threadIdx.x == 0 && a.lse != nullptr) a.lse[row] = lsum > 0.f ? (mx + log2f(lsum)) * 0.6931471805599453f : -INFINITY;
   }
 }
 
@@ -580,7 +580,7 @@ int launch_prefix(const Dims& dm, const PrefixPlan& pl, PrefixArgs a, void* ws, 
     hipLaunchKernelGGL(prefix_kernel<64>, grid, dim3(64 * kPrefixWaves), 0, st, a);
   if (hipGetLastError() != hipSuccess) return MSA_ERR_HIP;
   const long long rows = BM * dm.Hq;
-  const dim3 joins((unsigned)(rows < 1 << 20 ? rows : 1 << 20));
+  const dim3 joins((unsigned)(rows < 1 << 20 ? rows : 1 << 20), (unsigned)((rows + (1 << 20) - 1) >> 20));
   if (dm.d == 128)
     hipLaunchKernelGGL(prefix_join_kernel<128>, joins, dim3(256), 0, st, a, rows);
   else
