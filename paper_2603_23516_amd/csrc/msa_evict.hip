@@ -3,7 +3,11 @@
 // Two launches.  evict_select_kernel, a workgroup to a (sequence, KV head), finds the weight of the lightest row that stays (as an
 // integer of the same order, in digits of up to 11 bits from the top, each by counting), then lists the rows that stay in
 // ascending order and moves their weights.  Counted in LDS, where the order of additions changes nothing.  evict_move_kernel copies
-// the rows of K and V.
+// the rows of K and V, 64 to a workgroup.
+//
+// The copy is bound by memory (32 sequences of 8 heads of 128 cut to 4096 rows, 830 MB in and out, 149 us, 5.6 TB/s), the choice by
+// what follows on what in one workgroup: 16384 rows 16 us, of which the first loads 5, a digit 2.6 and the listing 5 (bit by bit with
+// the weights in registers 35, with the weights read for every bit 118; digits of all 32 bits 20).
 #include "msa_device.h"
 #include "msa_host.h"
 

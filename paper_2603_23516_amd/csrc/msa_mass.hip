@@ -8,10 +8,13 @@
 //
 // mass_rows_kernel, up to 64 columns: a wave to 32 rows, all of them and all columns in registers.  Bound by memory: K is read once.
 //
-// mass_tiled_kernel, more columns: a wave keeps 64 rows in registers, the queries come by in steps of 32 columns through LDS.  Per 64 x
-// 32 weights 16 products of 32x32x16 (d = 128) stand against 96 vector instructions of which 32 are exponentials at a quarter of the
-// rate: bound by those and the matrix pipe together.  The columns that a tile of 256 rows needs are shared out to several workgroups,
-// whose sums mass_join_kernel adds in order.
+// mass_tiled_kernel, more columns: a wave keeps 32 rows in registers, the queries come by in steps of 32 columns through LDS, with them
+// the log-sum and the position of every column.  Per 32 x 32 weights stand 8 products of 32x32x16 (d = 128) against 80 vector
+// instructions, of which 48 are the weights (fma, exponential, sum) and 16 of these take twice the time: 8192 tokens of 32 / 8 heads of
+// 128 (275 GFLOP) 330 us, 0.83 PFLOP/s, vector ALU 74 % and matrix pipe 46 % busy.  64 rows to a wave would halve what is not
+// the weights and leave two waves to a SIMD for four: 367.  The columns that a tile of 128 rows needs are shared out to several
+// workgroups, whose sums mass_join_kernel adds in order (2048 workgroups in all: with 1024 362, with 4096 333 and short calls up to
+// 40 % longer; eight steps at least to a part).
 #include "msa_encoded.h"
 
 #include <type_traits>

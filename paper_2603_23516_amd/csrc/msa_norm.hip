@@ -13,7 +13,8 @@
 // passes them around through LDS.
 //
 // msa_norm_rotate_axes is the same pass with several positions per token: the lane that works out angle u takes the position of
-// axis axes[u], and the row of the cache comes with the token (AXES; a variant of its own, so that the other keeps its registers).
+// axis axes[u], and the row of the cache comes with the token (AXES; a variant of its own, so that the other keeps its
+// registers; the same times: 16384 tokens 74 us, 8 tokens 4.2).
 #include "msa_attend.h"
 
 namespace msa {

@@ -1,16 +1,20 @@
 // msa_prefix_attend: one softmax over the rows of a prefix that all sequences share and over the rows of a sequence's own cache.
 //
 // Where a sequence has tokens enough to fill tiles of its own, encoded_tiled_kernel takes them over the prefix and the cache in one
-// go.  With fewer, one launch has workgroups of two kinds:
+// go (8 questions of 128 tokens, 32 / 8 heads of 128, over 16384 + 640 rows 298 us, 0.95 PFLOP/s).  With fewer, one launch has
+// workgroups of two kinds:
 //   over the prefix  tiles of 128 columns, (token, query head) pairs of one KV head and of all sequences together, 32 to a wave, so
-//                    that a row is read once for all of them (per tile); bound by the matrix cores once there are more than a few
-//                    tiles' worth, by memory below that.  As encoded_tiled_kernel, without windows and runs: 32 key and 32 value
-//                    rows a step, global -> LDS asynchronously, two steps ahead.
+//                    that a row is read once for all of them (per tile).  As encoded_tiled_kernel, without windows and runs: 32 key
+//                    and 32 value rows a step, global -> LDS asynchronously, two steps ahead, in n parts of which each takes every
+//                    n-th step.  Bound by memory with one tile (8 tokens over 65536 rows 55 us, 5.2 TB/s), by the matrix pipe and
+//                    the vector ALU with more: a step takes 0.85 us with one workgroup on a CU (64 dims: 0.56).
 //   over the caches  sixteen columns of one (sequence, KV head); the rows go straight from memory into registers, dealt to the
-//                    four waves 32 at a time; bound by memory.
-// Both leave (max, sum, output) parts by (token, head) row, which a launch joins.  Parts over the prefix may be many; the two kinds
-// fill each other's gaps, one at the matrix pipe and one at memory.
-// Softmax weights are rounded to bf16 for the second product (2^-8 of themselves at most), their sum is taken before the rounding.
+//                    four waves 32 at a time.  Bound by memory (64 tokens, up to 1024 rows each, 134 MB: 34 us).
+// Both leave (max, sum, output) parts by (token, head) row, which a launch joins.  The two kinds fill each other's gaps: 64 tokens
+// over 32768 rows 56 us, over the caches 34, both 69.  256 workgroups over the prefix, one to a CU, leave the others of a CU to
+// the caches: with 384, 512 and 768 the call of 80 us takes 81, 89 and 107 (without caches 66: 62, 60, 71).
+// Softmax weights are rounded to bf16 for the second product (2^-8 of themselves at most), their sum is taken before the rounding:
+// as (hi, lo) pairs they would take that product twice.
 #include "msa_prefix.h"
 
 #include <type_traits>
@@ -405,8 +409,8 @@ __global__ __launch_bounds__(64 * kPrefixWaves) __attribute__((amdgpu_waves_per_
 }
 
 // The parts of every (token, head): a workgroup to a row, its waves the parts i, i + 4, ..., eight of them at a time under way
-// together with all (max, sum) pairs.  (A wave to a row, as the other paths join theirs, is one part after another where rows are few
-// and parts many: 256 rows of 68 parts 22 us, 2048 of 33 13.)
+// together with all (max, sum) pairs.  2048 rows of 17 parts 6.4 us.  (A wave to a row, as the other paths join theirs, is one part
+// after another where rows are few and parts many: 256 rows of 68 parts 22 us for 5, 2048 of 33 13 for 8.)
 template <int D>
 __global__ __launch_bounds__(256) void prefix_join_kernel(PrefixArgs a, long long rows) {
   constexpr int V = D / 64, U = 8;
