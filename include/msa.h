@@ -466,8 +466,9 @@ int msa_norm_rotate_axes(const msa_config_t* cfg, const void* q, int64_t q_strid
  *   lse         out  fp32 [B][M][Hq], may be NULL
  *   workspace        >= msa_prefix_attend_workspace_bytes(cfg, B, M, Lpre, Lloc), which does not fall as Lpre or Lloc grows;
  *                    contents undefined on entry/exit
- * B, n_kv_heads <= 65535, B * M <= 2^25, Lpre, Lloc <= 2^28.  Scores, their maximum and sum and the outputs are accumulated in
- * fp32; the softmax weights are rounded to bf16 for the second product (2^-8 relative).
+ * B, n_kv_heads <= 65535, B * M <= 2^25, Lpre, Lloc <= 2^28, and grids that hold the call (about 2^22 groups of 16 (token, head)
+ * pairs of a KV head where a sequence brings fewer than 96 of them, else 2^24 tiles of 128).  Scores, their maximum and sum and the
+ * outputs are accumulated in fp32; the softmax weights are rounded to bf16 for the second product (2^-8 relative).
  */
 size_t msa_prefix_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lpre, int32_t Lloc);
 int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kpre, const void* Vpre,
@@ -494,7 +495,7 @@ int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *   mass_out  out  fp32 [B][Hkv][Lloc]
  *   workspace      >= msa_attend_mass_workspace_bytes(cfg, B, M, Lloc, window, sinks), which does not fall as Lloc, window or
  *                  sinks grow; contents undefined on entry/exit
- * B, n_kv_heads <= 65535, B * M <= 2^25, Lloc <= 2^28.
+ * B, n_kv_heads <= 65535, B * M <= 2^25, Lloc <= 2^28, and fewer than 2^24 blocks of 128 rows in all.
  */
 size_t msa_attend_mass_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lloc, int32_t window,
                                        int32_t sinks);

@@ -31,6 +31,7 @@ def _call(lib, cfg, **kw):
     (dict(B=0), -1), (dict(M=0), -1), (dict(L=0), -1), (dict(W=0), -1), (dict(S=-1), -1), (dict(pos0=-1), -1),
     (dict(decay=-0.1), -1), (dict(decay=1.5), -1), (dict(decay=float("nan")), -1),
     (dict(B=65536), -2), (dict(B=1 << 13, M=1 << 13), -2), (dict(L=(1 << 28) + 1), -2), (dict(bytes=255), -3),
+    (dict(B=4, L=1 << 28), -2), (dict(B=4, M=100, L=1 << 28), -2),      # 2^24 blocks of 128 rows
     (dict(q=ctypes.c_void_p(0x10008)), -4), (dict(K=ctypes.c_void_p(0x10002)), -4), (dict(q_pos=ctypes.c_void_p(0x10002)), -4),
     (dict(lse=ctypes.c_void_p(0x10002)), -4), (dict(mass=ctypes.c_void_p(0x10002)), -4), (dict(out=ctypes.c_void_p(0x10002)), -4),
     (dict(ws=ctypes.c_void_p(0x10010 + 4)), -4),
