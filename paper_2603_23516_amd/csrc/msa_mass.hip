@@ -6,7 +6,8 @@
 // row at the end.  Nothing depends on an order of arrival.  Queries and keys are bf16 as given, products and sums fp32: nothing is
 // rounded to fewer bits.
 //
-// mass_rows_kernel, up to 64 columns: a wave to 32 rows, all of them and all columns in registers.  Bound by memory: K is read once.
+// mass_rows_kernel, up to 64 columns: a wave to 32 rows, all of them and all columns in registers.  Bound by memory: K is read once,
+// and of it the blocks of 32 rows that some column sees (16 sequences of 8192 rows under a window of 1024 33 us, so 15).
 //
 // mass_tiled_kernel, more columns: a wave keeps 32 rows in registers, the queries come by in steps of 32 columns through LDS, with them
 // the log-sum and the position of every column.  Per 32 x 32 weights stand 8 products of 32x32x16 (d = 128) against 80 vector
@@ -36,23 +37,26 @@ __device__ __forceinline__ SeenBy seen_by(const MassArgs& a, int32_t q_pos) {
   s.lo = lo < 0 ? 0 : lo;
   return s;
 }
+// Bits 0 to x; none for x < 0, all for x > 30.
+__device__ __forceinline__ uint32_t up_to(int x) { return x < 0 ? 0u : ~0u >> (x < 31 ? 31 - x : 0); }
 __device__ __forceinline__ float old_weight(const MassArgs& a, long long at) {
   return a.mass != nullptr && a.decay != 0.f ? a.mass[at] * a.decay : 0.f;
 }
 
 // ---- few columns ---------------------------------------------------------------------------------------------------------
-// (A wave to 32 rows and eight of them to a SIMD: 40 sequences of 8192 rows, 8 heads of 128, 115 us, 6.0 TB/s, of 0 to 8192 rows,
-// 4000 on average, 72.  Waves that go on through 64 to 512 rows with one or two blocks ahead 120 to 139 and 88 to 93; 64 rows at once
-// 119 and 73; workgroups by rows first and sequences second 127 and 79.)
+// (A wave to 32 rows, a workgroup of its own, and eight of them to a SIMD: 40 sequences of 8192 rows, 8 heads of 128, 114 us, 6.0 TB/s,
+// of 0 to 8192 rows, 4000 on average, 67.  Two, four, eight and sixteen waves to a workgroup 116, 114, 118, 121 and 69, 72, 77, 80; waves
+// that go on through 64 to 512 rows with one or two blocks ahead 120 to 139 and 88 to 93; 64 rows at once 119 and 73; workgroups by rows
+// first and sequences second 127 and 79.)
+constexpr int kRowsRows = 32;  // rows of a wave
 template <int D, int CG>  // CG: groups of 16 columns
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 : 1))) void mass_rows_kernel(MassArgs a, int n_blocks) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 : 1))) void mass_rows_kernel(MassArgs a, int n_blocks) {
   constexpr int NS = D / 32;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x;
   const int qd = lane >> 4, n = lane & 15, r = a.r;
   const long long pair = blockIdx.x / n_blocks;
-  const int t0 = ((int)(blockIdx.x % n_blocks) * 4 + wave) * 32;
-  if (t0 >= a.Lloc) return;  // no barrier below
+  const int t0 = (int)(blockIdx.x % n_blocks) * kRowsRows;
+  if (t0 >= a.Lloc) return;
   const int g = (int)(pair % a.Hkv);
   const long long b = pair / a.Hkv;
   const int cols = a.M * r;
@@ -66,7 +70,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8
   bf16x8_t q[CG][NS];
   float ls[CG];
   SeenBy see[CG];
-  int most = -1;  // the last row that any column sees
+  int most = -1, least = INT32_MAX;  // the last row that any column sees, and the first one of the windows
 #pragma unroll
   for (int c = 0; c < CG; ++c) {
     const int at = 16 * c + n, col = at < cols ? at : cols - 1;
@@ -75,22 +79,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8
     ls[c] = a.lse[qh] * kLog2e;
     if (at >= cols || ls[c] == -INFINITY) see[c].p = -1;  // (a token that saw nothing)
     most = see[c].p > most ? see[c].p : most;
+    least = see[c].p >= 0 && see[c].lo < least ? see[c].lo : least;
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[c][s] = as_bf16x8(*reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd));
   }
 #pragma unroll
   for (int off = 8; off > 0; off >>= 1) {
-    const int v = __shfl_xor(most, off, 64);
+    const int u = __shfl_xor(least, off, 64), v = __shfl_xor(most, off, 64);
+    least = u < least ? u : least;
     most = v > most ? v : most;
   }
   most = __builtin_amdgcn_readfirstlane(most);
-  if (t0 > most && a.mass == a.out && a.decay == 1.f) return;  // rows that nobody sees, in place: as they are
+  least = __builtin_amdgcn_readfirstlane(least);
+  const bool seen = t0 <= most && (t0 + kRowsRows > least || t0 < a.sinks);  // wave-uniform
+  if (!seen && a.mass == a.out && a.decay == 1.f) return;  // rows that nobody sees, in place: as they are
   float sum[2][4];
 #pragma unroll
   for (int k = 0; k < 2; ++k)
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[k][i] = 0.f;
-  if (t0 <= most) {  // wave-uniform
+  if (seen) {
     const uint16_t* const keys = a.Kloc + pair * a.Lloc * D + 8 * qd;
     u32x4_t key[2][NS];
 #pragma unroll
@@ -146,6 +154,7 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
   constexpr int TILE = 32 * ROW;          // bytes of a step's queries
   constexpr int NPW = 32 * NP / 64 / NW;  // copies of a wave per step
   static_assert(NPW >= 1, "a step is a whole number of copies per wave");
+  static_assert(KT == 1, "a column's rows of a wave are the bits of a word");
   constexpr int SIDE = NW * 256;           // behind them, for every wave: 32 log-sums and 32 positions
   __shared__ __attribute__((aligned(16))) unsigned char smem[STAGES * (TILE + SIDE)];
   __shared__ int lo_s[NW], hi_s[NW];
@@ -189,8 +198,16 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
   }
   s_lo = __builtin_amdgcn_readfirstlane(s_lo) / pp.tpw;
   s_hi = __builtin_amdgcn_readfirstlane(s_hi);
-  const int n_steps = s_hi < 0 ? 0 : s_hi / pp.tpw + 1 - s_lo;
-  if (n_steps == 0) s_lo = 0;
+  if (s_hi < 0) {  // nobody sees the tile: most of a long cache's behind a window
+    for (int t = tile0 + tid; t <= tile1; t += NW * 64) {
+      if (pp.n_parts > 1)
+        pp.part[(pair * pp.n_parts + part) * a.Lloc + t] = 0.f;
+      else
+        a.out[pair * a.Lloc + t] = old_weight(a, pair * a.Lloc + t);
+    }
+    return;
+  }
+  const int n_steps = s_hi / pp.tpw + 1 - s_lo;
   const int sb = s_lo + (int)((long long)n_steps * part / pp.n_parts);
   const int se = s_lo + (int)((long long)n_steps * (part + 1) / pp.n_parts);
 
@@ -288,14 +305,15 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
           for (int i = 0; i < 16; ++i) sum[k][i] += __builtin_amdgcn_exp2f(fmaf(sc[k][i], a.qscale, nls));
       } else {
-        const int most = see.p - t0 - 4 * hf, least = see.lo - t0 - 4 * hf, few = a.sinks - t0 - 4 * hf;
+        // bit i: the column sees row t0 + 4 hf + i  (a weight is kept by an and, in two instructions; with three compares five)
+        const uint32_t bits = (up_to(see.p - t0) & (~up_to(see.lo - 1 - t0) | up_to(a.sinks - 1 - t0))) >> (4 * hf);
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int t = 32 * k + (i & 3) + 8 * (i >> 2);
+            const int t = (i & 3) + 8 * (i >> 2);
             const float w = __builtin_amdgcn_exp2f(fmaf(sc[k][i], a.qscale, nls));
-            sum[k][i] += (t <= most) & ((t >= least) | (t < few)) ? w : 0.f;
+            sum[k][i] += __uint_as_float(__float_as_uint(w) & (uint32_t)((int32_t)(bits << (31 - t)) >> 31));
           }
       }
     };
@@ -348,11 +366,11 @@ MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks
   const long long pairs = (long long)B * dm.Hkv;
   p.ws_bytes = 256;
   if (M * dm.r <= 64) {
-    p.n_blocks = (Lloc + 127) / 128;
     // An odd number to a (sequence, KV head): an even one puts the same blocks of all of them, and with them the ones behind the
-    // sequences' ends, on the same XCDs and shader engines.  (40 sequences of 0 to 8192 rows 83 us, so 72; one of 8192 6.5, so 7.2.)
-    if (B > 1 && pairs * p.n_blocks >= 4096) p.n_blocks |= 1;
-    if (pairs * p.n_blocks >= 1 << 24) p.ws_bytes = 0;
+    // sequences' ends, on the same XCDs and shader engines.  (40 sequences of 0 to 8192 rows 70.6 us, so 67.4; 8 of 0 to 4096
+    // 12.6, so 10.7; one of 8192 6.4, so 6.2.)
+    p.n_blocks = ((Lloc + kRowsRows - 1) / kRowsRows) | 1;
+    if (pairs * p.n_blocks >= 1 << 26) p.ws_bytes = 0;
     return p;
   }
   p.tiled = 1;
@@ -379,7 +397,7 @@ int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws,
   a.qscale = (float)(1.4426950408889634 / sqrt((double)dm.d));
   const long long pairs = (long long)B * dm.Hkv;
   if (!pl.tiled) {
-    const dim3 grid((unsigned)(pairs * pl.n_blocks)), block(256);
+    const dim3 grid((unsigned)(pairs * pl.n_blocks)), block(64);
     const int groups = (a.M * dm.r + 15) / 16;
 #define MSA_MASS(DD, CC) hipLaunchKernelGGL((mass_rows_kernel<DD, CC>), grid, block, 0, st, a, pl.n_blocks)
 #define MSA_MASS_OF(DD)            \
