@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long long pair = blockIdx.x;
-  int n = a.lens[pair / a.Hkv];
+  int n = a.lens[blockIdx.x / (unsigned)a.Hkv];
   n = n < 0 ? 0 : (n > a.Lloc ? a.Lloc : n);
   const float* const mass = a.mass + pair * a.Lloc;
   float* const mass_out = a.mass_out + pair * a.Lout;
@@ -245,9 +245,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 template <int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int chunks) {
   constexpr int LPR = D / 8, RPB = 256 / LPR, TURNS = 4;
-  const long long x = blockIdx.x;
-  const int chunk = (int)(x % chunks);
-  const long long pair = x / chunks;
+  const int chunk = (int)(blockIdx.x % (unsigned)chunks);
+  const long long pair = blockIdx.x / (unsigned)chunks;
   const int lr = threadIdx.x % LPR, j0 = chunk * (RPB * TURNS) + threadIdx.x / LPR;
   const int32_t* const rows = a.rows + pair * a.keep;
   const uint16_t* const src = (blockIdx.y == 0 ? a.K : a.V) + pair * a.Lloc * D + 8 * lr;

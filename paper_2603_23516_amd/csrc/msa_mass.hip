@@ -54,11 +54,11 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 
   constexpr int NS = D / 32;
   const int lane = threadIdx.x;
   const int qd = lane >> 4, n = lane & 15, r = a.r;
-  const long long pair = blockIdx.x / n_blocks;
-  const int t0 = (int)(blockIdx.x % n_blocks) * kRowsRows;
+  const unsigned of = blockIdx.x / (unsigned)n_blocks;
+  const int t0 = (int)(blockIdx.x - of * n_blocks) * kRowsRows;
   if (t0 >= a.Lloc) return;
-  const int g = (int)(pair % a.Hkv);
-  const long long b = pair / a.Hkv;
+  const int g = (int)(of % (unsigned)a.Hkv);
+  const long long b = of / (unsigned)a.Hkv, pair = of;
   const int cols = a.M * r;
   const bool weighed = a.mass != nullptr && a.decay != 0.f;
   float old[2];  // of row 4 qd + n % 4 of either half of the 32
@@ -352,9 +352,9 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
 }
 
 __global__ __launch_bounds__(256) void mass_join_kernel(MassArgs a, const float* part, int n_parts, long long n) {
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const unsigned at = blockIdx.x * 256 + threadIdx.x;  // (n < 2^18: tiles in parts are fewer than kMassItems)
   if (at >= n) return;
-  const long long pair = at / a.Lloc;
+  const long long pair = at / (unsigned)a.Lloc;
   const float* const p = part + pair * n_parts * a.Lloc + (at - pair * a.Lloc);
   float v = old_weight(a, at);
   for (int i = 0; i < n_parts; ++i) v += p[(long long)i * a.Lloc];
