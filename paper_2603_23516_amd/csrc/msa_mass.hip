@@ -7,7 +7,8 @@
 // rounded to fewer bits.
 //
 // mass_rows_kernel, up to 64 columns: a wave to 32 rows, all of them and all columns in registers.  Bound by memory: K is read once,
-// and of it the blocks of 32 rows that some column sees (16 sequences of 8192 rows under a window of 1024 33 us, so 15).
+// and of it the blocks of 32 rows that some column sees (16 sequences of 8192 rows under a window of 1024 13.4 us,
+// without that 32).
 //
 // mass_tiled_kernel, more columns: a wave keeps 32 rows in registers, the queries come by in steps of 32 columns through LDS, with them
 // the log-sum and the position of every column.  Per 32 x 32 weights stand 8 products of 32x32x16 (d = 128) against 80 vector
@@ -47,18 +48,17 @@ __device__ __forceinline__ float old_weight(const MassArgs& a, long long at) {
 // (A wave to 32 rows, a workgroup of its own, and eight of them to a SIMD: 40 sequences of 8192 rows, 8 heads of 128, 114 us, 6.0 TB/s,
 // of 0 to 8192 rows, 4000 on average, 67.  Two, four, eight and sixteen waves to a workgroup 116, 114, 118, 121 and 69, 72, 77, 80; waves
 // that go on through 64 to 512 rows with one or two blocks ahead 120 to 139 and 88 to 93; 64 rows at once 119 and 73; workgroups by rows
-// first and sequences second 127 and 79.)
+// first and sequences second 127 and 79.  What a wave does ahead of its rows counts, since half of the waves have none: workgroup
+// numbers and columns taken apart by division and their ends compared through LDS 115 and 69.)
 constexpr int kRowsRows = 32;  // rows of a wave
 template <int D, int CG>  // CG: groups of 16 columns
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 : 1))) void mass_rows_kernel(MassArgs a, int n_blocks) {
-  constexpr int NS = D / 32;
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 : 1))) void mass_rows_kernel(MassArgs a, uint32_t by_r) {
+  constexpr int NS = D / 32;  // by_r: 2^16 / r and one more, so that col / r = col by_r / 2^16 for all 64 columns
   const int lane = threadIdx.x;
   const int qd = lane >> 4, n = lane & 15, r = a.r;
-  const unsigned of = blockIdx.x / (unsigned)n_blocks;
-  const int t0 = (int)(blockIdx.x - of * n_blocks) * kRowsRows;
+  const int t0 = (int)blockIdx.x * kRowsRows, g = blockIdx.y;
   if (t0 >= a.Lloc) return;
-  const int g = (int)(of % (unsigned)a.Hkv);
-  const long long b = of / (unsigned)a.Hkv, pair = of;
+  const long long b = blockIdx.z, pair = b * a.Hkv + g;
   const int cols = a.M * r;
   const bool weighed = a.mass != nullptr && a.decay != 0.f;
   float old[2];  // of row 4 qd + n % 4 of either half of the 32
@@ -74,7 +74,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 
 #pragma unroll
   for (int c = 0; c < CG; ++c) {
     const int at = 16 * c + n, col = at < cols ? at : cols - 1;
-    const long long tok = b * a.M + col / r, qh = tok * a.Hq + g * r + col % r;
+    const int m = (int)((uint32_t)col * by_r >> 16);
+    const long long tok = b * a.M + m, qh = tok * a.Hq + g * r + (col - m * r);
     see[c] = seen_by(a, a.q_pos[tok]);
     ls[c] = a.lse[qh] * kLog2e;
     if (at >= cols || ls[c] == -INFINITY) see[c].p = -1;  // (a token that saw nothing)
@@ -83,12 +84,14 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[c][s] = as_bf16x8(*reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd));
   }
-#pragma unroll
-  for (int off = 8; off > 0; off >>= 1) {
-    const int u = __shfl_xor(least, off, 64), v = __shfl_xor(most, off, 64);
-    least = u < least ? u : least;
-    most = v > most ? v : most;
-  }
+  auto over_16 = [](int x, auto f) {  // over the lanes of a quarter
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppXor1, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppXor2, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppHalfMirror, 0xf, 0xf, false));
+    return f(x, __builtin_amdgcn_update_dpp(0, x, kDppMirror, 0xf, 0xf, false));
+  };
+  most = over_16(most, [](int x, int y) { return x > y ? x : y; });
+  least = over_16(least, [](int x, int y) { return x < y ? x : y; });
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
   const bool seen = t0 <= most && (t0 + kRowsRows > least || t0 < a.sinks);  // wave-uniform
@@ -397,9 +400,10 @@ int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws,
   a.qscale = (float)(1.4426950408889634 / sqrt((double)dm.d));
   const long long pairs = (long long)B * dm.Hkv;
   if (!pl.tiled) {
-    const dim3 grid((unsigned)(pairs * pl.n_blocks)), block(64);
+    const dim3 grid((unsigned)pl.n_blocks, (unsigned)dm.Hkv, (unsigned)B), block(64);
+    const uint32_t by_r = 65536u / dm.r + 1;
     const int groups = (a.M * dm.r + 15) / 16;
-#define MSA_MASS(DD, CC) hipLaunchKernelGGL((mass_rows_kernel<DD, CC>), grid, block, 0, st, a, pl.n_blocks)
+#define MSA_MASS(DD, CC) hipLaunchKernelGGL((mass_rows_kernel<DD, CC>), grid, block, 0, st, a, by_r)
 #define MSA_MASS_OF(DD)            \
   if (groups == 1) MSA_MASS(DD, 1); \
   else if (groups == 2) MSA_MASS(DD, 2); \
