@@ -175,6 +175,37 @@ __device__ __forceinline__ float add_over_16(float x) {
   x += dpp_f<kDppHalfMirror>(x);
   return x + dpp_f<kDppMirror>(x);
 }
+// f of the sixteen lanes' x that share lane / 16, in all of them.
+template <class F>
+__device__ __forceinline__ int over_16(int x, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppXor1, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppXor2, 0xf, 0xf, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppHalfMirror, 0xf, 0xf, false));
+  return f(x, __builtin_amdgcn_update_dpp(0, x, kDppMirror, 0xf, 0xf, false));
+}
+// The smallest and the largest x of the first N lanes (N in {16, 32, 64}), a scalar.
+template <int N>
+__device__ __forceinline__ int min_of_lanes(int x) {
+  x = over_16(x, [](int a, int b) { return a < b ? a : b; });
+  int m = __builtin_amdgcn_readlane(x, 0);
+#pragma unroll
+  for (int i = 16; i < N; i += 16) {
+    const int v = __builtin_amdgcn_readlane(x, i);
+    m = v < m ? v : m;
+  }
+  return m;
+}
+template <int N>
+__device__ __forceinline__ int max_of_lanes(int x) {
+  x = over_16(x, [](int a, int b) { return a > b ? a : b; });
+  int m = __builtin_amdgcn_readlane(x, 0);
+#pragma unroll
+  for (int i = 16; i < N; i += 16) {
+    const int v = __builtin_amdgcn_readlane(x, i);
+    m = v > m ? v : m;
+  }
+  return m;
+}
 // x summed over the lanes that share lane % LPR (LPR in {4, 8, 16}).
 template <int LPR>
 __device__ __forceinline__ float add_row_groups(float x) {

@@ -107,15 +107,7 @@ void encoded_tiled_kernel(EncodedArgs a, TiledArgs ta) {
   }
   int lo = p - a.window + 1;
   if (lo < 0) lo = 0;  // (differences from it stay in 32 bits)
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const int u = __shfl_xor(pmin, off, 64), v = __shfl_xor(pmax, off, 64), w = __shfl_xor(plow, off, 64);
-    pmin = u < pmin ? u : pmin;
-    pmax = v > pmax ? v : pmax;
-    plow = w < plow ? w : plow;
-  }
-  const int pmin_w = __builtin_amdgcn_readfirstlane(pmin), pmax_w = __builtin_amdgcn_readfirstlane(pmax);
-  const int plow_w = __builtin_amdgcn_readfirstlane(plow);
+  const int pmin_w = min_of_lanes<32>(pmin), pmax_w = max_of_lanes<32>(pmax), plow_w = min_of_lanes<32>(plow);
   if (lane == 0) {
     pmin_s[wave] = plow_w;
     pmax_s[wave] = pmax_w;

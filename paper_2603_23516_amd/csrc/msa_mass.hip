@@ -84,16 +84,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(CG == 1 ? 8 
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[c][s] = as_bf16x8(*reinterpret_cast<const uint4*>(a.q + qh * D + 32 * s + 8 * qd));
   }
-  auto over_16 = [](int x, auto f) {  // over the lanes of a quarter
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppXor1, 0xf, 0xf, false));
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppXor2, 0xf, 0xf, false));
-    x = f(x, __builtin_amdgcn_update_dpp(0, x, kDppHalfMirror, 0xf, 0xf, false));
-    return f(x, __builtin_amdgcn_update_dpp(0, x, kDppMirror, 0xf, 0xf, false));
-  };
-  most = over_16(most, [](int x, int y) { return x > y ? x : y; });
-  least = over_16(least, [](int x, int y) { return x < y ? x : y; });
-  most = __builtin_amdgcn_readfirstlane(most);
-  least = __builtin_amdgcn_readfirstlane(least);
+  most = max_of_lanes<16>(most);
+  least = min_of_lanes<16>(least);
   const bool seen = t0 <= most && (t0 + kRowsRows > least || t0 < a.sinks);  // wave-uniform
   if (!seen && a.mass == a.out && a.decay == 1.f) return;  // rows that nobody sees, in place: as they are
   float sum[2][4];
@@ -148,6 +140,7 @@ constexpr long long kMassItems = 2048;  // fewer tiles than this: their columns 
 struct MassParts {
   float* part;      // [B * Hkv][n_parts][Lloc] sums of the parts, n_parts > 1
   int n_parts, n_tiles, tpw;  // tpw: tokens per step
+  uint32_t by_r;              // as in mass_rows_kernel
 };
 
 template <int D>
@@ -183,12 +176,8 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
       s_hi = m;
     }
   }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const int u = __shfl_xor(s_lo, off, 64), v = __shfl_xor(s_hi, off, 64);
-    s_lo = u < s_lo ? u : s_lo;
-    s_hi = v > s_hi ? v : s_hi;
-  }
+  s_lo = min_of_lanes<64>(s_lo);
+  s_hi = max_of_lanes<64>(s_hi);
   if (lane == 0) {
     lo_s[wave] = s_lo;
     hi_s[wave] = s_hi;
@@ -243,10 +232,10 @@ __global__ __launch_bounds__(kMassWaves * 64) __attribute__((amdgpu_waves_per_eu
       const int y = (i * NW + wave) * 64 + lane, row = y / NP;
       int c = row;
       if (c >= pp.tpw * r) c = 0;
-      ctok[i] = c / r;
-      coff[i] = (c % r) * ROW + ((y % NP) ^ swz(row)) * 16;
+      ctok[i] = (int)((uint32_t)c * pp.by_r >> 16);
+      coff[i] = (c - ctok[i] * r) * ROW + ((y % NP) ^ swz(row)) * 16;
     }
-    int my_tok = col / r, my_head = col - my_tok * r;
+    int my_tok = (int)((uint32_t)col * pp.by_r >> 16), my_head = col - my_tok * r;
     const bool col_ok = my_tok < pp.tpw;
     if (!col_ok) my_tok = my_head = 0;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem));
@@ -399,9 +388,9 @@ int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws,
   a.r = dm.r;
   a.qscale = (float)(1.4426950408889634 / sqrt((double)dm.d));
   const long long pairs = (long long)B * dm.Hkv;
+  const uint32_t by_r = 65536u / dm.r + 1;
   if (!pl.tiled) {
     const dim3 grid((unsigned)pl.n_blocks, (unsigned)dm.Hkv, (unsigned)B), block(64);
-    const uint32_t by_r = 65536u / dm.r + 1;
     const int groups = (a.M * dm.r + 15) / 16;
 #define MSA_MASS(DD, CC) hipLaunchKernelGGL((mass_rows_kernel<DD, CC>), grid, block, 0, st, a, by_r)
 #define MSA_MASS_OF(DD)            \
@@ -417,7 +406,7 @@ int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws,
 #undef MSA_MASS
     return hipGetLastError() == hipSuccess ? MSA_OK : MSA_ERR_HIP;
   }
-  const MassParts pp = {(float*)ws, pl.n_parts, pl.n_tiles, pl.tpw};
+  const MassParts pp = {(float*)ws, pl.n_parts, pl.n_tiles, pl.tpw, by_r};
   const dim3 grid((unsigned)(pairs * pl.n_tiles * pl.n_parts));
   if (dm.d == 128)
     hipLaunchKernelGGL(mass_tiled_kernel<128>, grid, dim3(kMassWaves * 64), 0, st, a, pp);

@@ -160,14 +160,8 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
     bq[s] = as_bf16x8(keep_if(*reinterpret_cast<const uint4*>(a.q + qh * D + 8 * hf + 16 * s), ok));
   const int lim = ok ? prefix_of(a, tok / a.M) : 0;
   int least = ok ? lim : INT32_MAX, most = lim;
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const int u = __shfl_xor(least, off, 64), v = __shfl_xor(most, off, 64);
-    least = u < least ? u : least;
-    most = v > most ? v : most;
-  }
-  least = __builtin_amdgcn_readfirstlane(least);
-  most = __builtin_amdgcn_readfirstlane(most);
+  least = min_of_lanes<32>(least);
+  most = max_of_lanes<32>(most);
   int* const most_s = reinterpret_cast<int*>(smem);
   if (lane == 0) most_s[wave] = most;
   __syncthreads();
@@ -322,15 +316,8 @@ __device__ __forceinline__ CacheColumn cache_column(const PrefixArgs& a, long lo
   c.head = c.ok ? n - tl * a.r : 0;
   const long long p1 = (long long)a.q_pos[b * a.M + c.tok] - a.pos0 + 1;
   c.lim = c.ok ? (p1 < 0 ? 0 : (p1 < a.Lloc ? (int)p1 : a.Lloc)) : 0;
-  int least = c.ok ? c.lim : INT32_MAX, most = c.lim;
-#pragma unroll
-  for (int off = 8; off > 0; off >>= 1) {
-    const int u = __shfl_xor(least, off, 64), v = __shfl_xor(most, off, 64);
-    least = u < least ? u : least;
-    most = v > most ? v : most;
-  }
-  c.least = __builtin_amdgcn_readfirstlane(least);
-  c.most = __builtin_amdgcn_readfirstlane(most);
+  c.least = min_of_lanes<16>(c.ok ? c.lim : INT32_MAX);
+  c.most = max_of_lanes<16>(c.lim);
   return c;
 }
 
