@@ -590,8 +590,7 @@ int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_
   a.M = M;
   a.Lloc = Lloc;
   a.pos0 = local_pos0;
-  a.window = INT32_MAX;
-  a.sinks = 0;
+  no_window(&a);
   return launch_encoded(dm, pl, a, B, workspace, (hipStream_t)stream);
 }
 

@@ -29,6 +29,10 @@ struct EncodedArgs {
   float qscale;            // log2(e) / sqrt(d)
 };
 
+// No window: every row up to a token's own is a first one.  (The longest window alone is one row short of what the last position
+// of 32 bits sees.)
+inline void no_window(EncodedArgs* a) { a->window = a->sinks = INT32_MAX; }
+
 struct TiledArgs {
   uint16_t *Kx, *Vx;  // [B][Hkv][mem_cap][D] rows of the selected documents in bf16, or null
   int* mem_rows;      // [B][Hkv] how many there are

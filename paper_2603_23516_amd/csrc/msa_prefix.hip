@@ -536,7 +536,7 @@ int launch_prefix(const Dims& dm, const PrefixPlan& pl, PrefixArgs a, void* ws, 
     e.r = a.r;
     e.Lloc = a.Lloc;
     e.pos0 = a.pos0;
-    e.window = INT32_MAX;
+    no_window(&e);
     e.n_splits = pl.tiles.n_splits;
     e.qscale = a.qscale;
     if (e.n_splits == 2) e.tickets = (unsigned long long*)(w + pl.tiles.off_tickets);

@@ -1,0 +1,35 @@
+"""Operators of a served cache at positions at the end of what 32 bits hold, against the plain definitions in 64 bits."""
+import pytest
+import torch
+
+import test_prefix_attend as prefix_of
+import test_sparse_attend4 as sparse4_of
+
+LAST = 2 ** 31 - 1
+
+
+# ---- a token at the last position sees every row that there is ---------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("B, M, Hq, Hkv", [(3, 2, 8, 1), (3, 16, 8, 1), (4, 24, 4, 1), (3, 128, 2, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prefix_attend_at_the_last_position(B, M, Hq, Hkv, d):
+    """Tokens of all sequences in a tile, and a sequence's own (96 columns a sequence and 384 in all); lengths of the prefix below
+    zero and past its end."""
+    x = prefix_of._make(B, M, Hq, Hkv, d, 130, 70, B + M)
+    lens = torch.tensor([-3, 500, 0, 64][:B], dtype=torch.int32)
+    q_pos = torch.full((B, M), LAST, dtype=torch.int32)
+    prefix_of._check(Hq, Hkv, d, *x, q_pos, 0, lens)
+    q_pos[:, ::2] = (torch.arange(M)[::2] % 71 - 1).to(torch.int32)      # beside tokens that see part of the cache, or nothing of it
+    prefix_of._check(Hq, Hkv, d, *x, q_pos, 0, lens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M, pool", [(2, 0), (3, 1), (40, 1)])
+def test_sparse_attend4_at_the_last_position(M, pool):
+    B, N, Hkv, k = 2, 9, 2, 2
+    g = torch.Generator().manual_seed(M)
+    idx = torch.stack([torch.randperm(N, generator=g)[:k] for _ in range(B * (1 if pool else M) * Hkv)])
+    idx = idx.reshape(B, 1 if pool else M, Hkv, k).to(torch.int32)
+    q_pos = torch.full((B, M), LAST, dtype=torch.int32)
+    q_pos[0, 1] = 5
+    sparse4_of._check(N, 4, 8, Hkv, 64, B, M, k, 33, 0, pool, None, idx, q_pos, 0)
