@@ -607,13 +607,20 @@ def msa_unpack_kv4(cfg, bank, doc_begin=0, doc_count=None, K=None, V=None, strea
     return K, V
 
 
-_MOST = 2 ** 31 - 1  # as many rows as there can be: a longer window, or more first tokens, see the same
+_MOST = 2 ** 31 - 1
+
+
+def _window(window, sinks):
+    """A window and a number of first tokens of any size as the library takes them.  2^31 - 1 first tokens are all that there can be; the
+    window of 2^31 - 1 is short of one row that the last position sees, so a longer one makes every row a first one."""
+    if window > _MOST and sinks >= 0:
+        sinks = _MOST
+    return _i32(min(window, _MOST), "window"), _i32(min(sinks, _MOST), "sinks")
 
 
 def window_attend_workspace_bytes(cfg, B, M, Lloc, window, sinks=0):
     return load_library().msa_window_attend_workspace_bytes(ctypes.byref(cfg), _i32(B, "B"), _i32(M, "M"), _i32(Lloc, "Lloc"),
-                                                            _i32(min(window, _MOST), "window"),
-                                                            _i32(min(sinks, _MOST), "sinks"))
+                                                            *_window(window, sinks))
 
 
 def sparse_attend4_workspace_bytes(cfg, B, M, k, Lloc):
@@ -633,7 +640,7 @@ def msa_window_attend(cfg, q, Kloc, Vloc, q_pos, window, sinks=0, local_pos0=0, 
     (out bf16 like q, lse fp32 [B][M][Hq]): attention over the last `window` tokens and the first `sinks`."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     dev = _gpu(q, "q")
-    window, sinks = _i32(min(window, _MOST), "window"), _i32(min(sinks, _MOST), "sinks")
+    window, sinks = _window(window, sinks)
     if q.dim() != 4 or Kloc.dim() != 4:
         raise ValueError("msa_window_attend: expected q [B][M][Hq][d] and Kloc [B][Hkv][Lloc][d]")
     B, M, Lloc = q.shape[0], q.shape[1], Kloc.shape[2]
@@ -721,8 +728,7 @@ def msa_prefix_attend(cfg, q, Kpre, Vpre, Kloc, Vloc, q_pos, local_pos0=0, prefi
 
 def attend_mass_workspace_bytes(cfg, B, M, Lloc, window, sinks=0):
     return load_library().msa_attend_mass_workspace_bytes(ctypes.byref(cfg), _i32(B, "B"), _i32(M, "M"), _i32(Lloc, "Lloc"),
-                                                          _i32(min(window, _MOST), "window"),
-                                                          _i32(min(sinks, _MOST), "sinks"))
+                                                          *_window(window, sinks))
 
 
 def msa_attend_mass(cfg, q, Kloc, lse, q_pos, window, sinks=0, local_pos0=0, mass=None, decay=1.0, out=None, workspace=None,
@@ -732,7 +738,7 @@ def msa_attend_mass(cfg, q, Kloc, lse, q_pos, window, sinks=0, local_pos0=0, mas
     msa_window_attend).  out may be mass."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     dev = _gpu(q, "q")
-    window, sinks = _i32(min(window, _MOST), "window"), _i32(min(sinks, _MOST), "sinks")
+    window, sinks = _window(window, sinks)
     if q.dim() != 4 or Kloc.dim() != 4:
         raise ValueError("msa_attend_mass: expected q [B][M][Hq][d] and Kloc [B][Hkv][Lloc][d]")
     B, M, Lloc = q.shape[0], q.shape[1], Kloc.shape[2]

@@ -2,10 +2,17 @@
 import pytest
 import torch
 
+import paper_2603_23516_amd as msa
+import plain64 as P
+import plain64_cache as C
 import test_prefix_attend as prefix_of
 import test_sparse_attend4 as sparse4_of
 
 LAST = 2 ** 31 - 1
+
+
+def _cfg(Hq=8, Hkv=2, d=64):
+    return msa.MsaConfig(1, 1, 1, Hq, Hkv, d, 1e4)
 
 
 # ---- a token at the last position sees every row that there is ---------------------------------------------------------------
@@ -33,3 +40,20 @@ def test_sparse_attend4_at_the_last_position(M, pool):
     q_pos = torch.full((B, M), LAST, dtype=torch.int32)
     q_pos[0, 1] = 5
     sparse4_of._check(N, 4, 8, Hkv, 64, B, M, k, 33, 0, pool, None, idx, q_pos, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [2, 40, 130])
+def test_windows_past_32_bits_at_the_last_position(M):
+    """A window of 2^31 and more holds every row up to a token's own; one of 2^31 - 1 has lost the first row by then."""
+    B, Hq, Hkv, d, L = 2, 4, 2, 64, 90
+    q, _, _, K, V = prefix_of._make(B, M, Hq, Hkv, d, 1, L, M)
+    q_pos = torch.full((B, M), LAST, dtype=torch.int32)
+    q_pos[0, 1] = 33
+    cfg = _cfg(Hq, Hkv, d)
+    for W in (2 ** 31, 2 ** 40, LAST):
+        out, lse = msa.msa_window_attend(cfg, q.cuda(), K.cuda(), V.cuda(), q_pos.cuda(), W)
+        P.window_attend(q.double(), K.double(), V.double(), q_pos, W, 0, 0).check(out, lse)
+        mass = msa.msa_attend_mass(cfg, q.cuda(), K.cuda(), lse, q_pos.cuda(), W)
+        want, tol = C.attend_mass(q.double(), K.double(), lse.double().cpu(), q_pos, W, 0, 0, None, 1.0)
+        assert bool(((mass.double().cpu() - want).abs() <= tol).all())
