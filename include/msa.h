@@ -468,7 +468,9 @@ int msa_norm_rotate_axes(const msa_config_t* cfg, const void* q, int64_t q_strid
  *                    contents undefined on entry/exit
  * B, n_kv_heads <= 65535, B * M <= 2^25, Lpre, Lloc <= 2^28, and grids that hold the call (about 2^22 groups of 16 (token, head)
  * pairs of a KV head where a sequence brings fewer than 96 of them, else 2^24 tiles of 128).  Scores, their maximum and sum and the
- * outputs are accumulated in fp32; the softmax weights are rounded to bf16 for the second product (2^-8 relative).
+ * outputs are accumulated in fp32.  The softmax weights are carried as bf16 (hi, lo) pairs; where a sequence brings 96 (token, head)
+ * pairs of a KV head or more, and the batch 384, as bf16: an output is then off by up to 2^-8 of the weighted mean of |v| more than
+ * its own rounding.
  */
 size_t msa_prefix_attend_workspace_bytes(const msa_config_t* cfg, int32_t B, int32_t M, int32_t Lpre, int32_t Lloc);
 int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t M, const void* Kpre, const void* Vpre,

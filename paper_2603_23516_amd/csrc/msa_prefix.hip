@@ -6,15 +6,19 @@
 //   over the prefix  tiles of 128 columns, (token, query head) pairs of one KV head and of all sequences together, 32 to a wave, so
 //                    that a row is read once for all of them (per tile).  As encoded_tiled_kernel, without windows and runs: 32 key
 //                    and 32 value rows a step, global -> LDS asynchronously, two steps ahead, in n parts of which each takes every
-//                    n-th step.  Bound by memory with one tile (8 tokens over 65536 rows 55 us, 5.2 TB/s), by the matrix pipe and
-//                    the vector ALU with more: a step takes 0.85 us with one workgroup on a CU (64 dims: 0.56).
+//                    n-th step.  Bound by what follows on what in a wave, scores, weights and second product in turn, with one
+//                    workgroup on a CU: a step takes 0.96 us (8 tokens over 65536 rows 63 us, 4.3 TB/s).
 //   over the caches  sixteen columns of one (sequence, KV head); the rows go straight from memory into registers, dealt to the
-//                    four waves 32 at a time.  Bound by memory (64 tokens, up to 1024 rows each, 134 MB: 34 us).
+//                    four waves 32 at a time.  Bound by memory (64 tokens, 1024 rows each, 268 MB: 59 us).
 // Both leave (max, sum, output) parts by (token, head) row, which a launch joins.  The two kinds fill each other's gaps: 64 tokens
-// over 32768 rows 56 us, over the caches 34, both 69.  256 workgroups over the prefix, one to a CU, leave the others of a CU to
-// the caches: with 384, 512 and 768 the call of 80 us takes 81, 89 and 107 (without caches 66: 62, 60, 71).
-// Softmax weights are rounded to bf16 for the second product (2^-8 of themselves at most), their sum is taken before the rounding:
-// as (hi, lo) pairs they would take that product twice.
+// over 32768 rows 70 us, over up to 1024 rows of caches 44, both 87.  256 workgroups over the prefix, one to a CU, leave the
+// others of a CU to the caches: with 384, 512 and 768 the call of 87 us takes 85, 86 and 101 (without caches 70: 72, 68, 73), one of
+// 16 x 4 tokens over 8000 rows and up to 1500 of caches 40 and 43 for 34.
+// Softmax weights go into the second product as bf16 (hi, lo) pairs, off by 2^-16 of themselves at most, as in msa_window_attend's
+// kernel for single tokens: these are single tokens, or a few of them, in both kinds.  Over the caches the second half of that
+// product costs nothing beside the loads, over the prefix 8 us of 70 (weights rounded to bf16, off by 2^-8: 64 tokens over
+// 32768 rows 62 us, with their caches 80 for 87, 24 x 5 tokens of 64 dims over 4999 rows 18.2 for 19.2, 16 over 8000 27.4 for 27.2;
+// products and the other half's exponentials one by one in turn: the same as products first).
 #include "msa_prefix.h"
 
 #include <type_traits>
@@ -103,14 +107,14 @@ __device__ __forceinline__ void attend_rows(const uint16_t* K, const uint16_t* V
       for (int c = 0; c < NC; ++c) x.o[c] *= alpha;
     }
     const float m_use = x.m_run == -INFINITY ? 0.f : x.m_run;
-    uint32_t pw[4];
+    uint32_t hi[4], lo[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float p0 = __builtin_amdgcn_exp2f(w[2 * j] - m_use), p1 = __builtin_amdgcn_exp2f(w[2 * j + 1] - m_use);
       x.l_run += p0 + p1;
-      pw[j] = pack_bf16(p0, p1);
+      split_pack_bf16(p0, p1, hi[j], lo[j]);
     }
-    const bf16x8_t pb = as_bf16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+    const bf16x8_t ph = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3])), pl = as_bf16x8(make_uint4(lo[0], lo[1], lo[2], lo[3]));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int row = 4 * qd + (n >> 2);
@@ -119,7 +123,7 @@ __device__ __forceinline__ void attend_rows(const uint16_t* K, const uint16_t* V
       const unsigned char* vp = vt + row * ROW + (((2 * c + ((n & 3) >> 1)) ^ swz(row)) * 16) + 8 * (n & 1);
       const s16x4_t v0 = lds_read_tr16(vp), v1 = lds_read_tr16(vp + 16 * ROW);  // rows 16 apart: the same swizzle
       const bf16x8_t av = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-      x.o[c] = mfma16(av, pb, x.o[c]);
+      x.o[c] = mfma16(av, pl, mfma16(av, ph, x.o[c]));
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -260,21 +264,21 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, int x, unsigned
     // contraction slot j of slice sg and half hf is key 16 sg + (j % 4) + 8 (j / 4) + 4 hf: the lane's own registers
 #pragma unroll
     for (int sg = 0; sg < 2; ++sg) {
-      uint32_t pw[4];
+      uint32_t hi[4], lo[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * sg + 2 * i], a.qscale, -m_use));
         const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * sg + 2 * i + 1], a.qscale, -m_use));
         l_run += p0 + p1;
-        pw[i] = pack_bf16(p0, p1);
+        split_pack_bf16(p0, p1, hi[i], lo[i]);
       }
-      const bf16x8_t pb = as_bf16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+      const bf16x8_t ph = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3])), pl = as_bf16x8(make_uint4(lo[0], lo[1], lo[2], lo[3]));
       __builtin_amdgcn_sched_barrier(0);  // (the products of one half beside the exponentials of the other)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const s16x4_t v0 = lds_read_tr16(st + vat[t] + 16 * sg * ROW), v1 = lds_read_tr16(st + vat[t] + (16 * sg + 8) * ROW);
         const bf16x8_t av = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[t] = mfma32e(av, pb, o[t]);
+        o[t] = mfma32e(av, pl, mfma32e(av, ph, o[t]));
       }
     }
   };
@@ -481,11 +485,11 @@ PrefixPlan plan_prefix(const Dims& dm, int B, int M, int Lpre, int Lloc) {
   PrefixPlan p = {};
   // A sequence's tokens in tiles of their own, where they fill three quarters of one and the batch fills three.  us, so / with tiles of
   // all sequences' tokens, 32 / 8 heads of 128, 600 rows of a cache, a prefix of 2000 (16384):
-  //   1 sequence    M = 32 21 / 16 (37 / 30), 48 22 / 21 (43 / 41)
-  //   2 sequences   M = 24 21 / 21 (44 / 41), 48 27 / 29 (58 / 66)
-  //   8 sequences   M = 16 27 / 32 (99 / 75), 24 30 / 42 (91 / 115), 48 43 / 71 (155 / 202)
-  //   32 sequences  M = 12 58 / 72 (268 / 205), 24 63 / 115 (288 / 323), 48 98 / 204 (540 / 566)
-  //   4 sequences, 8 / 8 heads of 64, 4000   M = 64 22 / 16, 128 25 / 23
+  //   1 sequence    M = 32 21 / 17 (35 / 32), 48 21 / 20 (43 / 45)
+  //   2 sequences   M = 24 21 / 20 (43 / 44), 48 26 / 28 (56 / 75)
+  //   8 sequences   M = 16 26 / 29 (99 / 81), 24 29 / 46 (91 / 133), 48 41 / 66 (156 / 234)
+  //   32 sequences  M = 12 57 / 72 (269 / 246), 24 61 / 119 (287 / 386), 48 95 / 207 (560 / 746)
+  //   4 sequences, 8 / 8 heads of 64, 4000   M = 64 22 / 17, 128 24 / 25
   if (M * dm.r >= 96 && (long long)B * M * dm.r >= 384) {
     p.tiled = 1;
     p.tiles = plan_encoded_prefix(dm, B, M, Lpre, Lloc);

@@ -1,4 +1,5 @@
-"""Operators of a served cache at positions at the end of what 32 bits hold, against the plain definitions in 64 bits."""
+"""Operators of a served cache at positions at the end of what 32 bits hold, and the bits that attention over a prefix keeps: against the
+plain definitions in 64 bits."""
 import pytest
 import torch
 
@@ -57,3 +58,18 @@ def test_windows_past_32_bits_at_the_last_position(M):
         mass = msa.msa_attend_mass(cfg, q.cuda(), K.cuda(), lse, q_pos.cuda(), W)
         want, tol = C.attend_mass(q.double(), K.double(), lse.double().cpu(), q_pos, W, 0, 0, None, 1.0)
         assert bool(((mass.double().cpu() - want).abs() <= tol).all())
+
+
+# ---- attention over a prefix carries its weights as the other calls for few tokens do ----------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("B, M, Hq, Hkv, n_pre, L", [(1, 1, 8, 1, 200, 65), (5, 1, 4, 1, 900, 300), (40, 1, 4, 4, 300, 97), (3, 3, 6, 2, 130, 400),
+                                                     (1, 11, 8, 1, 3000, 30), (2, 95, 2, 2, 64, 120), (1, 40, 2, 1, 33, 41), (9, 1, 5, 1, 0, 700),
+                                                     (9, 1, 7, 1, 700, 0)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prefix_attend_of_few_tokens_keeps_pairs(B, M, Hq, Hkv, n_pre, L, d):
+    """Weights as bf16 (hi, lo) pairs, off by 2^-16 of themselves at most, wherever tokens do not fill tiles of their own."""
+    q, Kp, Vp, K, V = prefix_of._make(B, M, Hq, Hkv, d, n_pre, L, B + M)
+    q_pos = prefix_of._ends(B, M, L, n_pre)
+    dev = [t.cuda() if t.numel() else None for t in (Kp, Vp, K, V)]
+    out, lse = msa.msa_prefix_attend(_cfg(Hq, Hkv, d), q.cuda(), *dev, q_pos.cuda(), local_pos0=n_pre)
+    C.prefix_attend(q.double(), Kp.double(), Vp.double(), None, K.double(), V.double(), q_pos, n_pre).check(out, lse, 2.0 ** -16)
