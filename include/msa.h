@@ -380,7 +380,7 @@ int msa_unpack_kv4(const msa_config_t* cfg, const void* K4, const void* K4s, con
  * query of a token that sees none.  out and lse overlap no input.
  *   q         in   bf16 [B][M][Hq][d]
  *   Kloc,Vloc in   bf16 [B][Hkv][Lloc][d]
- *   window         >= 1; Lloc or more: causal attention;  sinks >= 0
+ *   window         >= 1; greater than every q_pos - local_pos0: causal attention (so is sinks >= Lloc);  sinks >= 0
  *   q_pos     in   int32 [B][M]
  *   out       out  bf16 [B][M][Hq][d]
  *   lse       out  fp32 [B][M][Hq], may be NULL
@@ -480,14 +480,16 @@ int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
 
 /*
  * The attention weight that every row of the local cache receives from the tokens of a call, added to what it has: what
- * msa_evict goes by.  Token (b, m) sees the rows that msa_window_attend shows it for this window, sinks, local_pos0 and q_pos
- * (window = Lloc or more: the cache rows that msa_prefix_attend and msa_sparse_attend4 show it), and with lse as the attention
- * over them, and over whatever else was in its softmax, left it
+ * msa_evict goes by.  Token (b, m) sees the rows that msa_window_attend shows it for this window, sinks, local_pos0 and q_pos,
+ * and with lse as the attention over them, and over whatever else was in its softmax, left it
  *     mass_out[b][g][t] = decay * mass[b][g][t] + sum over the tokens m that see row t and the heads h of group g of
  *                         exp( q[b][m][h][:] . Kloc[b][g][t][:] / sqrt(d) - lse[b][m][h] )
  * in fp32.  decay == 0, or mass == NULL: nothing of mass is read.  Every entry of mass_out is written, those of rows that no
  * token sees with decay * mass, 0 without it; in place with decay == 1 they are left as they are.  A token whose lse is -inf
  * (it saw nothing) adds nothing.  The same bits from call to call.  mass_out is mass itself or overlaps no input.
+ * Behind msa_prefix_attend and msa_sparse_attend4, which have no window, it takes a window greater than every q_pos - local_pos0,
+ * or sinks >= Lloc: a window slides by positions also past the cache's end, so that one of Lloc rows shows a token at q_pos -
+ * local_pos0 >= Lloc fewer rows than they do.
  *   q         in   bf16 [B][M][Hq][d]
  *   Kloc      in   bf16 [B][Hkv][Lloc][d]; rows up to the largest position of a sequence's tokens hold numbers
  *   q_pos     in   int32 [B][M]

@@ -735,7 +735,8 @@ def msa_attend_mass(cfg, q, Kloc, lse, q_pos, window, sinks=0, local_pos0=0, mas
                     stream=None):
     """q bf16 [B][M][Hq][d], Kloc bf16 [B][Hkv][Lloc][d], lse fp32 [B][M][Hq] as an attention over them left it, q_pos int32
     [B][M] -> out fp32 [B][Hkv][Lloc] = decay * mass + the attention weights that every row receives (window, sinks: of
-    msa_window_attend).  out may be mass."""
+    msa_window_attend; behind an attention without a window, a window greater than every q_pos - local_pos0, or sinks = Lloc).
+    out may be mass."""
     Hq, Hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     dev = _gpu(q, "q")
     window, sinks = _window(window, sinks)

@@ -73,3 +73,33 @@ def test_prefix_attend_of_few_tokens_keeps_pairs(B, M, Hq, Hkv, n_pre, L, d):
     dev = [t.cuda() if t.numel() else None for t in (Kp, Vp, K, V)]
     out, lse = msa.msa_prefix_attend(_cfg(Hq, Hkv, d), q.cuda(), *dev, q_pos.cuda(), local_pos0=n_pre)
     C.prefix_attend(q.double(), Kp.double(), Vp.double(), None, K.double(), V.double(), q_pos, n_pre).check(out, lse, 2.0 ** -16)
+
+
+# ---- weights behind an attention that has no window ----------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 40, 130])
+@pytest.mark.parametrize("over", [0, 1, 50, 10 ** 9])
+def test_mass_behind_an_attention_without_a_window(M, over):
+    """Tokens at the cache's end and past it see all of its rows: with a window greater than their rows, or with all rows among the
+    first ones, every head's weights add up to the cache's share of the softmax."""
+    B, Hq, Hkv, d, n_pre, L = 2, 4, 2, 64, 30, 97
+    r = Hq // Hkv
+    q, Kp, Vp, K, V = prefix_of._make(B, M, Hq, Hkv, d, n_pre, L, M)
+    q_pos = (n_pre + L - 1 + over - (torch.arange(M) % 7)).expand(B, M).contiguous().to(torch.int32)
+    cfg = _cfg(Hq, Hkv, d)
+    dev = [t.cuda() for t in (q, Kp, Vp, K, V, q_pos)]
+    lse = msa.msa_prefix_attend(cfg, *dev, local_pos0=n_pre)[1]
+    most = int(q_pos.max()) - n_pre
+    all_rows = dict(q=dev[0], Kloc=dev[3], lse=lse, q_pos=dev[5], local_pos0=n_pre)
+    a, b, c = (msa.msa_attend_mass(cfg, **all_rows, **kw) for kw in (dict(window=most + 1), dict(window=1, sinks=L), dict(window=2 ** 40)))
+    assert torch.equal(a, b) and torch.equal(a, c)
+    want, tol = C.attend_mass(q.double(), K.double(), lse.double().cpu(), q_pos, 2 ** 40, 0, n_pre, None, 1.0)
+    assert bool(((a.double().cpu() - want).abs() <= tol).all())
+    # the prefix' share, in 64 bits: what is left of each head's 1 is the cache's
+    x = torch.matmul(q.double().reshape(B, M, Hkv, r, d).movedim(2, 0).reshape(Hkv, -1, d), Kp.double().transpose(1, 2)) / d ** 0.5
+    y = lse.double().cpu().reshape(B, M, Hkv, r).movedim(2, 0).reshape(Hkv, -1, 1)
+    left = (1 - torch.exp(x - y).sum(-1)).reshape(Hkv, B, M * r).sum(-1).T
+    # lse is off by 2^-16 (S + 1) + 2^-22 |lse| with S < 32 (the bound of plain64's Attended), and with it every share
+    assert bool(((a.double().cpu().sum(-1) - left).abs() <= tol.sum(-1) + M * r * 2.0 ** -10).all())
+    if over >= L:
+        assert float(msa.msa_attend_mass(cfg, **all_rows, window=L).abs().max()) == 0.0      # a window of Lloc rows has slid past all of them
