@@ -265,7 +265,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int chunks
 
 // In place: a workgroup has 64 bytes of every row of a (sequence, KV head), so that no other one's rows are in its way.  Row j comes
 // from row rows[j] >= j: a turn's rows are all in registers before the first of them is stored, and what later turns read lies
-// behind what this one stores.
+// behind what this one stores.  (32 sequences of 8 heads of 128, 4224 rows cut to 4096, 1.07 GB in and out, 259 us, 4.1 TB/s, where
+// the kernel above takes 177; of 2112 to 4224 rows 28; one sequence of 16384 cut to 4096 13.5, for 5.5.  The rows as uint4 in an array
+// went to 64 KiB of LDS: 273, 39, 18.)
 template <int D>
 __global__ __launch_bounds__(1024) void evict_move_in_place_kernel(EvictArgs a) {
   constexpr int LPR = 4, RPB = 1024 / LPR, TURNS = 4, SLICES = D * 2 / 64;
@@ -282,15 +284,15 @@ __global__ __launch_bounds__(1024) void evict_move_in_place_kernel(EvictArgs a) 
       row[t] = j < a.keep ? rows[j] : -1;
       if (row[t] == j) row[t] = -1;  // stays where it is
     }
-    uint4 v[TURNS];
+    u32x4_t v[TURNS];
 #pragma unroll
     for (int t = 0; t < TURNS; ++t)
-      if (row[t] >= 0) v[t] = *reinterpret_cast<const uint4*>(x + (long long)row[t] * D);
+      if (row[t] >= 0) v[t] = *reinterpret_cast<const u32x4_t*>(x + (long long)row[t] * D);
     wait_stores_done();  // (the loads too)
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < TURNS; ++t)
-      if (row[t] >= 0) *reinterpret_cast<uint4*>(x + (long long)(j0 + t * RPB + jt) * D) = v[t];
+      if (row[t] >= 0) *reinterpret_cast<u32x4_t*>(x + (long long)(j0 + t * RPB + jt) * D) = v[t];
   }
 }
 
