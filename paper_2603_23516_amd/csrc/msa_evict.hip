@@ -25,7 +25,8 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
   return orderable(x == 0.f ? 0.f : x);
 }
 
-// REGS: rows of a thread, held in registers, of at most 1024 REGS in all; 0: any number, read again for every digit.
+// REGS: rows of a thread, held in registers, of at most 1024 REGS in all; 0: any number, read again for every digit (20000 rows 35 us
+// for 23, 32768 58 for 33).
 template <int REGS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int WAVES = kSelectThreads / 64;
@@ -66,21 +67,48 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   };
   static_assert(REGS <= 32, "a bit per row");
   // a wave's rows are `blocks` times 64 in a row, from w0 on; without registers the workgroup's are taken 1024 at a time
-  const int blocks = (n + kSelectThreads - 1) / kSelectThreads, w0 = wave * blocks * 64 + lane;
+  const int blocks = (n + kSelectThreads - 1) / kSelectThreads;
+  int w0 = wave * blocks * 64 + lane;
+  // Beside the weights their order and whether a row is in the middle: of up to 16 rows kept as well; of 32 worked out again where it is
+  // wanted, from the weights and a bit per row (kept, they went to scratch memory: 16 x 8 heads of 32768 rows 45 us for 35).
+  constexpr bool KEPT = REGS <= 16;
   float x[REGS > 0 ? REGS : 1];
-  uint32_t key[REGS > 0 ? REGS : 1];
+  uint32_t keys[KEPT && REGS > 0 ? REGS : 1], inner = 0u;
   if constexpr (REGS > 0) {
 #pragma unroll
     for (int u = 0; u < REGS; ++u) x[u] = u < blocks && w0 + 64 * u < n ? mass[w0 + 64 * u] : 0.f;
 #pragma unroll
-    for (int u = 0; u < REGS; ++u) key[u] = weight_key(x[u]);
+    for (int u = 0; u < REGS; ++u) {
+      if constexpr (KEPT)
+        keys[u] = weight_key(x[u]);
+      else
+        inner |= u < blocks && w0 + 64 * u >= m0 && w0 + 64 * u < m1 ? 1u << u : 0u;
+    }
   }
+  auto again = [&](auto& v) {  // (what follows from v is not kept from here on)
+    if constexpr (!KEPT) asm volatile("" : "+v"(v));
+  };
+  auto key = [&](int u) {
+    if constexpr (KEPT) return keys[u];
+    again(x[u]);
+    return weight_key(x[u]);
+  };
+  auto in_middle = [&](int u) -> bool {
+    if constexpr (KEPT) return w0 + 64 * u >= m0 && w0 + 64 * u < m1;  // (of rows that are its own)
+    return (inner >> u) & 1u;
+  };
   auto each = [&](auto f) {  // the weights of this thread's rows in the middle
     if constexpr (REGS > 0) {
+      again(inner);
+      again(w0);
 #pragma unroll
       for (int u = 0; u < REGS; ++u) {
         const int i = w0 + 64 * u;
-        if (u < blocks && i >= m0 && i < m1) f(key[u], i);
+        if constexpr (KEPT) {  // (as a condition and not a value: 22 us for 23 over 16384 rows)
+          if (u < blocks && i >= m0 && i < m1) f(keys[u], i);
+        } else {
+          if (in_middle(u)) f(key(u), i);
+        }
       }
     } else {
       for (int i = m0 + tid; i < m1; i += kSelectThreads) f(weight_key(mass[i]), i);
@@ -181,30 +209,33 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   if constexpr (REGS > 0) {
     if (ties > 0) {
       int c = 0;
+      again(inner);
 #pragma unroll
-      for (int u = 0; u < REGS; ++u) {
-        const int i = w0 + 64 * u;
-        if (u < blocks) c += __popcll(__ballot(i >= m0 && i < m1 && key[u] == kth));
-      }
+      for (int u = 0; u < REGS; ++u)
+        if (u < blocks) c += __popcll(__ballot(in_middle(u) && key(u) == kth));
       total(c, tied_before);
     }
     uint32_t kept = 0u;  // bit u: row w0 + 64 u stays
     int c = 0, at;
+    again(inner);
+    again(w0);
 #pragma unroll
     for (int u = 0; u < REGS; ++u) {
       if (u >= blocks) continue;
       const int i = w0 + 64 * u;
-      const bool middle = i >= m0 && i < m1;
-      bool stays = i < n && (!middle || key[u] > kth || (key[u] == kth && i <= tie_row));
+      const bool middle = in_middle(u);
+      const uint32_t k = key(u);
+      bool stays = i < n && (!middle || k > kth || (k == kth && i <= tie_row));
       if (ties > 0) {
-        const unsigned long long tie = __ballot(middle && key[u] == kth);
-        stays |= middle && key[u] == kth && tied_before + __popcll(tie & ((1ull << lane) - 1ull)) < ties;
+        const unsigned long long tie = __ballot(middle && k == kth);
+        stays |= middle && k == kth && tied_before + __popcll(tie & ((1ull << lane) - 1ull)) < ties;
         tied_before += __popcll(tie);
       }
       kept |= stays ? 1u << u : 0u;
       c += __popcll(__ballot(stays));
     }
     total(c, at);  // (behind its barrier every weight is in a register)
+    again(w0);
 #pragma unroll
     for (int u = 0; u < REGS; ++u) {
       if (u >= blocks) continue;
