@@ -506,11 +506,15 @@ _axes_arrays = {}
 def _axes_array(axes, half):
     """A host array of the axis of every pair; the last ones asked for are kept (a model has one, and building it takes longer
     than the call)."""
-    key = tuple(axes)
+    axes = [*axes]
+    try:
+        key = bytes(axes)  # (refuses what is no integer; a tuple of 0.0 would be found as one of 0)
+    except (TypeError, ValueError):
+        key = None
     arr = _axes_arrays.get(key)
     if arr is None:
-        if not all(isinstance(x, int) and 0 <= x < MSA_MAX_AXES for x in key):
-            raise ValueError(f"axes: expected integers in [0, {MSA_MAX_AXES}), got {key}")
+        if key is None or max(key, default=0) >= MSA_MAX_AXES:
+            raise ValueError(f"axes: expected integers in [0, {MSA_MAX_AXES}), got {axes}")
         if len(_axes_arrays) >= 64:
             _axes_arrays.clear()
         arr = _axes_arrays[key] = (ctypes.c_int32 * len(key))(*key)
