@@ -497,8 +497,8 @@ int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
  *   mass      in   fp32 [B][Hkv][Lloc], may be NULL
  *   decay          0 to 1
  *   mass_out  out  fp32 [B][Hkv][Lloc]
- *   workspace      >= msa_attend_mass_workspace_bytes(cfg, B, M, Lloc, window, sinks), which does not fall as Lloc, window or
- *                  sinks grow; contents undefined on entry/exit
+ *   workspace      >= msa_attend_mass_workspace_bytes(cfg, B, M, Lloc, window, sinks), which does not fall as Lloc grows and is the
+ *                  same for every window and sinks; contents undefined on entry/exit
  * B, n_kv_heads <= 65535, B * M <= 2^25, Lloc <= 2^28, and fewer than 2^24 blocks of 128 rows in all (the cache of a (sequence, KV head)
  * counted as one block more).
  */

@@ -646,7 +646,7 @@ int msa_prefix_attend(const msa_config_t* cfg, const void* q, int32_t B, int32_t
 static int plan_mass_of(const Dims& dm, int32_t B, int32_t M, int32_t Lloc, int32_t window, int32_t sinks, MassPlan* pl) {
   if (B < 1 || M < 1 || Lloc < 1 || window < 1 || sinks < 0) return MSA_ERR_INVALID_ARG;
   if (!encoded_sizes_ok(dm, B, M) || Lloc > (1 << 28)) return MSA_ERR_UNSUPPORTED;
-  *pl = plan_mass(dm, B, M, Lloc, window, sinks);
+  *pl = plan_mass(dm, B, M, Lloc);
   return pl->ws_bytes != 0 ? MSA_OK : MSA_ERR_UNSUPPORTED;
 }
 

@@ -225,7 +225,7 @@ struct MassPlan {
   int n_tiles, n_parts, tpw;
   size_t ws_bytes;
 };
-MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks);
+MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc);
 int launch_mass(const Dims& dm, const MassPlan& pl, MassArgs a, int B, void* ws, hipStream_t st);
 
 // The heaviest rows of a cache (msa_evict.hip).

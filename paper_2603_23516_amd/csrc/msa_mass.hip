@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256) void mass_join_kernel(MassArgs a, const float*
   a.out[at] = v;
 }
 
-MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks) {
+MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc) {
   MassPlan p = {};
   const long long pairs = (long long)B * dm.Hkv;
   p.ws_bytes = 256;
@@ -376,6 +376,7 @@ MassPlan plan_mass(const Dims& dm, int B, int M, int Lloc, int window, int sinks
     p.ws_bytes = 0;
     return p;
   }
+  // (the parts are of all columns, whatever the window: which of them a tile meets the kernel finds from their positions)
   // (tiles in parts are fewer than kMassItems, so less than twice as many workgroups in all; no less for a longer cache)
   const long long sums = most * pairs * Lloc, bound = 2 * kMassItems * kMassWaves * kMassRows;
   if (most > 1) p.ws_bytes = round_up256((size_t)(sums < bound ? sums : bound) * sizeof(float));

@@ -103,3 +103,9 @@ def test_mass_behind_an_attention_without_a_window(M, over):
     assert bool(((a.double().cpu().sum(-1) - left).abs() <= tol.sum(-1) + M * r * 2.0 ** -10).all())
     if over >= L:
         assert float(msa.msa_attend_mass(cfg, **all_rows, window=L).abs().max()) == 0.0      # a window of Lloc rows has slid past all of them
+
+
+def test_workspace_of_masses_is_the_same_for_every_window():
+    for B, M, L in ((1, 1, 1), (4, 509, 5003), (1, 9000, 9000), (40, 1, 8192)):
+        sizes = {msa.attend_mass_workspace_bytes(_cfg(32, 8, 128), B, M, L, W, S) for W in (1, 1000, L, 2 ** 40) for S in (0, 16, L, 2 ** 40)}
+        assert len(sizes) == 1 and min(sizes) >= 256
