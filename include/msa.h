@@ -243,7 +243,9 @@ int msa_score_topk_noalloc(const msa_config_t* cfg, const void* q_route, int32_t
  *     out[b][m][h][:] = softmax_j( RoPE(q[b][m][h][:], q_pos[b][m]) . key_j / sqrt(d) ) . value_j
  *     lse[b][m][h]    = log sum_j exp( ... )          (natural log; -inf and out = 0 if no key is visible)
  * RoPE pairs element u with u + d/2, angle p * base^(-2u/d).  Positions restart at 0 in every document
- * (with cfg->bank_keys_rotated the bank keys are taken as stored, un-rotated here);
+ * (with cfg->bank_keys_rotated the bank keys are taken as stored, un-rotated here).  Local row t is the token at position
+ * local_pos0 + t: of a cache whose rows are told apart from positions (msa_norm_rotate_axes with rows, msa_evict) the keys
+ * would be turned to positions that are not theirs, and nothing here can tell; msa_layers_step alike.
  * idx == -1 (or any id outside [0, N)) marks "no document"; a document listed twice is attended twice.
  *   q         in   bf16 [B][M][Hq][d]
  *   K, V      in   bf16 [N][Hkv][G][d]
@@ -436,6 +438,7 @@ int msa_sparse_attend4(const msa_config_t* cfg, const void* q, int32_t B, int32_
  * A token whose first position is negative is padding, nothing of it is written (its other positions are not read); the other
  * tokens' positions may have any sign on the further axes.  A row outside [0, Lloc) is none: the query alone is written.  Of a
  * row that two tokens claim the contents are undefined.
+ * A cache whose rows are not its positions is for the calls that read rows as they are, as under msa_evict.
  *   pos       in   int32 [B][M][n_axes], 1 <= n_axes <= MSA_MAX_AXES
  *   axes      in   HOST int32 [d/2], each in [0, n_axes); read before the call returns
  *   rows      in   int32 [B][M], may be NULL
@@ -518,6 +521,10 @@ int msa_attend_mass(const msa_config_t* cfg, const void* q, int32_t B, int32_t M
  *     rows[b][g][j]    = -1 for j >= n
  *     mass_out[b][g][j] = 0 for j >= min(n, keep): a row that is appended there begins without weight
  * Rows of Kout and Vout from min(n, keep) on are left as they are.  The caller's new lengths are min(lens, keep).
+ * A cut cache has rows and no positions any longer.  msa_window_attend, msa_prefix_attend, msa_sparse_attend4 and msa_attend_mass read
+ * it, with keys that carry their positions: a token's q_pos is local_pos0 plus the row of its own key, and a window counts rows.
+ * msa_norm_rotate_axes writes it, with rows.  msa_norm_rotate would take a position for the row, and msa_sparse_attend and
+ * msa_layers_step, which turn row t to position local_pos0 + t, must not be given it: the keys of their caches are raw.
  *   Kloc,Vloc   in   bf16 [B][Hkv][Lloc][d]
  *   mass        in   fp32 [B][Hkv][Lloc]
  *   lens        in   int32 [B]

@@ -527,7 +527,7 @@ def msa_norm_rotate_axes(cfg, q, k, v, pos, axes, Kloc, Vloc, rows=None, q_weigh
                          local_pos0=0, q_out=None, stream=None):
     """msa_norm_rotate with positions of several axes: pos int32 [B][M][A], pair u of a head turned by the position of axis
     axes[u] (d/2 integers).  Keys and values go into rows rows[b][m] (int32 [B][M]) of Kloc, Vloc, None: pos[b][m][0] -
-    local_pos0."""
+    local_pos0.  A cache with rows of its own is not for msa_sparse_attend (see msa_evict)."""
     if pos.dim() != 3:
         raise ValueError("msa_norm_rotate_axes: expected pos [B][M][A]")
     A = pos.shape[2]
@@ -762,7 +762,10 @@ def msa_attend_mass(cfg, q, Kloc, lse, q_pos, window, sinks=0, local_pos0=0, mas
 def msa_evict(cfg, Kloc, Vloc, mass, lens, keep, sinks=0, recent=0, Kout=None, Vout=None, mass_out=None, rows=None, stream=None):
     """Kloc, Vloc bf16 [B][Hkv][Lloc][d] with lens int32 [B] rows each, mass fp32 [B][Hkv][Lloc]: per KV head the first `sinks`
     rows, the last `recent` and the heaviest of the others stay, `keep` in all -> (Kout, Vout, mass_out, rows int32
-    [B][Hkv][keep]).  In place without Kout, Vout and mass_out, which come together ([B][Hkv][Lout]..., Lout >= keep)."""
+    [B][Hkv][keep]).  In place without Kout, Vout and mass_out, which come together ([B][Hkv][Lout]..., Lout >= keep).
+    A cut cache is read by row, its keys carrying their positions: by msa_window_attend, msa_prefix_attend, msa_sparse_attend4 and
+    msa_attend_mass (q_pos: local_pos0 and the row of a token's own key), not by msa_sparse_attend and the layers built on it, which turn
+    row t to position local_pos0 + t; msa_norm_rotate_axes appends to it with `rows`."""
     Hkv, d = cfg.n_kv_heads, cfg.head_dim
     dev = _gpu(Kloc, "Kloc")
     if Kloc.dim() != 4 or (Kout is not None and Kout.dim() != 4):

@@ -120,8 +120,9 @@ class LayerStack:
 
     # ---- online: one batch of query tokens through every routed layer --------------------------------------
     def step(self, qs, Klocs, Vlocs, pos0, q_pos, outs, lses, overlap=True):
-        """qs[l] bf16 [B][M][Hq][d]: the routing/attention query of layer l; Klocs[l], Vlocs[l] its local cache;
-        outs[l], lses[l] receive its attention output (None: not wanted).  overlap=False runs everything on one stream.
+        """qs[l] bf16 [B][M][Hq][d]: the routing/attention query of layer l; Klocs[l], Vlocs[l] its local cache, raw keys with
+        row t at position pos0 + t (not one that msa_evict has cut); outs[l], lses[l] receive its attention output (None: not
+        wanted).  overlap=False runs everything on one stream.
         One host thread at a time: the stack's workspaces, selections and events are shared by its steps.  Steps of the
         "hbm" tier from different streams follow each other; replays of a captured step are ordered by whoever replays it."""
         cur = torch.cuda.current_stream(self.dev)
