@@ -13,7 +13,7 @@
 // A weight in bf16 is off by 2^-8 of itself at most, either way, and the output by what that comes to; their sum is taken before
 // the rounding.  As (hi, lo) pairs, as the single-token kernel carries them at no cost, they would take the second product twice:
 // relative error against 64 bits 0.0023 -> 0.0017 (what rounding the output costs by itself), window_prefill 407 -> 535 us,
-// window_chunk_64 25 -> 28, attend4_question 168 -> 211.
+// window_chunk_64 25 -> 28, attend4_question 168 -> 211, prefix_question 300 -> 396.
 // Masks are worked out only in steps that some column of the wave does not see whole; steps that a wave does not see at all
 // are passed over.
 //

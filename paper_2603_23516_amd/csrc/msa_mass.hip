@@ -13,7 +13,7 @@
 // mass_tiled_kernel, more columns: a wave keeps 32 rows in registers, the queries come by in steps of 32 columns through LDS, with them
 // the log-sum and the position of every column.  Per 32 x 32 weights stand 8 products of 32x32x16 (d = 128) against 80 vector
 // instructions, of which 48 are the weights (fma, exponential, sum) and 16 of these take twice the time: 8192 tokens of 32 / 8 heads of
-// 128 (275 GFLOP) 330 us, 0.83 PFLOP/s, vector ALU 74 % and matrix pipe 46 % busy.  64 rows to a wave would halve what is not
+// 128 (275 GFLOP) 330 to 345 us by card, 0.80 to 0.83 PFLOP/s, vector ALU 74 % and matrix pipe 46 % busy.  64 rows to a wave would halve what is not
 // the weights and leave two waves to a SIMD for four: 367.  The columns that a tile of 128 rows needs are shared out to several
 // workgroups, whose sums mass_join_kernel adds in order (2048 workgroups in all: with 1024 362, with 4096 333 and short calls up to
 // 40 % longer; eight steps at least to a part).

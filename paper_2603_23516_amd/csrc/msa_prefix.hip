@@ -1,7 +1,7 @@
 // msa_prefix_attend: one softmax over the rows of a prefix that all sequences share and over the rows of a sequence's own cache.
 //
 // Where a sequence has tokens enough to fill tiles of its own, encoded_tiled_kernel takes them over the prefix and the cache in one
-// go (8 questions of 128 tokens, 32 / 8 heads of 128, over 16384 + 640 rows 298 us, 0.95 PFLOP/s).  With fewer, one launch has
+// go (8 questions of 128 tokens, 32 / 8 heads of 128, over 16384 + 640 rows 298 to 308 us by card, 0.92 to 0.95 PFLOP/s).  With fewer, one launch has
 // workgroups of two kinds:
 //   over the prefix  tiles of 128 columns, (token, query head) pairs of one KV head and of all sequences together, 32 to a wave, so
 //                    that a row is read once for all of them (per tile).  As encoded_tiled_kernel, without windows and runs: 32 key
